@@ -1,6 +1,7 @@
 """MI355X-native banded Sinkhorn attention (forward + exact surrogate backward).
 
-`binding` is the thin ctypes layer over the C ABI of include/sinkhorn_attn.h;
+`binding` is the thin ctypes layer over the C ABI of include/sinkhorn_attn.h, `layer` over
+that of include/sinkhorn_attn_layer.h (layer norm, rotary positions, softmax attention on the band);
 `workloads` holds the seeded synthetic inputs; `build` compiles the library.
 """
 from .binding import (SinkhornAttnError, sinkhorn_attn_base_vjp, sinkhorn_attn_bwd,
@@ -12,3 +13,6 @@ from .binding import (SinkhornAttnError, sinkhorn_attn_base_vjp, sinkhorn_attn_b
                       sinkhorn_attn_select_tail_depth, sinkhorn_attn_select_workspace_bytes, sinkhorn_attn_set_fused_half_steps, sinkhorn_attn_set_split_min_edges, sinkhorn_attn_set_streams, sinkhorn_attn_step,
                       sinkhorn_attn_step_static,
                       sinkhorn_attn_strerror, sinkhorn_attn_workspace_bytes)
+from .layer import (ska_layer_norm_bwd, ska_layer_norm_fwd, ska_layer_norm_workspace_bytes, ska_rope_bwd,  # noqa: F401
+                    ska_rope_frequencies, ska_rope_fwd, ska_softmax_attn_bwd, ska_softmax_attn_fwd,
+                    ska_softmax_attn_workspace_bytes)

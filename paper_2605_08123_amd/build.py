@@ -19,9 +19,13 @@ HIPCC_FLAGS = [
     "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-I" + os.path.join(ROOT, "include"),
 ]
-# Objects: the library, and the step kernel's instances by storage type and head dimension (most of it).  Compiled side by side.
+# Objects: the library, the step kernel's instances by storage type and head dimension (most of it), and the operators of the layer
+# around it.  Compiled side by side.
 UNITS = [("sinkhorn_attn", "sinkhorn_attn.hip", [])] + [
     (f"steps_{name}_{d}", "ska_step_launch.hip", [f"-DSKA_T={t}", f"-DSKA_D={d}", f"-DSKA_NAME=ska_launch_steps_{name}_{d}"])
+    for name, t in (("bf16", "__bf16"), ("f32", "float")) for d in (64, 32, 128)] + [
+    ("layer_norm", "ska_layer_norm.hip", []), ("rope", "ska_rope.hip", []), ("softmax", "ska_softmax.hip", [])] + [
+    (f"softmax_{name}_{d}", "ska_softmax_launch.hip", [f"-DSKA_T={t}", f"-DSKA_D={d}", f"-DSKA_NAME=ska_launch_softmax_{name}_{d}"])
     for name, t in (("bf16", "__bf16"), ("f32", "float")) for d in (64, 32, 128)]
 
 

@@ -1,0 +1,179 @@
+// Softmax attention on a band, forward and gradient: the host side (sinkhorn_attn_layer.h; kernels in ska_softmax.h).
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "sinkhorn_attn_layer.h"
+#include "ska_softmax_launch.h"
+
+namespace {
+
+struct SmProblem {
+    int B, Hq, Hk, Lq, Lk, d, W, causal, dtype;
+    int G() const { return Hq / Hk; }
+    long R() const { return (long)Lq * G(); }
+    long N() const { return (long)B * Hk; }
+};
+int check(const SmProblem &p)
+{
+    if (p.B < 1 || p.Hq < 1 || p.Hk < 1 || p.Lq < 1 || p.Lk < 1 || p.W < 0 || p.Hq % p.Hk) return SKA_EINVAL;
+    if (p.d != 32 && p.d != 64 && p.d != 128) return SKA_EUNSUPPORTED;
+    if (p.dtype != SKA_F32 && p.dtype != SKA_BF16) return SKA_EUNSUPPORTED;
+    if (p.Lq > 1 << 24 || p.Lk > 1 << 24 || p.N() > 65535 || p.R() > 1 << 27) return SKA_EUNSUPPORTED;
+    return SKA_OK;
+}
+
+// How one kernel of a call is launched: wavefronts per workgroup, blocks of owners, parts of a walk
+struct SmGrid { int nw; long blocks; int parts; };
+// owners: rows of the side that is kept; walk: rows of the other side that a block may meet, at most
+SmGrid sm_grid(const SmProblem &p, long owners, long walk)
+{
+    SmGrid g{4, 0, 1};
+    if (owners <= 32) g.nw = 1;
+    g.blocks = (owners + 32 * g.nw - 1) / (32 * g.nw);
+    const long tile = p.dtype == SKA_BF16 ? 64 : 32, tiles = (walk + tile - 1) / tile, waves = g.blocks * p.N() * g.nw;
+    if (waves < 1024) g.parts = (int)std::max(1L, std::min({2048 / waves, tiles / 4, 256L}));
+    return g;
+}
+long walk_of_rows(const SmProblem &p)
+{
+    const long W = std::min<long>(p.W, p.Lk);
+    return std::min<long>(p.Lk, (p.Lq < 128 ? p.Lq : 128) + W + (p.causal ? 0 : W));
+}
+long walk_of_keys(const SmProblem &p)
+{
+    const long W = std::min<long>(p.W, p.Lq);
+    return std::min<long>(p.Lq, (p.Lk < 128 ? p.Lk : 128) + W + (p.causal ? 0 : W)) * p.G();
+}
+SmGrid rows_grid(const SmProblem &p) { return sm_grid(p, p.R(), walk_of_rows(p)); }
+SmGrid keys_grid(const SmProblem &p) { return sm_grid(p, p.Lk, walk_of_keys(p)); }
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+size_t delta_bytes(const SmProblem &p) { return up256((size_t)p.N() * p.R() * sizeof(float)); }
+size_t part_lse_bytes(const SmProblem &p, const SmGrid &g) { return g.parts > 1 ? up256((size_t)g.parts * p.N() * p.R() * sizeof(float)) : 0; }
+size_t ws_fwd(const SmProblem &p)
+{
+    const SmGrid g = rows_grid(p);
+    return g.parts > 1 ? part_lse_bytes(p, g) + (size_t)g.parts * p.N() * p.R() * p.d * sizeof(float) : 0;
+}
+size_t ws_bwd(const SmProblem &p)
+{
+    const SmGrid r = rows_grid(p), k = keys_grid(p);
+    const size_t pr = r.parts > 1 ? (size_t)r.parts * p.N() * p.R() * p.d : 0, pk = k.parts > 1 ? (size_t)k.parts * p.N() * p.Lk * 2 * p.d : 0;
+    return delta_bytes(p) + std::max(pr, pk) * sizeof(float);   // (one after the other)
+}
+
+// strides in bytes multiples of 16; SKA_EINVAL where they cannot be strides, SKA_EUNSUPPORTED where the kernels cannot use them
+int tensor_of(SmTensor &t, const void *p, const ska_strides *s, int B, int H, long L, int d, int dtype, bool out)
+{
+    if (!p) return SKA_EINVAL;
+    t.p = p;
+    if (s) {
+        t.b = (long)s->b; t.h = (long)s->h; t.l = (long)s->l;
+        if (t.b < 0 || t.h < 0 || t.l < 0) return SKA_EINVAL;
+        if (out && ((B > 1 && !t.b) || (H > 1 && !t.h) || (L > 1 && !t.l))) return SKA_EINVAL;
+        if (B == 1) t.b = 0;   // (never stepped over, whatever it says)
+        if (H == 1) t.h = 0;
+        if (L == 1) t.l = 0;
+    } else {
+        t.l = d; t.h = L * d; t.b = t.h * H;
+    }
+    const long e = dtype == SKA_F32 ? 4 : 2;
+    const unsigned long off = (unsigned long)reinterpret_cast<uintptr_t>(p) | (unsigned long)((t.b | t.h | t.l) * e);
+    return off & 15 ? SKA_EUNSUPPORTED : SKA_OK;
+}
+
+int launch(int what, const SmProblem &p, const SmGrid &g, SmArgs a, hipStream_t st)
+{
+    a.parts = g.parts;
+    a.blocks = (int)g.blocks;
+    const long total = g.blocks * g.parts * p.N();
+    if (total > 0x7ffffff0L) return SKA_EUNSUPPORTED;
+    a.total = (int)total;
+    const long other = what == SM_DKV ? p.Lq : p.Lk;
+    a.order = 2L * p.W + 1 < other / 2 ? SM_NEIGHBOURS : what == SM_DKV && p.causal ? SM_FIRST_FIRST : SM_LAST_FIRST;
+    const auto f = p.dtype == SKA_F32 ? (p.d == 32 ? ska_launch_softmax_f32_32 : p.d == 64 ? ska_launch_softmax_f32_64 : ska_launch_softmax_f32_128)
+                                      : (p.d == 32 ? ska_launch_softmax_bf16_32 : p.d == 64 ? ska_launch_softmax_bf16_64 : ska_launch_softmax_bf16_128);
+    return f(what, g.nw, &a, st);
+}
+
+SmArgs args_of(const SmProblem &p, float eps, float *lse, const int *start_q, const int *len_q, const int *len_k, const unsigned char *mask_q,
+               const unsigned char *mask_k)
+{
+    SmArgs a{};
+    a.lse = lse;
+    a.start = start_q; a.len_q = len_q; a.len_k = len_k; a.mask_q = mask_q; a.mask_k = mask_k;
+    a.B = p.B; a.Hk = p.Hk; a.G = p.G(); a.Lq = p.Lq; a.Lk = p.Lk; a.causal = p.causal;
+    a.W = std::min(p.W, 1 << 26);   // (positions are below 2^25: this reaches everything, and sums with it stay in 32 bits)
+    a.cs = 1.f / (eps * sqrtf((float)p.d));
+    a.c2 = a.cs * LOG2E;
+    return a;
+}
+bool eps_ok(float eps) { return eps > 0.f && isfinite(eps); }
+
+}  // namespace
+
+extern "C" {
+
+size_t ska_softmax_attn_workspace_bytes(int backward, int B, int Hq, int Hk, int Lq, int Lk, int d, int W, int causal, int dtype)
+{
+    const SmProblem p{B, Hq, Hk, Lq, Lk, d, W, causal, dtype};
+    if (check(p) != SKA_OK) return 0;
+    return backward ? ws_bwd(p) : ws_fwd(p);
+}
+
+int ska_softmax_attn_fwd(const void *Q, const ska_strides *q_strides, const void *K, const ska_strides *k_strides, const void *V,
+                         const ska_strides *v_strides, void *O, const ska_strides *o_strides, float *LSE, const int *start_q,
+                         const int *len_q, const int *len_k, const unsigned char *mask_q, const unsigned char *mask_k, int B, int Hq,
+                         int Hk, int Lq, int Lk, int d, int W, int causal, float eps, int dtype, void *workspace, size_t workspace_bytes,
+                         void *stream)
+{
+    const SmProblem p{B, Hq, Hk, Lq, Lk, d, W, causal, dtype};
+    if (!LSE || !eps_ok(eps)) return SKA_EINVAL;
+    int rc = check(p);
+    if (rc != SKA_OK) return rc;
+    SmArgs a = args_of(p, eps, LSE, start_q, len_q, len_k, mask_q, mask_k);
+    if ((rc = tensor_of(a.q, Q, q_strides, B, Hq, Lq, d, dtype, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.k, K, k_strides, B, Hk, Lk, d, dtype, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.v, V, v_strides, B, Hk, Lk, d, dtype, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.oq, O, o_strides, B, Hq, Lq, d, dtype, true)) != SKA_OK) return rc;
+    const size_t need = ws_fwd(p);
+    if (need && (!workspace || workspace_bytes < need)) return SKA_EWORKSPACE;
+    if (reinterpret_cast<uintptr_t>(workspace) & 15) return SKA_EINVAL;
+    const SmGrid g = rows_grid(p);
+    a.part_lse = static_cast<float *>(workspace);
+    a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + part_lse_bytes(p, g));
+    return launch(SM_FWD, p, g, a, static_cast<hipStream_t>(stream));
+}
+
+int ska_softmax_attn_bwd(const void *Q, const ska_strides *q_strides, const void *K, const ska_strides *k_strides, const void *V,
+                         const ska_strides *v_strides, const void *O, const ska_strides *o_strides, const void *dO,
+                         const ska_strides *do_strides, const float *LSE, void *dQ, const ska_strides *dq_strides, void *dK,
+                         const ska_strides *dk_strides, void *dV, const ska_strides *dv_strides, const int *start_q, const int *len_q,
+                         const int *len_k, const unsigned char *mask_q, const unsigned char *mask_k, int B, int Hq, int Hk, int Lq,
+                         int Lk, int d, int W, int causal, float eps, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const SmProblem p{B, Hq, Hk, Lq, Lk, d, W, causal, dtype};
+    if (!LSE || !eps_ok(eps)) return SKA_EINVAL;
+    int rc = check(p);
+    if (rc != SKA_OK) return rc;
+    SmArgs a = args_of(p, eps, const_cast<float *>(LSE), start_q, len_q, len_k, mask_q, mask_k);
+    if ((rc = tensor_of(a.q, Q, q_strides, B, Hq, Lq, d, dtype, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.k, K, k_strides, B, Hk, Lk, d, dtype, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.v, V, v_strides, B, Hk, Lk, d, dtype, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.o, O, o_strides, B, Hq, Lq, d, dtype, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.g, dO, do_strides, B, Hq, Lq, d, dtype, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.oq, dQ, dq_strides, B, Hq, Lq, d, dtype, true)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.ok, dK, dk_strides, B, Hk, Lk, d, dtype, true)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.ov, dV, dv_strides, B, Hk, Lk, d, dtype, true)) != SKA_OK) return rc;
+    if (!workspace || workspace_bytes < ws_bwd(p)) return SKA_EWORKSPACE;
+    if (reinterpret_cast<uintptr_t>(workspace) & 15) return SKA_EINVAL;
+    a.delta = static_cast<float *>(workspace);
+    a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + delta_bytes(p));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    rc = launch(SM_DQ, p, rows_grid(p), a, st);   // (writes delta, which dK reads)
+    return rc != SKA_OK ? rc : launch(SM_DKV, p, keys_grid(p), a, st);
+}
+
+}  // extern "C"

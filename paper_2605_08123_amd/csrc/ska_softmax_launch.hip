@@ -1,0 +1,35 @@
+// The softmax attention kernels' instances for one storage type and head dimension (SKA_T, SKA_D; the function's name: SKA_NAME).
+#include "sinkhorn_attn_layer.h"
+#include "ska_softmax_launch.h"
+
+namespace {
+template <typename T, int D> int launch(int what, int nw, const SmArgs &a, hipStream_t st)
+{
+    const dim3 grid((unsigned)((a.total + 7) / 8 * 8));
+    switch (what) {
+    case SM_FWD:
+        if (nw == 1) hipLaunchKernelGGL((sm_rows_kernel<T, D, 1, false>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((sm_rows_kernel<T, D, 4, false>), grid, dim3(256), 0, st, a);
+        break;
+    case SM_DQ:
+        if (nw == 1) hipLaunchKernelGGL((sm_rows_kernel<T, D, 1, true>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((sm_rows_kernel<T, D, 4, true>), grid, dim3(256), 0, st, a);
+        break;
+    default:
+        if (nw == 1) hipLaunchKernelGGL((sm_keys_kernel<T, D, 1>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((sm_keys_kernel<T, D, 4>), grid, dim3(256), 0, st, a);
+    }
+    if (hipGetLastError() != hipSuccess) return SKA_EHIP;
+    if (a.parts > 1) {
+        const long n = (long)a.B * a.Hk * (what == SM_DKV ? (long)a.Lk * 2 : (long)a.Lq * a.G) * (D / 4);
+        const dim3 jg((unsigned)((n + NTHREADS - 1) / NTHREADS));
+        if (what == SM_FWD) hipLaunchKernelGGL((sm_join_kernel<T, D, SM_JOIN_O>), jg, dim3(NTHREADS), 0, st, a);
+        else if (what == SM_DQ) hipLaunchKernelGGL((sm_join_kernel<T, D, SM_JOIN_DQ>), jg, dim3(NTHREADS), 0, st, a);
+        else hipLaunchKernelGGL((sm_join_kernel<T, D, SM_JOIN_DKV>), jg, dim3(NTHREADS), 0, st, a);
+        if (hipGetLastError() != hipSuccess) return SKA_EHIP;
+    }
+    return SKA_OK;
+}
+}  // namespace
+
+SKA_DECLARE_SOFTMAX(SKA_NAME) { return launch<SKA_T, SKA_D>(what, nw, *static_cast<const SmArgs *>(args), st); }
