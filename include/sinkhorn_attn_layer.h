@@ -109,7 +109,7 @@ int ska_rope_bwd(const void *dQr, const ska_strides *dqr_strides, void *dQ, cons
  *   finite to leave the item's other queries alone.
  *   W >= 0 (W >= max(Lq, Lk) with starts of 0 is the dense problem); eps > 0 and finite.
  *   d in {32, 64, 128}; 1 <= Lq, Lk <= 2^24; B * Hk <= 65535, Lq * (Hq / Hk) <= 2^27.
- *   Pointers and strides in bytes: multiples of 16 (SKA_EUNSUPPORTED otherwise).
+ *   Pointers and strides in bytes: multiples of 16, tokens less than 128 MiB apart (SKA_EUNSUPPORTED otherwise).
  *   workspace: ska_softmax_attn_workspace_bytes(...) bytes (may be 0: then NULL is fine), 16-byte aligned; scratch.
  * Few queries on many keys (an answer's next token; W >= Lk for a whole cache) are split over the keys, and the parts joined.
  */

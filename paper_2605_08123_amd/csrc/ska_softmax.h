@@ -25,7 +25,7 @@ struct SmTensor {
 struct SmArgs {
     SmTensor q, k, v, o, g;        // g: dO
     SmTensor oq, ok, ov;           // forward: oq = O; backward: dQ, dK, dV (written)
-    float *lse, *delta;            // [B][Hq][Lq]
+    float *lse, *lse2, *delta;     // [B][Hq][Lq]; lse2: LSE log2(e) as dK reads it, inf where there is no row
     const int *start, *len_q, *len_k;
     const unsigned char *mask_q, *mask_k;
     float *part, *part_lse;        // walks in parts: [parts][problems][rows][D] (forward: and their LSE [parts][problems][rows])
@@ -68,30 +68,95 @@ __device__ __forceinline__ bool sm_place(const SmArgs &a, SmPlace &w)
 __device__ __forceinline__ int sm_len(const int *len, int b, int L) { return len ? min(max(len[b], 0), L) : L; }
 __device__ __forceinline__ int sm_start(const SmArgs &a, int b) { return a.start ? min(max(a.start[b], 0), 1 << 24) : 0; }
 
-// Tiles: KT walked rows (two score tiles of 32 for bf16, one for fp32: the same bytes)
+// Tiles: KT walked rows (two score tiles of 32 for narrow bf16 heads, else one), row-major, 16-byte chunks XOR-swizzled
+// by the row so that reads of one chunk of many rows, and of one row of many chunks, touch all banks.
 template <typename T, int D> struct SmTile {
-    static constexpr int KT = sizeof(T) == 2 ? 64 : 32;
-    static constexpr int CPR = D * (int)sizeof(T) / 16;                      // 16-byte pieces per row
-    static constexpr int SUB = Tile<T, D>::RM_BYTES;                         // bytes of 32 rows in LDS
-    static constexpr int BYTES = SUB * (KT / 32);
-};
-// A walked tile of one matrix on its way from memory to LDS, by the NT threads of a workgroup
-template <typename T, int D, int NT> struct SmStage {
-    using TL = SmTile<T, D>;
-    static constexpr int N = TL::KT * TL::CPR / NT;   // pieces per thread
-    static_assert(TL::KT * TL::CPR % NT == 0 && NT % TL::CPR == 0, "whole pieces");
-    uint4 r[N];
-    static __device__ __forceinline__ int row(int c) { return (int)threadIdx.x / TL::CPR + c * (NT / TL::CPR); }
-    static __device__ __forceinline__ int chunk() { return (int)threadIdx.x % TL::CPR; }
-    __device__ __forceinline__ void load(int c, const T *row_at) { r[c] = *reinterpret_cast<const uint4 *>(row_at + chunk() * (16 / (int)sizeof(T))); }
-    __device__ __forceinline__ void store(int c, unsigned char *lds, bool there)
+    static constexpr int KT = sizeof(T) == 2 && D < 128 ? 64 : 32;
+    static constexpr int ROWB = D * (int)sizeof(T), CPR = ROWB / 16;
+    static constexpr int SUB = 32 * ROWB;      // bytes of one score tile's rows
+    static constexpr int BYTES = KT * ROWB;
+    static constexpr int RPI = 64 / CPR;       // rows that one load instruction of a wavefront brings (1 KB)
+    static __device__ __forceinline__ int swz(int row)
     {
-        const uint4 x = there ? r[c] : make_uint4(0, 0, 0, 0);
-        const int i = row(c);
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint4 *>(lds + bf16_chunk_off<D>(i, chunk())) = x;
-        else *reinterpret_cast<uint4 *>(lds + (i * f32_row_floats<D>() + chunk() * 4) * 4) = x;
+        if constexpr (sizeof(T) == 2) return bf16_swizzle<D>(row);
+        else return row & 7;
     }
 };
+
+// Tiles come by loads that write LDS directly, KT / RPI instructions a tile dealt to the NW wavefronts: no registers, no
+// stores, and the next tile is under way while this one is worked on.
+template <typename T, int D, int NW> struct SmLoader {
+    using TL = SmTile<T, D>;
+    static constexpr int PER = TL::KT / TL::RPI / NW;   // instructions per wavefront and matrix
+    static_assert(PER * NW * TL::RPI == TL::KT, "whole instructions");
+    int lane, wv, lrow;
+    __device__ __forceinline__ SmLoader(int lane, int wv) : lane(lane), wv(wv), lrow(lane / TL::CPR) {}
+    // first row of instruction k; this lane's row is lrow below it
+    __device__ __forceinline__ int first(int k) const { return (wv + NW * k) * TL::RPI; }
+    // rows 0 ... rows - 1 of the tile at `base` (uniform), `stride` bytes apart, exist: the others repeat the last one
+    __device__ __forceinline__ void load(unsigned lds, const unsigned char *base, long stride, int rows) const
+    {
+        const bool whole = rows >= TL::KT;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int r0 = first(k);
+            // (the swizzle takes single bits of the row: that of a sum without carries is the exclusive or)
+            const unsigned col = (unsigned)((lane % TL::CPR) ^ TL::swz(lrow) ^ TL::swz(r0)) * 16;
+            int r = r0, l = lrow;
+            if (!whole) {
+                r = min(r0, rows - 1);
+                l = min(lrow, rows - 1 - r);
+            }
+            // (written out, because the compiler takes every later LDS read for one of these bytes and waits at once; the
+            // kernel waits where it needs them.  No register is written.)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds + (unsigned)r0 * TL::ROWB),
+                         "v"((unsigned)l * (unsigned)stride + col), "s"(base + r * stride)
+                         : "memory", "m0");
+        }
+    }
+    // after this wavefront's loads have arrived: zeros into those of its rows that do not count
+    __device__ __forceinline__ void clear(unsigned char *lds, int rows, unsigned on) const
+    {
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (first(k) + lrow >= rows || !(on >> k & 1))
+                *reinterpret_cast<uint4 *>(lds + first(k) * TL::ROWB + lane * 16) = make_uint4(0, 0, 0, 0);
+    }
+};
+// Activity of a tile's rows, read beside its loads and looked at when they have arrived: of the rows that this lane's loads
+// bring, and of row `lane`; rows beyond the last repeat it.
+template <typename T, int D, int NW> struct SmActivity {
+    using L = SmLoader<T, D, NW>;
+    unsigned char mine[L::PER], lane;
+    __device__ __forceinline__ void load(const L &l, const unsigned char *mask, int rows)
+    {
+#pragma unroll
+        for (int k = 0; k < L::PER; ++k) mine[k] = mask[min(l.first(k) + l.lrow, rows - 1)];
+        lane = mask[min(l.lane & (SmTile<T, D>::KT - 1), rows - 1)];
+    }
+    __device__ __forceinline__ unsigned rows() const   // a bit per instruction
+    {
+        unsigned on = 0;
+#pragma unroll
+        for (int k = 0; k < L::PER; ++k) on |= (mine[k] ? 1u : 0u) << k;
+        return on;
+    }
+    __device__ __forceinline__ unsigned long long bits() const { return __ballot(lane != 0); }
+};
+__device__ __forceinline__ void sm_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ unsigned sm_lds(const void *p) { return (unsigned)(size_t)(__attribute__((address_space(3))) const unsigned char *)p; }
+// 64 floats at `p` + `at` (bytes, per lane) into LDS
+__device__ __forceinline__ void sm_load_words(unsigned lds, const float *p, unsigned at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(at), "s"(p) : "memory", "m0");
+}
+// the larger of the two lane halves' values, in both
+__device__ __forceinline__ float sm_max_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 template <typename T, int D> __device__ __forceinline__ void sm_frag(OwnerFrag<T, D> &x, const T *row, int h)
 {
     if constexpr (sizeof(T) == 2) {
@@ -122,6 +187,80 @@ template <int D> __device__ __forceinline__ float sm_dot(const OwnerFrag<float, 
     for (int k = 0; k < D / 2; ++k) s = fmaf(x.v[k], y.v[k], s);
     return s + __shfl_xor(s, 32);
 }
+
+// s[f][t, o] = sum_k tile[t][k] own[f][o][k]: the tile's fragments are read once for all owners
+template <typename T, int D, int FR>
+__device__ __forceinline__ void sm_scores(f32x16 (&s)[FR], const unsigned char *tile, const OwnerFrag<T, D> (&own)[FR], int lane)
+{
+    using TL = SmTile<T, D>;
+    const int t = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int f = 0; f < FR; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[f][e] = 0.f;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            const bf16x8 a = *reinterpret_cast<const bf16x8 *>(tile + bf16_chunk_off<D>(t, 2 * k + h));
+#pragma unroll
+            for (int f = 0; f < FR; ++f) s[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, own[f].v[k], s[f], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < D / 8; ++q) {
+            const float4 a = *reinterpret_cast<const float4 *>(tile + t * TL::ROWB + ((h * (D / 8) + q) ^ TL::swz(t)) * 16);
+#pragma unroll
+            for (int f = 0; f < FR; ++f) {
+                s[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, own[f].v[4 * q + 0], s[f], 0, 0, 0);
+                s[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, own[f].v[4 * q + 1], s[f], 0, 0, 0);
+                s[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, own[f].v[4 * q + 2], s[f], 0, 0, 0);
+                s[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, own[f].v[4 * q + 3], s[f], 0, 0, 0);
+            }
+        }
+    }
+}
+// out[f][v, o] += sum_t tile[t][v] p[f][t, o]
+template <typename T, int D, int FR>
+__device__ __forceinline__ void sm_accum(f32x16 (&out)[FR][D / 32], const unsigned char *tile, const float (&p)[FR][16], int lane)
+{
+    using TL = SmTile<T, D>;
+    const int c = lane & 31, h = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+        // transposing reads: within 16 lanes, lane i receives element (i & 3) of the 8-byte pieces addressed by lanes
+        // (i >> 2) + 4 e, e = 0..3
+        typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
+        const int row = 4 * h + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        const unsigned char *sub = tile + (lane & 1) * 8;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            bf16x8 pf[FR];
+#pragma unroll
+            for (int f = 0; f < FR; ++f) pf[f] = pack8(&p[f][8 * m]);
+#pragma unroll
+            for (int v = 0; v < D / 32; ++v) {
+                bf16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4v __attribute__((address_space(3))) *)(
+                    sub + bf16_chunk_off<D>(row + 16 * m, ch + 4 * v)));
+                bf16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4v __attribute__((address_space(3))) *)(
+                    sub + bf16_chunk_off<D>(row + 16 * m + 8, ch + 4 * v)));
+                const bf16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+                for (int f = 0; f < FR; ++f) out[f][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[f], out[f][v], 0, 0, 0);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int t = 8 * (r >> 2) + 4 * h + (r & 3);
+#pragma unroll
+            for (int v = 0; v < D / 32; ++v) {
+                const float a = *reinterpret_cast<const float *>(tile + t * TL::ROWB + ((8 * v + (c >> 2)) ^ TL::swz(t)) * 16 + (c & 3) * 4);
+#pragma unroll
+                for (int f = 0; f < FR; ++f) out[f][v] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[f][r], out[f][v], 0, 0, 0);
+            }
+        }
+    }
+}
+
 // x where bit `bit` of m is set, otherwise -inf
 __device__ __forceinline__ float sm_keep(float x, unsigned m, int bit)
 {
@@ -138,386 +277,465 @@ __device__ __forceinline__ unsigned sm_bits(int a, int b)
 
 constexpr float SM_LAZY = 8.f;   // powers of two that a row's maximum may grow by before its sums are scaled to it
 
+enum { SM_FWD, SM_DQ, SM_DKV };
+// Fragments of 32 owners that a wavefront of a kernel holds (nw: wavefronts of the workgroup), and wavefronts per SIMD that its
+// registers are to allow
+constexpr int sm_fr(int what, int bytes, int d, int nw) { return 1; }
+constexpr int sm_waves(int what, int bytes, int d, int fr) { return 1; }
+
 // ------------------------------------------------------------------ queries as owners: forward, dQ
-// BWD: dQ instead of O.  NW wavefronts, 32 rows each.
-template <typename T, int D, int NW, bool BWD>
-__global__ __launch_bounds__(64 * NW) void sm_rows_kernel(const SmArgs a)
+// BWD: dQ instead of O.  NW wavefronts, 32 FR rows each.
+template <typename T, int D, int NW, int FR, bool BWD>
+__global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeof(T), D, FR))) void sm_rows_kernel(const SmArgs a)
 {
     using TL = SmTile<T, D>;
-    using Stage = SmStage<T, D, 64 * NW>;
-    constexpr int KT = TL::KT, NS = KT / 32, BM = 32 * NW;
-    constexpr int NBUF = 4 * TL::BYTES <= 65536 ? 2 : 1;
-    __shared__ __align__(16) unsigned char lds[NBUF][2][TL::BYTES];
+    constexpr int KT = TL::KT, NS = KT / 32, BM = 32 * NW * FR;
+    __shared__ __align__(1024) unsigned char lds[2][2][TL::BYTES];
 
     SmPlace w;
     if (!sm_place(a, w)) return;
     const int R = a.Lq * a.G, r0 = w.blk * BM;
     const int lq = sm_len(a.len_q, w.b, a.Lq), lk = sm_len(a.len_k, w.b, a.Lk), start = sm_start(a, w.b);
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const long prob = (long)w.b * a.Hk + w.hk;
+    const int up = a.causal ? 0 : a.W;
 
-    // this lane's row
-    const int r = r0 + 32 * wv + (lane & 31), rc = min(r, R - 1), i = rc / a.G, hq = w.hk * a.G + (rc - i * a.G);
-    bool live = r < R && i < lq;
-    if (live && a.mask_q) live = a.mask_q[(long)w.b * a.Lq + i] != 0;
-    const long head = (long)w.b * a.G * a.Hk + hq;   // of [B][Hq][Lq] vectors
-    OwnerFrag<T, D> q, g;
-    sm_frag<T, D>(q, reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + hq * a.q.h + i * a.q.l, h);
-    float m = -INFINITY, sum = 0.f, delta = 0.f;   // BWD: m = LSE log2(e)
-    if constexpr (BWD) {
-        OwnerFrag<T, D> o;
-        sm_frag<T, D>(g, reinterpret_cast<const T *>(a.g.p) + w.b * a.g.b + hq * a.g.h + i * a.g.l, h);
-        sm_frag<T, D>(o, reinterpret_cast<const T *>(a.o.p) + w.b * a.o.b + hq * a.o.h + i * a.o.l, h);
-        const float lse = a.lse[head * a.Lq + i];
-        live = live && lse > -INFINITY;
-        m = live ? lse * LOG2E : INFINITY;      // (exp2(s - inf) = 0)
-        delta = sm_dot<D>(g, o);
-        if (!live) delta = 0.f;
-        if (w.part == 0 && h == 0 && r < R) a.delta[head * a.Lq + i] = delta;
+    // this lane's rows
+    OwnerFrag<T, D> q[FR], g[FR];
+    bool live[FR];
+    int my_lo[FR], my_hi[FR];
+    float m[FR], sum[FR], delta[FR];   // BWD: m = LSE log2(e)
+    const int wr0 = r0 + 32 * FR * wv;
+#pragma unroll
+    for (int f = 0; f < FR; ++f) {
+        const int r = wr0 + 32 * f + (lane & 31), rc = min(r, R - 1), i = rc / a.G, hq = w.hk * a.G + (rc - i * a.G);
+        live[f] = r < R && i < lq;
+        if (live[f] && a.mask_q) live[f] = a.mask_q[(long)w.b * a.Lq + i] != 0;
+        my_lo[f] = start + i - a.W;
+        my_hi[f] = min(start + i + up, lk - 1);
+        sm_frag<T, D>(q[f], reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + hq * a.q.h + i * a.q.l, h);
+        m[f] = -INFINITY;
+        sum[f] = delta[f] = 0.f;
+        if constexpr (BWD) {
+            OwnerFrag<T, D> o;
+            sm_frag<T, D>(g[f], reinterpret_cast<const T *>(a.g.p) + w.b * a.g.b + hq * a.g.h + i * a.g.l, h);
+            sm_frag<T, D>(o, reinterpret_cast<const T *>(a.o.p) + w.b * a.o.b + hq * a.o.h + i * a.o.l, h);
+            const long at = ((long)w.b * a.G * a.Hk + hq) * a.Lq + i;
+            const float lse = a.lse[at];
+            live[f] = live[f] && lse > -INFINITY;
+            m[f] = live[f] ? lse * LOG2E : INFINITY;      // (exp2(s - inf) = 0)
+            delta[f] = sm_dot<D>(g[f], o);
+            if (!live[f]) delta[f] = 0.f;
+            if (w.part == 0 && h == 0 && r < R) {
+                a.lse2[at] = m[f];
+                a.delta[at] = delta[f];
+            }
+        }
     }
 
     // keys that the block's rows, and this wavefront's, can reach
-    const int i_last = min(min(r0 + BM, R) - 1, lq * a.G - 1) / a.G;   // (lq 0: no row, and no key below)
-    int j_lo = max(0, start + r0 / a.G - a.W), j_hi = min(lk - 1, start + i_last + (a.causal ? 0 : a.W));
+    const int i_last = (min(min(r0 + BM, R), lq * a.G) - 1) / a.G;   // (lq 0: no row, and no key below)
+    int j_lo = max(0, start + r0 / a.G - a.W), j_hi = min(lk - 1, start + i_last + up);
     if (lq * a.G <= r0) j_hi = j_lo - 1;
-    const int w_first = start + min(r0 + 32 * wv, R - 1) / a.G, w_last = start + min(r0 + 32 * wv + 31, R - 1) / a.G;
-    const int up = a.causal ? 0 : a.W;
-    const int w_lo = w_first - a.W, w_hi = w_last + up;                  // any of its rows
-    const int all_lo = w_last - a.W, all_hi = min(w_first + up, lk - 1); // all of them
+    const int w_first = start + min(wr0, R - 1) / a.G, w_last = start + min(wr0 + 32 * FR - 1, R - 1) / a.G;
+    const int w_lo = w_first - a.W, w_hi = w_last + up;                        // any of its rows
+    const int all_lo = w_last - a.W, all_hi = min(min(w_first + up, lk - 1), j_hi);   // all of them
     int tiles = (j_hi - j_lo + KT) / KT;
     if (a.parts > 1) {
         const int per = (tiles + a.parts - 1) / a.parts;
         j_lo += w.part * per * KT;
         tiles = min(per, tiles - w.part * per);
     }
-    const int my_lo = start + i - a.W, my_hi = min(start + i + up, lk - 1);
 
-    f32x16 acc[D / 32];
+    f32x16 acc[FR][D / 32];
 #pragma unroll
-    for (int v = 0; v < D / 32; ++v)
+    for (int f = 0; f < FR; ++f)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[v][e] = 0.f;
+        for (int v = 0; v < D / 32; ++v)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[f][v][e] = 0.f;
 
-    const T *kb = reinterpret_cast<const T *>(a.k.p) + w.b * a.k.b + w.hk * a.k.h;
-    const T *vb = reinterpret_cast<const T *>(a.v.p) + w.b * a.v.b + w.hk * a.v.h;
+    const unsigned char *kb = reinterpret_cast<const unsigned char *>(reinterpret_cast<const T *>(a.k.p) + w.b * a.k.b + w.hk * a.k.h);
+    const unsigned char *vb = reinterpret_cast<const unsigned char *>(reinterpret_cast<const T *>(a.v.p) + w.b * a.v.b + w.hk * a.v.h);
+    const long ks = a.k.l * (long)sizeof(T), vs = a.v.l * (long)sizeof(T);
     const unsigned char *mk = a.mask_k ? a.mask_k + (long)w.b * a.Lk : nullptr;
-    Stage sk, sv;
-    unsigned char on = 1, row_on[Stage::N];   // activity of key `lane` of the tile, and of the rows this thread stages
-    auto fetch = [&](int j0) {
-#pragma unroll
-        for (int c = 0; c < Stage::N; ++c) {
-            const int j = min(j0 + Stage::row(c), j_hi);
-            sk.load(c, kb + j * a.k.l);
-            sv.load(c, vb + j * a.v.l);
-            row_on[c] = mk ? mk[j] : 1;
-        }
-        if (mk) on = mk[min(j0 + (lane & (KT - 1)), j_hi)];
+    const SmLoader<T, D, NW> loader(lane, wv);
+    const unsigned lds_at = sm_lds(lds);
+    SmActivity<T, D, NW> act;
+    auto fetch = [&](int j0, int buf) {
+        const int rows = j_hi + 1 - j0;
+        loader.load(lds_at + buf * 2 * TL::BYTES, kb + j0 * ks, ks, rows);
+        loader.load(lds_at + (buf * 2 + 1) * TL::BYTES, vb + j0 * vs, vs, rows);
+        if (mk) act.load(loader, mk + j0, rows);
     };
-    auto put = [&](int j0, int buf) {
-#pragma unroll
-        for (int c = 0; c < Stage::N; ++c) {
-            const bool there = j0 + Stage::row(c) <= j_hi && row_on[c];
-            sk.store(c, lds[buf][0], there);
-            sv.store(c, lds[buf][1], there);
-        }
-    };
-    if (tiles > 0) fetch(j_lo);
+    if (tiles > 0) fetch(j_lo, 0);
     for (int t = 0; t < tiles; ++t) {
-        const int j0 = j_lo + t * KT, buf = NBUF == 2 ? t & 1 : 0;
-        if (NBUF == 1 && t) __syncthreads();
-        put(j0, buf);
-        const unsigned long long active = mk ? __ballot(on != 0) : ~0ull;
-        __syncthreads();
-        if (t + 1 < tiles) fetch(j0 + KT);
-        if (j0 > w_hi || j0 + KT - 1 < w_lo) continue;
-        const unsigned char *kt = lds[buf][0], *vt = lds[buf][1];
-        f32x16 s[NS], z[NS];
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[n][e] = z[n][e] = 0.f;
-            s[n] = tile_dot<D>(kt + n * TL::SUB, q, lane, s[n]);
-            if constexpr (BWD) z[n] = tile_dot<D>(vt + n * TL::SUB, g, lane, z[n]);
-        }
-        const bool whole = j0 >= all_lo && j0 + KT - 1 <= all_hi && active == ~0ull;
-        if (!whole) {
-#pragma unroll
-            for (int n = 0; n < NS; ++n) {
-                const int base = j0 + 32 * n;
-                const unsigned keep = (sm_bits(my_lo - base, min(my_hi, j_hi) - base) & (unsigned)(active >> (32 * n))) >> (4 * h);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[n][e] = sm_keep(s[n][e], keep, 8 * (e >> 2) + (e & 3));
+        const int j0 = j_lo + t * KT, buf = t & 1;
+        sm_arrived();
+        unsigned long long here = ~0ull;   // active keys
+        if (j_hi + 1 - j0 < KT || mk) {    // (products with rows that do not count must not meet what they hold)
+            unsigned on = ~0u;
+            if (mk) {
+                on = act.rows();
+                here = act.bits();
             }
+            loader.clear(lds[buf][0], j_hi + 1 - j0, on);
+            loader.clear(lds[buf][1], j_hi + 1 - j0, on);
         }
+        __syncthreads();
+        if (t + 1 < tiles) fetch(j0 + KT, buf ^ 1);
         if constexpr (!BWD) {
+            if (j0 > w_hi || j0 + KT - 1 < w_lo) continue;
+            const bool whole = j0 >= all_lo && j0 + KT - 1 <= all_hi && here == ~0ull;
+            f32x16 s[NS][FR];
+#pragma unroll
+            for (int n = 0; n < NS; ++n) sm_scores<T, D, FR>(s[n], lds[buf][0] + n * TL::SUB, q, lane);
+            if (!whole) {
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+#pragma unroll
+                    for (int f = 0; f < FR; ++f) {
+                        const int base = j0 + 32 * n;
+                        const unsigned keep = (sm_bits(my_lo[f] - base, min(my_hi[f], j_hi) - base) & (unsigned)(here >> (32 * n))) >> (4 * h);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[n][f][e] = sm_keep(s[n][f][e], keep, 8 * (e >> 2) + (e & 3));
+                    }
+            }
             // Running maximum: sums stay relative to an older one until a score exceeds it by 2^SM_LAZY, so that the
             // accumulators are scaled a few times per row and not once per tile; P up to 2^8 loses nothing in either type.
-            float top = s[0][0];
+            float top[FR], mu[FR];
+            bool grow = false;
 #pragma unroll
-            for (int n = 0; n < NS; ++n)
+            for (int f = 0; f < FR; ++f) {
+                top[f] = s[0][f][0];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[n][e]);
-            top = fmaxf(top, __shfl_xor(top, 32)) * a.c2;
-            if (__any(top > m + SM_LAZY)) {
-                const float mn = fmaxf(m, top), f = mn > -INFINITY ? fast_exp2(m - mn) : 1.f;
-                sum *= f;
+                for (int n = 0; n < NS; ++n)
 #pragma unroll
-                for (int v = 0; v < D / 32; ++v)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[v][e] *= f;
-                m = mn;
+                    for (int e = 0; e < 16; ++e) top[f] = fmaxf(top[f], s[n][f][e]);
+                top[f] = sm_max_halves(top[f]) * a.c2;
+                grow = grow || top[f] > m[f] + SM_LAZY;
             }
-            const float mu = m > -INFINITY ? m : 0.f;
+            if (__any(grow)) {
+#pragma unroll
+                for (int f = 0; f < FR; ++f) {
+                    const float mn = fmaxf(m[f], top[f]), x = mn > -INFINITY ? fast_exp2(m[f] - mn) : 1.f;
+                    sum[f] *= x;
+#pragma unroll
+                    for (int v = 0; v < D / 32; ++v)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[f][v][e] *= x;
+                    m[f] = mn;
+                }
+            }
+#pragma unroll
+            for (int f = 0; f < FR; ++f) mu[f] = m[f] > -INFINITY ? m[f] : 0.f;
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
-                float p[16];
+                float p[FR][16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    p[e] = fast_exp2(fmaf(s[n][e], a.c2, -mu));
-                    sum += p[e];
-                }
-                tile_accum<T, D>(acc, vt + n * TL::SUB, p, lane);
+                for (int f = 0; f < FR; ++f)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        p[f][e] = fast_exp2(fmaf(s[n][f][e], a.c2, -mu[f]));
+                        sum[f] += p[f][e];
+                    }
+                sm_accum<T, D, FR>(acc, lds[buf][1] + n * TL::SUB, p, lane);
             }
         } else {
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
-                float p[16];
+                const int base = j0 + 32 * n;
+                if (base > w_hi || base + 31 < w_lo) continue;
+                const bool whole = base >= all_lo && base + 31 <= all_hi && (unsigned)(here >> (32 * n)) == ~0u;
+                f32x16 s[FR], z[FR];
+                sm_scores<T, D, FR>(s, lds[buf][0] + n * TL::SUB, q, lane);
+                sm_scores<T, D, FR>(z, lds[buf][1] + n * TL::SUB, g, lane);
+                if (!whole) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) p[e] = fast_exp2(fmaf(s[n][e], a.c2, -m)) * (z[n][e] - delta);
-                tile_accum<T, D>(acc, kt + n * TL::SUB, p, lane);
+                    for (int f = 0; f < FR; ++f) {
+                        const unsigned keep = (sm_bits(my_lo[f] - base, min(my_hi[f], j_hi) - base) & (unsigned)(here >> (32 * n))) >> (4 * h);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[f][e] = sm_keep(s[f][e], keep, 8 * (e >> 2) + (e & 3));
+                    }
+                }
+                float p[FR][16];
+#pragma unroll
+                for (int f = 0; f < FR; ++f)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) p[f][e] = fast_exp2(fmaf(s[f][e], a.c2, -m[f])) * (z[f][e] - delta[f]);
+                sm_accum<T, D, FR>(acc, lds[buf][0] + n * TL::SUB, p, lane);
             }
         }
     }
 
-    float scale = a.cs;
-    if constexpr (!BWD) {
-        sum += __shfl_xor(sum, 32);
-        live = live && sum > 0.f;
-        scale = live ? 1.f / sum : 0.f;
-        const float lse = live ? (m + fast_log2(sum)) * LN2 : -INFINITY;
-        if (h == 0 && r < R) {
-            if (a.parts > 1) a.part_lse[((long)w.part * a.B * a.Hk + prob) * R + r] = lse;
-            else a.lse[head * a.Lq + i] = lse;
+#pragma unroll
+    for (int f = 0; f < FR; ++f) {
+        const int r = wr0 + 32 * f + (lane & 31), rc = min(r, R - 1), i = rc / a.G, hq = w.hk * a.G + (rc - i * a.G);
+        float scale = a.cs;
+        if constexpr (!BWD) {
+            sum[f] += __shfl_xor(sum[f], 32);
+            live[f] = live[f] && sum[f] > 0.f;
+            scale = live[f] ? 1.f / sum[f] : 0.f;
+            const float lse = live[f] ? (m[f] + fast_log2(sum[f])) * LN2 : -INFINITY;
+            if (h == 0 && r < R) {
+                if (a.parts > 1) a.part_lse[((long)w.part * a.B * a.Hk + prob) * R + r] = lse;
+                else a.lse[((long)w.b * a.G * a.Hk + hq) * a.Lq + i] = lse;
+            }
+        }
+        if (r >= R) continue;
+        if (a.parts > 1) {
+            float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * R + r) * D;
+#pragma unroll
+            for (int v = 0; v < D / 32; ++v)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *reinterpret_cast<float4 *>(out + 32 * v + 8 * e + 4 * h) =
+                        live[f] ? make_float4(acc[f][v][4 * e] * scale, acc[f][v][4 * e + 1] * scale, acc[f][v][4 * e + 2] * scale, acc[f][v][4 * e + 3] * scale)
+                                : make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+            T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + w.b * a.oq.b + hq * a.oq.h + i * a.oq.l;
+#pragma unroll
+            for (int v = 0; v < D / 32; ++v)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    T *at = out + 32 * v + 8 * e + 4 * h;
+                    if (live[f]) store4<T>(at, acc[f][v][4 * e] * scale, acc[f][v][4 * e + 1] * scale, acc[f][v][4 * e + 2] * scale, acc[f][v][4 * e + 3] * scale);
+                    else store4<T>(at, 0.f, 0.f, 0.f, 0.f);
+                }
         }
     }
-    if (r >= R) return;
-    if (a.parts > 1) {
-        float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * R + r) * D;
-#pragma unroll
-        for (int v = 0; v < D / 32; ++v)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                *reinterpret_cast<float4 *>(out + 32 * v + 8 * e + 4 * h) =
-                    live ? make_float4(acc[v][4 * e] * scale, acc[v][4 * e + 1] * scale, acc[v][4 * e + 2] * scale, acc[v][4 * e + 3] * scale)
-                         : make_float4(0.f, 0.f, 0.f, 0.f);
-        return;
-    }
-    T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + w.b * a.oq.b + hq * a.oq.h + i * a.oq.l;
-#pragma unroll
-    for (int v = 0; v < D / 32; ++v)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            T *at = out + 32 * v + 8 * e + 4 * h;
-            if (live) store4<T>(at, acc[v][4 * e] * scale, acc[v][4 * e + 1] * scale, acc[v][4 * e + 2] * scale, acc[v][4 * e + 3] * scale);
-            else store4<T>(at, 0.f, 0.f, 0.f, 0.f);
-        }
 }
 
 // ------------------------------------------------------------------ keys as owners: dK, dV
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW) void sm_keys_kernel(const SmArgs a)
+// The queries of one head after another: each is a walk of its own over the same positions.
+template <typename T, int D, int NW, int FR>
+__global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR))) void sm_keys_kernel(const SmArgs a)
 {
     using TL = SmTile<T, D>;
-    using Stage = SmStage<T, D, 64 * NW>;
-    constexpr int KT = TL::KT, NS = KT / 32, BM = 32 * NW;
-    constexpr int NBUF = 4 * TL::BYTES + 2 * 3 * KT * 4 <= 65536 ? 2 : 1;
-    __shared__ __align__(16) unsigned char lds[NBUF][2][TL::BYTES];
-    __shared__ __align__(16) float vec[NBUF][3][KT];   // of the tile's rows: LSE log2(e) (inf: no such row), delta, position
+    constexpr int KT = TL::KT, NS = KT / 32, BM = 32 * NW * FR;
+    constexpr int NBUF = 4 * TL::BYTES + 1024 <= 65536 ? 2 : 1;   // (fp32, d = 128: one, and other workgroups while it is filled)
+    __shared__ __align__(1024) unsigned char lds[NBUF][2][TL::BYTES];
+    __shared__ __align__(256) float vec[2][2][64];   // of the tile's rows: LSE log2(e) (inf: no such row), delta
 
     SmPlace w;
     if (!sm_place(a, w)) return;
-    const int R = a.Lq * a.G, k0 = w.blk * BM;
+    const int k0 = w.blk * BM;
     const int lq = sm_len(a.len_q, w.b, a.Lq), lk = sm_len(a.len_k, w.b, a.Lk), start = sm_start(a, w.b);
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const long prob = (long)w.b * a.Hk + w.hk;
-    const int j = k0 + 32 * wv + (lane & 31), jc = min(j, a.Lk - 1);
-    bool live = j < lk;
-    if (live && a.mask_k) live = a.mask_k[(long)w.b * a.Lk + j] != 0;
-    OwnerFrag<T, D> k, v;
-    sm_frag<T, D>(k, reinterpret_cast<const T *>(a.k.p) + w.b * a.k.b + w.hk * a.k.h + jc * a.k.l, h);
-    sm_frag<T, D>(v, reinterpret_cast<const T *>(a.v.p) + w.b * a.v.b + w.hk * a.v.h + jc * a.v.l, h);
-
-    // queries that reach the block's keys, and this wavefront's: p - W <= j <= p + up
     const int up = a.causal ? 0 : a.W;
-    const int k_last = min(min(k0 + BM, a.Lk), lk) - 1;
-    const int i_lo = max(0, k0 - up - start), i_hi = min(lq - 1, k_last + a.W - start);
-    int r_lo = i_lo * a.G, r_hi = i_hi * a.G + a.G - 1;
-    if (k_last < k0 || i_hi < i_lo) { r_lo = 0; r_hi = -1; }
-    const int w_first = k0 + 32 * wv, w_last = w_first + 31;
-    int tiles = (r_hi - r_lo + KT) / KT;
-    if (a.parts > 1) {
-        const int per = (tiles + a.parts - 1) / a.parts;
-        r_lo += w.part * per * KT;
-        tiles = min(per, tiles - w.part * per);
+    OwnerFrag<T, D> k[FR], v[FR];
+    const int w_first = k0 + 32 * FR * wv, w_last = w_first + 32 * FR - 1;
+#pragma unroll
+    for (int f = 0; f < FR; ++f) {
+        const int jc = min(w_first + 32 * f + (lane & 31), a.Lk - 1);
+        sm_frag<T, D>(k[f], reinterpret_cast<const T *>(a.k.p) + w.b * a.k.b + w.hk * a.k.h + jc * a.k.l, h);
+        sm_frag<T, D>(v[f], reinterpret_cast<const T *>(a.v.p) + w.b * a.v.b + w.hk * a.v.h + jc * a.v.l, h);
     }
 
-    f32x16 dk[D / 32], dv[D / 32];
+    // queries that reach the block's keys: p - W <= j <= p + up
+    const int k_last = min(min(k0 + BM, a.Lk), lk) - 1;
+    const int i_lo = max(0, k0 - up - start), i_hi = min(lq - 1, k_last + a.W - start);
+    const int per_head = k_last < k0 || i_hi < i_lo ? 0 : (i_hi - i_lo + KT) / KT;
+    int t0 = 0, t1 = per_head * a.G;
+    if (a.parts > 1) {
+        const int per = (t1 + a.parts - 1) / a.parts;
+        t0 = w.part * per;
+        t1 = min(t1, t0 + per);
+    }
+
+    f32x16 dk[FR][D / 32], dv[FR][D / 32];
 #pragma unroll
-    for (int x = 0; x < D / 32; ++x)
+    for (int f = 0; f < FR; ++f)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dk[x][e] = dv[x][e] = 0.f;
+        for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) dk[f][x][e] = dv[f][x][e] = 0.f;
 
     const long head0 = (long)w.b * a.G * a.Hk + w.hk * a.G;
     const T *qb = reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + (long)w.hk * a.G * a.q.h;
     const T *gb = reinterpret_cast<const T *>(a.g.p) + w.b * a.g.b + (long)w.hk * a.G * a.g.h;
+    const long qs = a.q.l * (long)sizeof(T), gs = a.g.l * (long)sizeof(T);
     const unsigned char *mq = a.mask_q ? a.mask_q + (long)w.b * a.Lq : nullptr;
-    Stage sq, sg;
-    unsigned char row_on[Stage::N];
-    float lse = 0.f, del = 0.f;
-    int pos = 0;
-    auto fetch = [&](int r0) {
-#pragma unroll
-        for (int c = 0; c < Stage::N; ++c) {
-            const int r = min(r0 + Stage::row(c), r_hi), i = a.G == 1 ? r : r / a.G, hg = r - i * a.G;
-            sq.load(c, qb + hg * a.q.h + i * a.q.l);
-            sg.load(c, gb + hg * a.g.h + i * a.g.l);
-            row_on[c] = mq ? mq[i] : 1;
+    const SmLoader<T, D, NW> loader(lane, wv);
+    const unsigned lds_at = sm_lds(lds), vec_at = sm_lds(vec);
+    SmActivity<T, D, NW> act;
+    int head = t0 < t1 ? t0 / per_head : 0, at = t0 - head * per_head;   // of the next tile to fetch
+    auto fetch = [&](int buf) {
+        const int i0 = i_lo + at * KT, rows = i_hi + 1 - i0;
+        loader.load(lds_at + buf * 2 * TL::BYTES, reinterpret_cast<const unsigned char *>(qb + head * a.q.h) + i0 * qs, qs, rows);
+        loader.load(lds_at + (buf * 2 + 1) * TL::BYTES, reinterpret_cast<const unsigned char *>(gb + head * a.g.h) + i0 * gs, gs, rows);
+        if (wv == 0) {   // 64 entries of both vectors: rows beyond the last repeat it
+            const long e = (head0 + head) * a.Lq + i0;
+            const unsigned o = (unsigned)min(lane, rows - 1) * 4;
+            sm_load_words(vec_at + buf * 512, a.lse2 + e, o);
+            sm_load_words(vec_at + buf * 512 + 256, a.delta + e, o);
         }
-        if (threadIdx.x < KT) {
-            const int r = min(r0 + (int)threadIdx.x, r_hi), i = a.G == 1 ? r : r / a.G, hg = r - i * a.G;
-            lse = a.lse[(head0 + hg) * a.Lq + i] * LOG2E;
-            del = a.delta[(head0 + hg) * a.Lq + i];
-            pos = start + i;
-            if (r0 + (int)threadIdx.x > r_hi || !(lse > -INFINITY) || (mq && !mq[i])) { lse = INFINITY; del = 0.f; }
-        }
+        if (mq) act.load(loader, mq + i0, rows);
+        if (++at == per_head) { at = 0; ++head; }
     };
-    auto put = [&](int r0, int buf) {
-#pragma unroll
-        for (int c = 0; c < Stage::N; ++c) {
-            const bool there = r0 + Stage::row(c) <= r_hi && row_on[c];
-            sq.store(c, lds[buf][0], there);
-            sg.store(c, lds[buf][1], there);
+    int i0 = i_lo + at * KT;   // first query of the tile at hand
+    if (NBUF == 2 && t0 < t1) fetch(0);
+    for (int t = t0; t < t1; ++t) {
+        const int buf = NBUF == 2 ? (t - t0) & 1 : 0, rows = i_hi + 1 - i0;
+        if (NBUF == 1) {
+            if (t > t0) __syncthreads();
+            fetch(0);
         }
-        if (threadIdx.x < KT) {
-            vec[buf][0][threadIdx.x] = lse;
-            vec[buf][1][threadIdx.x] = del;
-            vec[buf][2][threadIdx.x] = __int_as_float(pos);
+        sm_arrived();
+        if (rows < KT || mq) {
+            const unsigned on = mq ? act.rows() : ~0u;
+            loader.clear(lds[buf][0], rows, on);
+            loader.clear(lds[buf][1], rows, on);
+            if (wv == 0 && lane >= rows) {
+                vec[buf][0][lane] = INFINITY;
+                vec[buf][1][lane] = 0.f;
+            }
         }
-    };
-    if (tiles > 0) fetch(r_lo);
-    for (int t = 0; t < tiles; ++t) {
-        const int r0 = r_lo + t * KT, buf = NBUF == 2 ? t & 1 : 0;
-        if (NBUF == 1 && t) __syncthreads();
-        put(r0, buf);
         __syncthreads();
-        if (t + 1 < tiles) fetch(r0 + KT);
-        // positions of the tile's first and last row
-        const int p_first = __float_as_int(vec[buf][2][0]), p_last = __float_as_int(vec[buf][2][KT - 1]);
-        if (p_last + up < w_first || p_first - a.W > w_last) continue;
-        const bool whole = p_first + up >= w_last && p_last - a.W <= w_first;
-        const unsigned char *qt = lds[buf][0], *gt = lds[buf][1];
+        const int next = i_lo + at * KT;
+        if (NBUF == 2 && t + 1 < t1) fetch(buf ^ 1);
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            f32x16 s, z;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = z[e] = 0.f;
-            s = tile_dot<D>(qt + n * TL::SUB, k, lane, s);
-            z = tile_dot<D>(gt + n * TL::SUB, v, lane, z);
-            float p[16], ds[16];
+            const int p_first = start + i0 + 32 * n, p_last = p_first + 31;   // positions of the score tile's rows
+            if (p_last + up < w_first || p_first - a.W > w_last || 32 * n >= rows) continue;
+            const bool whole = p_first + up >= w_last && p_last - a.W <= w_first;
+            f32x16 s[FR], z[FR];
+            sm_scores<T, D, FR>(s, lds[buf][0] + n * TL::SUB, k, lane);
+            sm_scores<T, D, FR>(z, lds[buf][1] + n * TL::SUB, v, lane);
+            float p[FR][16], ds[FR][16];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float4 l4 = *reinterpret_cast<const float4 *>(&vec[buf][0][32 * n + 8 * e + 4 * h]);
                 const float4 d4 = *reinterpret_cast<const float4 *>(&vec[buf][1][32 * n + 8 * e + 4 * h]);
                 const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    p[4 * e + x] = fast_exp2(fmaf(s[4 * e + x], a.c2, -ls[x]));
-                    ds[4 * e + x] = z[4 * e + x] - dl[x];
-                }
+                for (int f = 0; f < FR; ++f)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        p[f][4 * e + x] = fast_exp2(fmaf(s[f][4 * e + x], a.c2, -ls[x]));
+                        ds[f][4 * e + x] = z[f][4 * e + x] - dl[x];
+                    }
             }
             if (!whole) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int4 p4 = *reinterpret_cast<const int4 *>(&vec[buf][2][32 * n + 8 * e + 4 * h]);
-                    const int ps[4] = {p4.x, p4.y, p4.z, p4.w};
+                for (int f = 0; f < FR; ++f) {
+                    // pair (p, j): p - W <= j <= p + up, p = p_first + 8 (e >> 2) + 4 h + (e & 3)
+                    const int d = w_first + 32 * f + (lane & 31) - p_first - 4 * h + a.W;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        if ((unsigned)(j - ps[x] + a.W) > (unsigned)(a.W + up)) p[4 * e + x] = 0.f;
+                    for (int e = 0; e < 16; ++e)
+                        if ((unsigned)(d - 8 * (e >> 2) - (e & 3)) > (unsigned)(a.W + up)) p[f][e] = 0.f;
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) ds[e] *= p[e];
-            tile_accum<T, D>(dv, gt + n * TL::SUB, p, lane);
-            tile_accum<T, D>(dk, qt + n * TL::SUB, ds, lane);
+            for (int f = 0; f < FR; ++f)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) ds[f][e] *= p[f][e];
+            sm_accum<T, D, FR>(dv, lds[buf][1] + n * TL::SUB, p, lane);
+            sm_accum<T, D, FR>(dk, lds[buf][0] + n * TL::SUB, ds, lane);
         }
+        i0 = next;
     }
 
-    if (j >= a.Lk) return;
-    if (a.parts > 1) {
-        float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * a.Lk + j) * 2 * D;
 #pragma unroll
-        for (int x = 0; x < D / 32; ++x)
+    for (int f = 0; f < FR; ++f) {
+        const int j = w_first + 32 * f + (lane & 31);
+        if (j >= a.Lk) continue;
+        bool live = j < lk;
+        if (live && a.mask_k) live = a.mask_k[(long)w.b * a.Lk + j] != 0;
+        if (a.parts > 1) {
+            float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * a.Lk + j) * 2 * D;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float f = live ? a.cs : 0.f;
-                float *at = out + 32 * x + 8 * e + 4 * h;
-                *reinterpret_cast<float4 *>(at) = live ? make_float4(dk[x][4 * e] * f, dk[x][4 * e + 1] * f, dk[x][4 * e + 2] * f, dk[x][4 * e + 3] * f) : make_float4(0.f, 0.f, 0.f, 0.f);
-                *reinterpret_cast<float4 *>(at + D) = live ? make_float4(dv[x][4 * e], dv[x][4 * e + 1], dv[x][4 * e + 2], dv[x][4 * e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-        return;
-    }
-    T *ok = reinterpret_cast<T *>(const_cast<void *>(a.ok.p)) + w.b * a.ok.b + w.hk * a.ok.h + j * a.ok.l;
-    T *ov = reinterpret_cast<T *>(const_cast<void *>(a.ov.p)) + w.b * a.ov.b + w.hk * a.ov.h + j * a.ov.l;
+            for (int x = 0; x < D / 32; ++x)
 #pragma unroll
-    for (int x = 0; x < D / 32; ++x)
+                for (int e = 0; e < 4; ++e) {
+                    float *o = out + 32 * x + 8 * e + 4 * h;
+                    *reinterpret_cast<float4 *>(o) = live ? make_float4(dk[f][x][4 * e] * a.cs, dk[f][x][4 * e + 1] * a.cs, dk[f][x][4 * e + 2] * a.cs, dk[f][x][4 * e + 3] * a.cs) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    *reinterpret_cast<float4 *>(o + D) = live ? make_float4(dv[f][x][4 * e], dv[f][x][4 * e + 1], dv[f][x][4 * e + 2], dv[f][x][4 * e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+        } else {
+            T *ok = reinterpret_cast<T *>(const_cast<void *>(a.ok.p)) + w.b * a.ok.b + w.hk * a.ok.h + j * a.ok.l;
+            T *ov = reinterpret_cast<T *>(const_cast<void *>(a.ov.p)) + w.b * a.ov.b + w.hk * a.ov.h + j * a.ov.l;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int f = 32 * x + 8 * e + 4 * h;
-            if (live) {
-                store4<T>(ok + f, dk[x][4 * e] * a.cs, dk[x][4 * e + 1] * a.cs, dk[x][4 * e + 2] * a.cs, dk[x][4 * e + 3] * a.cs);
-                store4<T>(ov + f, dv[x][4 * e], dv[x][4 * e + 1], dv[x][4 * e + 2], dv[x][4 * e + 3]);
-            } else {
-                store4<T>(ok + f, 0.f, 0.f, 0.f, 0.f);
-                store4<T>(ov + f, 0.f, 0.f, 0.f, 0.f);
-            }
+            for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int o = 32 * x + 8 * e + 4 * h;
+                    if (live) {
+                        store4<T>(ok + o, dk[f][x][4 * e] * a.cs, dk[f][x][4 * e + 1] * a.cs, dk[f][x][4 * e + 2] * a.cs, dk[f][x][4 * e + 3] * a.cs);
+                        store4<T>(ov + o, dv[f][x][4 * e], dv[f][x][4 * e + 1], dv[f][x][4 * e + 2], dv[f][x][4 * e + 3]);
+                    } else {
+                        store4<T>(ok + o, 0.f, 0.f, 0.f, 0.f);
+                        store4<T>(ov + o, 0.f, 0.f, 0.f, 0.f);
+                    }
+                }
         }
+    }
 }
 
 // ------------------------------------------------------------------ joining the parts of a walk
 enum { SM_JOIN_O, SM_JOIN_DQ, SM_JOIN_DKV };
-// A thread takes four features of a row: O from the parts' rows weighted by exp(their LSE - the row's), gradients as sums.
-template <typename T, int D, int WHAT> __global__ __launch_bounds__(NTHREADS) void sm_join_kernel(const SmArgs a)
+// A thread takes four features of a row over every slices-th part; the slices are joined by LDS in their order.  O: the parts'
+// rows weighted by exp(their LSE - the largest); gradients: sums.
+template <typename T, int D, int WHAT> __global__ __launch_bounds__(NTHREADS) void sm_join_kernel(const SmArgs a, int slices)
 {
-    constexpr int F = WHAT == SM_JOIN_DKV ? 2 * D : D;   // features of a part's row
+    constexpr int F = WHAT == SM_JOIN_DKV ? 2 * D : D, FT = F / 4;   // features of a part's row, threads for them
+    __shared__ float4 sx[NTHREADS];
+    __shared__ float sm[NTHREADS], sl[NTHREADS];
     const int R = WHAT == SM_JOIN_DKV ? a.Lk : a.Lq * a.G;
-    const long rows = (long)a.B * a.Hk * R, at = (long)blockIdx.x * NTHREADS + threadIdx.x;
-    const long row = at / (F / 4);
-    const int f = (int)(at - row * (F / 4)) * 4;
-    if (row >= rows) return;
+    const int f = (threadIdx.x % FT) * 4, rest = threadIdx.x / FT, slice = rest % slices;
+    const long rows = (long)a.B * a.Hk * R, row = (long)blockIdx.x * (NTHREADS / FT / slices) + rest / slices;
+    const bool have = row < rows;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = -INFINITY, l = 0.f;
+    if (have) {
+#pragma unroll 4
+        for (int s = slice; s < a.parts; s += slices) {
+            const float4 y = *reinterpret_cast<const float4 *>(a.part + (s * rows + row) * F + f);
+            float c = 1.f;
+            if constexpr (WHAT == SM_JOIN_O) {
+                const float lse = a.part_lse[s * rows + row], mn = fmaxf(m, lse);
+                const float old = mn > -INFINITY ? fast_exp2((m - mn) * LOG2E) : 0.f;
+                c = mn > -INFINITY ? fast_exp2((lse - mn) * LOG2E) : 0.f;
+                l = fmaf(l, old, c);
+                x.x *= old; x.y *= old; x.z *= old; x.w *= old;
+                m = mn;
+            }
+            x.x = fmaf(c, y.x, x.x); x.y = fmaf(c, y.y, x.y); x.z = fmaf(c, y.z, x.z); x.w = fmaf(c, y.w, x.w);
+        }
+    }
+    if (slices > 1) {
+        sx[threadIdx.x] = x;
+        sm[threadIdx.x] = m;
+        sl[threadIdx.x] = l;
+        __syncthreads();
+        if (slice) return;
+        for (int s = 1; s < slices; ++s) {
+            const int o = threadIdx.x + s * FT;
+            const float4 y = sx[o];
+            float c = 1.f, old = 1.f;
+            if constexpr (WHAT == SM_JOIN_O) {
+                const float mn = fmaxf(m, sm[o]);
+                old = mn > -INFINITY ? fast_exp2((m - mn) * LOG2E) : 0.f;
+                c = mn > -INFINITY ? fast_exp2((sm[o] - mn) * LOG2E) : 0.f;
+                l = l * old + sl[o] * c;
+                m = mn;
+            }
+            x.x = x.x * old + y.x * c; x.y = x.y * old + y.y * c; x.z = x.z * old + y.z * c; x.w = x.w * old + y.w * c;
+        }
+    }
+    if (!have) return;
     const int prob = (int)(row / R), r = (int)(row - (long)prob * R), b = prob / a.Hk, hk = prob - b * a.Hk;
-    float x[4] = {0.f, 0.f, 0.f, 0.f}, lse = 0.f, top = -INFINITY;
-    if constexpr (WHAT == SM_JOIN_O) {
-        for (int s = 0; s < a.parts; ++s) top = fmaxf(top, a.part_lse[s * rows + row]);
-        float sum = 0.f;
-        if (top > -INFINITY)
-            for (int s = 0; s < a.parts; ++s) sum += fast_exp2((a.part_lse[s * rows + row] - top) * LOG2E);
-        lse = top > -INFINITY ? top + fast_log2(sum) * LN2 : -INFINITY;
-    }
-    for (int s = 0; s < a.parts; ++s) {
-        const float4 y = *reinterpret_cast<const float4 *>(a.part + (s * rows + row) * F + f);
-        float c = 1.f;
-        if constexpr (WHAT == SM_JOIN_O) c = top > -INFINITY ? fast_exp2((a.part_lse[s * rows + row] - lse) * LOG2E) : 0.f;
-        x[0] = fmaf(c, y.x, x[0]); x[1] = fmaf(c, y.y, x[1]); x[2] = fmaf(c, y.z, x[2]); x[3] = fmaf(c, y.w, x[3]);
-    }
     if constexpr (WHAT == SM_JOIN_DKV) {
         const SmTensor &t = f < D ? a.ok : a.ov;
         T *out = reinterpret_cast<T *>(const_cast<void *>(t.p)) + b * t.b + hk * t.h + r * t.l;
-        store4<T>(out + (f < D ? f : f - D), x[0], x[1], x[2], x[3]);
+        store4<T>(out + (f < D ? f : f - D), x.x, x.y, x.z, x.w);
     } else {
         const int i = r / a.G, hq = hk * a.G + (r - i * a.G);
+        const float c = WHAT == SM_JOIN_O ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
         T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + b * a.oq.b + hq * a.oq.h + i * a.oq.l;
-        store4<T>(out + f, x[0], x[1], x[2], x[3]);
-        if (WHAT == SM_JOIN_O && f == 0) a.lse[((long)b * a.Hk * a.G + hq) * a.Lq + i] = lse;
+        store4<T>(out + f, x.x * c, x.y * c, x.z * c, x.w * c);
+        if (WHAT == SM_JOIN_O && f == 0) a.lse[((long)b * a.Hk * a.G + hq) * a.Lq + i] = l > 0.f ? m + fast_log2(l) * LN2 : -INFINITY;
     }
 }
 

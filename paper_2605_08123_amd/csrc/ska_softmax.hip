@@ -28,11 +28,12 @@ int check(const SmProblem &p)
 // How one kernel of a call is launched: wavefronts per workgroup, blocks of owners, parts of a walk
 struct SmGrid { int nw; long blocks; int parts; };
 // owners: rows of the side that is kept; walk: rows of the other side that a block may meet, at most
-SmGrid sm_grid(const SmProblem &p, long owners, long walk)
+SmGrid sm_grid(const SmProblem &p, int what, long owners, long walk)
 {
     SmGrid g{4, 0, 1};
     if (owners <= 32) g.nw = 1;
-    g.blocks = (owners + 32 * g.nw - 1) / (32 * g.nw);
+    const int rows = 32 * g.nw * sm_fr(what, p.dtype == SKA_F32 ? 4 : 2, p.d, g.nw);
+    g.blocks = (owners + rows - 1) / rows;
     const long tile = p.dtype == SKA_BF16 ? 64 : 32, tiles = (walk + tile - 1) / tile, waves = g.blocks * p.N() * g.nw;
     if (waves < 1024) g.parts = (int)std::max(1L, std::min({2048 / waves, tiles / 4, 256L}));
     return g;
@@ -40,28 +41,28 @@ SmGrid sm_grid(const SmProblem &p, long owners, long walk)
 long walk_of_rows(const SmProblem &p)
 {
     const long W = std::min<long>(p.W, p.Lk);
-    return std::min<long>(p.Lk, (p.Lq < 128 ? p.Lq : 128) + W + (p.causal ? 0 : W));
+    return std::min<long>(p.Lk, std::min(p.Lq, 256) + W + (p.causal ? 0 : W));
 }
 long walk_of_keys(const SmProblem &p)
 {
     const long W = std::min<long>(p.W, p.Lq);
-    return std::min<long>(p.Lq, (p.Lk < 128 ? p.Lk : 128) + W + (p.causal ? 0 : W)) * p.G();
+    return std::min<long>(p.Lq, std::min(p.Lk, 256) + W + (p.causal ? 0 : W)) * p.G();
 }
-SmGrid rows_grid(const SmProblem &p) { return sm_grid(p, p.R(), walk_of_rows(p)); }
-SmGrid keys_grid(const SmProblem &p) { return sm_grid(p, p.Lk, walk_of_keys(p)); }
+SmGrid rows_grid(const SmProblem &p, int what) { return sm_grid(p, what, p.R(), walk_of_rows(p)); }
+SmGrid keys_grid(const SmProblem &p) { return sm_grid(p, SM_DKV, p.Lk, walk_of_keys(p)); }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 size_t delta_bytes(const SmProblem &p) { return up256((size_t)p.N() * p.R() * sizeof(float)); }
 size_t part_lse_bytes(const SmProblem &p, const SmGrid &g) { return g.parts > 1 ? up256((size_t)g.parts * p.N() * p.R() * sizeof(float)) : 0; }
 size_t ws_fwd(const SmProblem &p)
 {
-    const SmGrid g = rows_grid(p);
+    const SmGrid g = rows_grid(p, SM_FWD);
     return g.parts > 1 ? part_lse_bytes(p, g) + (size_t)g.parts * p.N() * p.R() * p.d * sizeof(float) : 0;
 }
 size_t ws_bwd(const SmProblem &p)
 {
-    const SmGrid r = rows_grid(p), k = keys_grid(p);
+    const SmGrid r = rows_grid(p, SM_DQ), k = keys_grid(p);
     const size_t pr = r.parts > 1 ? (size_t)r.parts * p.N() * p.R() * p.d : 0, pk = k.parts > 1 ? (size_t)k.parts * p.N() * p.Lk * 2 * p.d : 0;
-    return delta_bytes(p) + std::max(pr, pk) * sizeof(float);   // (one after the other)
+    return 2 * delta_bytes(p) + std::max(pr, pk) * sizeof(float);   // (one after the other)
 }
 
 // strides in bytes multiples of 16; SKA_EINVAL where they cannot be strides, SKA_EUNSUPPORTED where the kernels cannot use them
@@ -80,6 +81,7 @@ int tensor_of(SmTensor &t, const void *p, const ska_strides *s, int B, int H, lo
         t.l = d; t.h = L * d; t.b = t.h * H;
     }
     const long e = dtype == SKA_F32 ? 4 : 2;
+    if (t.l * e >= 1L << 27) return SKA_EUNSUPPORTED;   // (rows of a load instruction, 16 at most, lie within 32 bits)
     const unsigned long off = (unsigned long)reinterpret_cast<uintptr_t>(p) | (unsigned long)((t.b | t.h | t.l) * e);
     return off & 15 ? SKA_EUNSUPPORTED : SKA_OK;
 }
@@ -141,7 +143,7 @@ int ska_softmax_attn_fwd(const void *Q, const ska_strides *q_strides, const void
     const size_t need = ws_fwd(p);
     if (need && (!workspace || workspace_bytes < need)) return SKA_EWORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 15) return SKA_EINVAL;
-    const SmGrid g = rows_grid(p);
+    const SmGrid g = rows_grid(p, SM_FWD);
     a.part_lse = static_cast<float *>(workspace);
     a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + part_lse_bytes(p, g));
     return launch(SM_FWD, p, g, a, static_cast<hipStream_t>(stream));
@@ -169,10 +171,11 @@ int ska_softmax_attn_bwd(const void *Q, const ska_strides *q_strides, const void
     if ((rc = tensor_of(a.ov, dV, dv_strides, B, Hk, Lk, d, dtype, true)) != SKA_OK) return rc;
     if (!workspace || workspace_bytes < ws_bwd(p)) return SKA_EWORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 15) return SKA_EINVAL;
-    a.delta = static_cast<float *>(workspace);
-    a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + delta_bytes(p));
+    a.lse2 = static_cast<float *>(workspace);
+    a.delta = a.lse2 + delta_bytes(p) / sizeof(float);
+    a.part = a.delta + delta_bytes(p) / sizeof(float);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    rc = launch(SM_DQ, p, rows_grid(p), a, st);   // (writes delta, which dK reads)
+    rc = launch(SM_DQ, p, rows_grid(p, SM_DQ), a, st);   // (writes delta, which dK reads)
     return rc != SKA_OK ? rc : launch(SM_DKV, p, keys_grid(p), a, st);
 }
 

@@ -5,7 +5,6 @@
 #include "ska_softmax.h"
 
 // what: SM_FWD, SM_DQ or SM_DKV; nw: wavefronts of a workgroup, 1 or 4; args: SmArgs.  Joins the parts where there are several.
-enum { SM_FWD, SM_DQ, SM_DKV };
 #define SKA_DECLARE_SOFTMAX(NAME) extern "C" __attribute__((visibility("hidden"))) int NAME(int what, int nw, const void *args, hipStream_t st)
 SKA_DECLARE_SOFTMAX(ska_launch_softmax_f32_32);
 SKA_DECLARE_SOFTMAX(ska_launch_softmax_f32_64);
