@@ -83,6 +83,23 @@ template <typename T, int D> struct SmTile {
     }
 };
 
+// one such load: 16 bytes a lane from `base` + `at` into `lds` + 16 lane (lds, base uniform: said once more, where a kernel runs
+// out of scalar registers)
+__device__ __forceinline__ const unsigned char *sm_uniform(const unsigned char *p)
+{
+    const unsigned long x = (unsigned long)p;
+    return reinterpret_cast<const unsigned char *>((unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)x) |
+                                                   (unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
+}
+__device__ __forceinline__ void sm_load_pieces(unsigned lds, const unsigned char *base, unsigned at)
+{
+    // (written out, because the compiler takes every later LDS read for one of these bytes and waits at once; the kernel
+    // waits where it needs them.  No register is written.)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(at),
+                 "s"(sm_uniform(base))
+                 : "memory", "m0");
+}
+
 // Tiles come by loads that write LDS directly, KT / RPI instructions a tile dealt to the NW wavefronts: no registers, no
 // stores, and the next tile is under way while this one is worked on.
 template <typename T, int D, int NW> struct SmLoader {
@@ -93,25 +110,26 @@ template <typename T, int D, int NW> struct SmLoader {
     __device__ __forceinline__ SmLoader(int lane, int wv) : lane(lane), wv(wv), lrow(lane / TL::CPR) {}
     // first row of instruction k; this lane's row is lrow below it
     __device__ __forceinline__ int first(int k) const { return (wv + NW * k) * TL::RPI; }
+    // byte of a row that this lane brings: its place in LDS is fixed, and the chunk that belongs there depends on the row
+    // (the swizzle takes single bits of the row: that of a sum without carries is the exclusive or)
+    __device__ __forceinline__ unsigned col(int k) const { return (unsigned)((lane % TL::CPR) ^ TL::swz(lrow) ^ TL::swz(first(k))) * 16; }
     // rows 0 ... rows - 1 of the tile at `base` (uniform), `stride` bytes apart, exist: the others repeat the last one
     __device__ __forceinline__ void load(unsigned lds, const unsigned char *base, long stride, int rows) const
     {
-        const bool whole = rows >= TL::KT;
+        lds += (unsigned)wv * 1024;
+        if (rows >= TL::KT) {
+            const unsigned char *at = base + wv * (TL::RPI * stride);
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const int r0 = first(k);
-            // (the swizzle takes single bits of the row: that of a sum without carries is the exclusive or)
-            const unsigned col = (unsigned)((lane % TL::CPR) ^ TL::swz(lrow) ^ TL::swz(r0)) * 16;
-            int r = r0, l = lrow;
-            if (!whole) {
-                r = min(r0, rows - 1);
-                l = min(lrow, rows - 1 - r);
+            for (int k = 0; k < PER; ++k) {
+                sm_load_pieces(lds + k * NW * 1024, at, (unsigned)lrow * (unsigned)stride + col(k));
+                at += NW * TL::RPI * stride;
             }
-            // (written out, because the compiler takes every later LDS read for one of these bytes and waits at once; the
-            // kernel waits where it needs them.  No register is written.)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds + (unsigned)r0 * TL::ROWB),
-                         "v"((unsigned)l * (unsigned)stride + col), "s"(base + r * stride)
-                         : "memory", "m0");
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < PER; ++k) {
+                const int r = min(first(k), rows - 1), l = min(lrow, rows - 1 - r);
+                sm_load_pieces(lds + k * NW * 1024, base + r * stride, (unsigned)l * (unsigned)stride + col(k));
+            }
         }
     }
     // after this wavefront's loads have arrived: zeros into those of its rows that do not count
@@ -368,9 +386,9 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
         loader.load(lds_at + (buf * 2 + 1) * TL::BYTES, vb + j0 * vs, vs, rows);
         if (mk) act.load(loader, mk + j0, rows);
     };
-    if (tiles > 0) fetch(j_lo, 0);
-    for (int t = 0; t < tiles; ++t) {
-        const int j0 = j_lo + t * KT, buf = t & 1;
+    auto step = [&](auto which, int t) {
+        constexpr int buf = decltype(which)::value;   // (a constant: LDS addresses are offsets of the instructions)
+        const int j0 = j_lo + t * KT;
         sm_arrived();
         unsigned long long here = ~0ull;   // active keys
         if (j_hi + 1 - j0 < KT || mk) {    // (products with rows that do not count must not meet what they hold)
@@ -385,7 +403,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
         __syncthreads();
         if (t + 1 < tiles) fetch(j0 + KT, buf ^ 1);
         if constexpr (!BWD) {
-            if (j0 > w_hi || j0 + KT - 1 < w_lo) continue;
+            if (j0 > w_hi || j0 + KT - 1 < w_lo) return;
             const bool whole = j0 >= all_lo && j0 + KT - 1 <= all_hi && here == ~0ull;
             f32x16 s[NS][FR];
 #pragma unroll
@@ -466,6 +484,11 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                 sm_accum<T, D, FR>(acc, lds[buf][0] + n * TL::SUB, p, lane);
             }
         }
+    };
+    if (tiles > 0) fetch(j_lo, 0);
+    for (int t = 0; t < tiles; t += 2) {
+        step(std::integral_constant<int, 0>{}, t);
+        if (t + 1 < tiles) step(std::integral_constant<int, 1>{}, t + 1);
     }
 
 #pragma unroll
@@ -575,9 +598,9 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
         if (++at == per_head) { at = 0; ++head; }
     };
     int i0 = i_lo + at * KT;   // first query of the tile at hand
-    if (NBUF == 2 && t0 < t1) fetch(0);
-    for (int t = t0; t < t1; ++t) {
-        const int buf = NBUF == 2 ? (t - t0) & 1 : 0, rows = i_hi + 1 - i0;
+    auto step = [&](auto which, int t) {
+        constexpr int buf = decltype(which)::value;
+        const int rows = i_hi + 1 - i0;
         if (NBUF == 1) {
             if (t > t0) __syncthreads();
             fetch(0);
@@ -635,6 +658,11 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
             sm_accum<T, D, FR>(dk, lds[buf][0] + n * TL::SUB, ds, lane);
         }
         i0 = next;
+    };
+    if (NBUF == 2 && t0 < t1) fetch(0);
+    for (int t = t0; t < t1; t += 2) {
+        step(std::integral_constant<int, 0>{}, t);
+        if (t + 1 < t1) step(std::integral_constant<int, NBUF - 1>{}, t + 1);
     }
 
 #pragma unroll
