@@ -58,36 +58,48 @@ def _code(t: torch.Tensor) -> int:
     return c
 
 
-def _on_gpu(x: torch.Tensor, name: str):
+# (A call of a microsecond's work is bound by what follows here: sizes are compared as they are, contiguous tensors pass no
+# strides, and the device and its stream are asked for once.)
+_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+
+
+def _here(x: torch.Tensor, name: str) -> int:
+    """The current device's number, which x must live on."""
     if not x.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
-    if x.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} lives on {x.device}, the current device is cuda:{torch.cuda.current_device()}")
+    dev = _device()
+    if x.get_device() != dev:
+        raise ValueError(f"{name} lives on {x.device}, the current device is cuda:{dev}")
+    return dev
 
 
-def _plain(x, shape, dtype, name):
+def _wrong(x, shape, dtype, dev, name, contiguous=""):
+    if not x.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if x.get_device() != dev:
+        raise ValueError(f"{name} lives on {x.device}, the other tensors on cuda:{dev}")
+    raise ValueError(f"{name}: expected {contiguous}{tuple(shape)} {dtype}, got {tuple(x.shape)} {x.dtype}")
+
+
+def _plain(x, shape, dtype, dev, name):
     """Pointer of an optional contiguous tensor."""
     if x is None:
         return None
-    _on_gpu(x, name)
-    if tuple(x.shape) != tuple(shape) or x.dtype != dtype or not x.is_contiguous():
-        raise ValueError(f"{name}: expected contiguous {tuple(shape)} {dtype}, got {tuple(x.shape)} {x.dtype}")
+    if x.get_device() != dev or x.shape != shape or x.dtype != dtype or not x.is_contiguous():
+        _wrong(x, shape, dtype, dev, name, "contiguous ")
     return x.data_ptr()
 
 
-def _heads(x, shape, dtype, name):
-    """Pointer and strides of a [B, H, L, d] tensor."""
-    _on_gpu(x, name)
-    if tuple(x.shape) != tuple(shape) or x.dtype != dtype:
-        raise ValueError(f"{name}: expected {tuple(shape)} {dtype}, got {tuple(x.shape)} {x.dtype}")
+def _heads(x, shape, dtype, dev, name):
+    """Pointer and strides of a [B, H, L, d] tensor (no strides: contiguous)."""
+    if x.get_device() != dev or x.shape != shape or x.dtype != dtype:
+        _wrong(x, shape, dtype, dev, name)
+    if x.is_contiguous():
+        return x.data_ptr(), None
     b, h, l, f = x.stride()
     if f != 1 and shape[3] > 1:
         raise ValueError(f"{name}: the features of a token must lie next to each other")
     return x.data_ptr(), ctypes.byref(Strides(b, h, l))   # (the reference keeps it alive)
-
-
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
 
 
 def _done(rc):
@@ -95,29 +107,28 @@ def _done(rc):
         raise SinkhornAttnError(rc)
 
 
-def _workspace(given, need, device):
+def _workspace(given, need, like, dev):
+    """Pointer and bytes of the caller's workspace or of one of this call, and what keeps it alive until the launch."""
     if given is not None:
-        _on_gpu(given, "workspace")
+        if given.get_device() != dev or not given.is_contiguous():
+            raise ValueError("workspace: expected a contiguous tensor on the current device")
         return given.data_ptr(), given.numel() * given.element_size(), given
     if not need:
         return None, 0, None
-    w = torch.empty(need, device=device, dtype=torch.uint8)
+    w = like.new_empty(need, dtype=torch.uint8)
     return w.data_ptr(), need, w
 
 
 # ------------------------------------------------------------------ layer norm
-def _rows(x, like, name):
-    """Pointer and row distance of a tensor of `like`'s shape and type whose leading dimensions are evenly spaced rows."""
-    _on_gpu(x, name)
-    if x.shape != like.shape or x.dtype != like.dtype:
-        raise ValueError(f"{name}: expected {tuple(like.shape)} {like.dtype}, got {tuple(x.shape)} {x.dtype}")
-    shape, stride = x.shape, x.stride()
-    if x.dim() < 1 or shape[-1] < 1:
-        raise ValueError(f"{name}: needs features in its last dimension")
-    if stride[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"{name}: the features of a row must lie next to each other")
+def _rows(x, shape, dtype, dev, name):
+    """Pointer and row distance of a tensor whose leading dimensions are evenly spaced rows."""
+    if x.get_device() != dev or x.shape != shape or x.dtype != dtype:
+        _wrong(x, shape, dtype, dev, name)
     if x.is_contiguous():
         return x.data_ptr(), shape[-1]
+    stride = x.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: the features of a row must lie next to each other")
     ld, rows = None, 1   # dimensions from the last row dimension outwards: each steps over the whole of the ones inside it
     for n, s in zip(reversed(shape[:-1]), reversed(stride[:-1])):
         if n == 1:
@@ -130,30 +141,40 @@ def _rows(x, like, name):
     return x.data_ptr(), shape[-1] if ld is None else ld
 
 
+def _features(x, name):
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"{name}: needs features in its last dimension")
+    return x.shape[-1]
+
+
 def ska_layer_norm_fwd(X, weight=None, bias=None, residual=None, eps=1e-5, Y=None, S=None, stats=None):
     """Layer norm over the last dimension of X, or of X + residual.  weight, bias: [D], of X's type or float32.
     Returns (Y, S, stats): S the sum (X itself without a residual), stats [2, rows...] float32, as the backward takes them."""
-    xp, ldx = _rows(X, X, "X")
-    D = X.shape[-1]
+    dev, shape, dt, D = _here(X, "X"), X.shape, X.dtype, _features(X, "X")
+    xp, ldx = _rows(X, shape, dt, dev, "X")
     w = weight if weight is not None else bias
-    wp = _plain(weight, (D,), w.dtype, "weight") if w is not None else None
-    bp = _plain(bias, (D,), w.dtype, "bias") if w is not None else None
-    Y = torch.empty(X.shape, device=X.device, dtype=X.dtype) if Y is None else Y
-    yp, ldy = _rows(Y, X, "Y")
+    wp = bp = None
+    if w is not None:
+        wp, bp = _plain(weight, (D,), w.dtype, dev, "weight"), _plain(bias, (D,), w.dtype, dev, "bias")
+    if Y is None:
+        Y = X.new_empty(shape)
+    yp, ldy = _rows(Y, shape, dt, dev, "Y")
     rp = sp = None
     ldr = lds = 0
     if residual is not None:
-        rp, ldr = _rows(residual, X, "residual")
-        S = torch.empty(X.shape, device=X.device, dtype=X.dtype) if S is None else S
-        sp, lds = _rows(S, X, "S")
+        rp, ldr = _rows(residual, shape, dt, dev, "residual")
+        if S is None:
+            S = X.new_empty(shape)
+        sp, lds = _rows(S, shape, dt, dev, "S")
+    elif S is not None:
+        raise ValueError("S is the sum with a residual: there is none")
     else:
-        if S is not None:
-            raise ValueError("S is the sum with a residual: there is none")
         S = X
-    shape = (2,) + tuple(X.shape[:-1])
-    stats = torch.empty(shape, device=X.device, dtype=torch.float32) if stats is None else stats
-    _done(_lib().ska_layer_norm_fwd(xp, ldx, rp, ldr, wp, bp, sp, lds, yp, ldy, _plain(stats, shape, torch.float32, "stats"),
-                                    X.numel() // D, D, eps, _code(X), SKA_F32 if w is None else _code(w), _stream()))
+    sshape = (2,) + shape[:-1]
+    if stats is None:
+        stats = X.new_empty(sshape, dtype=torch.float32)
+    _done(_lib().ska_layer_norm_fwd(xp, ldx, rp, ldr, wp, bp, sp, lds, yp, ldy, _plain(stats, sshape, torch.float32, dev, "stats"),
+                                    X.numel() // D, D, eps, _code(X), SKA_F32 if w is None else _code(w), _raw_stream(dev)))
     return Y, S, stats
 
 
@@ -165,24 +186,25 @@ def ska_layer_norm_bwd(dY, S, weight, stats, dS=None, want_weight=True, want_bia
                        workspace=None):
     """Gradient of ska_layer_norm_fwd: S, stats as it returned them, dS the gradient that reaches S on the residual's way.
     Returns (dX, dweight, dbias): dX is that of X and of the residual; the others are None where they are not wanted."""
-    gp, ldg = _rows(dY, S, "dY")
-    sp, lds = _rows(S, S, "S")
-    D = S.shape[-1]
+    dev, shape, dt, D = _here(S, "S"), S.shape, S.dtype, _features(S, "S")
+    gp, ldg = _rows(dY, shape, dt, dev, "dY")
+    sp, lds = _rows(S, shape, dt, dev, "S")
     N = S.numel() // D
     wt = torch.float32 if weight is None else weight.dtype
-    wp = _plain(weight, (D,), wt, "weight")
-    rp, ldr = _rows(dS, S, "dS") if dS is not None else (None, 0)
-    dX = torch.empty(S.shape, device=S.device, dtype=S.dtype) if dX is None else dX
-    xp, ldx = _rows(dX, S, "dX")
+    wp = _plain(weight, (D,), wt, dev, "weight")
+    rp, ldr = _rows(dS, shape, dt, dev, "dS") if dS is not None else (None, 0)
+    if dX is None:
+        dX = S.new_empty(shape)
+    xp, ldx = _rows(dX, shape, dt, dev, "dX")
     if want_weight and dweight is None:
-        dweight = torch.empty(D, device=S.device, dtype=wt)
+        dweight = S.new_empty(D, dtype=wt)
     if want_bias and dbias is None:
-        dbias = torch.empty(D, device=S.device, dtype=wt)
-    dwp, dbp = _plain(dweight, (D,), wt, "dweight"), _plain(dbias, (D,), wt, "dbias")
+        dbias = S.new_empty(D, dtype=wt)
+    dwp, dbp = _plain(dweight, (D,), wt, dev, "dweight"), _plain(dbias, (D,), wt, dev, "dbias")
     lib = _lib()
-    ws, n, keep = _workspace(workspace, lib.ska_layer_norm_workspace_bytes(N, D) if dwp or dbp else 0, S.device)
-    _done(lib.ska_layer_norm_bwd(gp, ldg, sp, lds, wp, _plain(stats, (2,) + tuple(S.shape[:-1]), torch.float32, "stats"), rp, ldr, xp, ldx,
-                                 dwp, dbp, N, D, _code(S), SKA_F32 if weight is None else _code(weight), ws, n, _stream()))
+    ws, n, keep = _workspace(workspace, lib.ska_layer_norm_workspace_bytes(N, D) if dwp or dbp else 0, S, dev)
+    _done(lib.ska_layer_norm_bwd(gp, ldg, sp, lds, wp, _plain(stats, (2,) + shape[:-1], torch.float32, dev, "stats"), rp, ldr, xp, ldx,
+                                 dwp, dbp, N, D, _code(S), SKA_F32 if weight is None else _code(weight), ws, n, _raw_stream(dev)))
     return dX, dweight, dbias
 
 
@@ -202,25 +224,29 @@ def ska_rope_frequencies(rot, base=10000.0, scaling="none", factor=1.0, trained_
 def _rope(call, Q, K, freq, amplitude, interleaved, start, positions, Qo, Ko, names):
     if Q.dim() != 4:
         raise ValueError(f"{names[0]}: expected [B, H, L, d], got {tuple(Q.shape)}")
-    B, Hq, L, d = Q.shape
-    qp, qs = _heads(Q, Q.shape, Q.dtype, names[0])
-    Qo = torch.empty(Q.shape, device=Q.device, dtype=Q.dtype) if Qo is None else Qo
-    op, os = _heads(Qo, Q.shape, Q.dtype, names[2])
+    dev, shape, dt = _here(Q, names[0]), Q.shape, Q.dtype
+    B, Hq, L, d = shape
+    qp, qs = _heads(Q, shape, dt, dev, names[0])
+    if Qo is None:
+        Qo = Q.new_empty(shape)
+    op, os = _heads(Qo, shape, dt, dev, names[2])
     kp = kop = ks = kos = None
     Hk = 0
     if K is not None:
         Hk = K.shape[1] if K.dim() == 4 else 0
-        kp, ks = _heads(K, (B, Hk, L, d), Q.dtype, names[1])
-        Ko = torch.empty(K.shape, device=Q.device, dtype=Q.dtype) if Ko is None else Ko
-        kop, kos = _heads(Ko, K.shape, Q.dtype, names[3])
+        kshape = (B, Hk, L, d)
+        kp, ks = _heads(K, kshape, dt, dev, names[1])
+        if Ko is None:
+            Ko = Q.new_empty(kshape)
+        kop, kos = _heads(Ko, kshape, dt, dev, names[3])
     elif Ko is not None:
         raise ValueError(f"{names[3]} without {names[1]}")
     if freq.dim() != 1:
         raise ValueError(f"freq: expected one dimension, got {tuple(freq.shape)}")
-    fp = _plain(freq, freq.shape, torch.float64, "freq")
-    _done(call(qp, qs, op, os, kp, ks, kop, kos, fp, amplitude, _plain(start, (B,), torch.int32, "start"),
-               _plain(positions, (B, L), torch.int32, "positions"), B, Hq, Hk, L, d, 2 * freq.shape[0], int(bool(interleaved)), _code(Q),
-               _stream()))
+    pairs = freq.shape[0]
+    _done(call(qp, qs, op, os, kp, ks, kop, kos, _plain(freq, (pairs,), torch.float64, dev, "freq"), amplitude,
+               _plain(start, (B,), torch.int32, dev, "start"), _plain(positions, (B, L), torch.int32, dev, "positions"), B, Hq, Hk, L, d,
+               2 * pairs, 1 if interleaved else 0, _code(Q), _raw_stream(dev)))
     return Qo, Ko
 
 
@@ -254,20 +280,22 @@ def ska_softmax_attn_fwd(Q, K, V, W, causal=False, eps=1.0, len_q=None, len_k=No
     only), scores / (eps sqrt d).  len_q, len_k, start_q: int32 CUDA tensors [B]; mask_q, mask_k: uint8 [B,Lq], [B,Lk]
     (nonzero = active).  Returns (O, LSE [B,Hq,Lq] float32); a query without a key: 0, -inf."""
     B, Hq, Hk, Lq, Lk, d = _sizes(Q, K)
-    dt, code = Q.dtype, _code(Q)
-    qp, qs = _heads(Q, Q.shape, dt, "Q")
-    kp, ks = _heads(K, (B, Hk, Lk, d), dt, "K")
-    vp, vs = _heads(V, (B, Hk, Lk, d), dt, "V")
-    O = torch.empty(Q.shape, device=Q.device, dtype=dt) if O is None else O
-    op, os = _heads(O, Q.shape, dt, "O")
-    LSE = torch.empty((B, Hq, Lq), device=Q.device, dtype=torch.float32) if LSE is None else LSE
+    dev, qshape, kshape, dt, code = _here(Q, "Q"), Q.shape, (B, Hk, Lk, d), Q.dtype, _code(Q)
+    qp, qs = _heads(Q, qshape, dt, dev, "Q")
+    kp, ks = _heads(K, kshape, dt, dev, "K")
+    vp, vs = _heads(V, kshape, dt, dev, "V")
+    if O is None:
+        O = Q.new_empty(qshape)
+    op, os = _heads(O, qshape, dt, dev, "O")
+    if LSE is None:
+        LSE = Q.new_empty((B, Hq, Lq), dtype=torch.float32)
     lib = _lib()
-    W, causal = int(W), int(bool(causal))
-    ws, n, keep = _workspace(workspace, lib.ska_softmax_attn_workspace_bytes(0, B, Hq, Hk, Lq, Lk, d, W, causal, code), Q.device)
+    W, causal, i32, u8 = int(W), 1 if causal else 0, torch.int32, torch.uint8
+    ws, n, keep = _workspace(workspace, lib.ska_softmax_attn_workspace_bytes(0, B, Hq, Hk, Lq, Lk, d, W, causal, code), Q, dev)
     _done(lib.ska_softmax_attn_fwd(
-        qp, qs, kp, ks, vp, vs, op, os, _plain(LSE, (B, Hq, Lq), torch.float32, "LSE"), _plain(start_q, (B,), torch.int32, "start_q"),
-        _plain(len_q, (B,), torch.int32, "len_q"), _plain(len_k, (B,), torch.int32, "len_k"), _plain(mask_q, (B, Lq), torch.uint8, "mask_q"),
-        _plain(mask_k, (B, Lk), torch.uint8, "mask_k"), B, Hq, Hk, Lq, Lk, d, W, causal, eps, code, ws, n, _stream()))
+        qp, qs, kp, ks, vp, vs, op, os, _plain(LSE, (B, Hq, Lq), torch.float32, dev, "LSE"), _plain(start_q, (B,), i32, dev, "start_q"),
+        _plain(len_q, (B,), i32, dev, "len_q"), _plain(len_k, (B,), i32, dev, "len_k"), _plain(mask_q, (B, Lq), u8, dev, "mask_q"),
+        _plain(mask_k, (B, Lk), u8, dev, "mask_k"), B, Hq, Hk, Lq, Lk, d, W, causal, eps, code, ws, n, _raw_stream(dev)))
     return O, LSE
 
 
@@ -275,22 +303,27 @@ def ska_softmax_attn_bwd(Q, K, V, O, dO, LSE, W, causal=False, eps=1.0, len_q=No
                          start_q=None, dQ=None, dK=None, dV=None, workspace=None):
     """Gradient of ska_softmax_attn_fwd (O, LSE as it returned them, the same other arguments).  Returns (dQ, dK, dV)."""
     B, Hq, Hk, Lq, Lk, d = _sizes(Q, K)
-    dt, code = Q.dtype, _code(Q)
-    kv = (B, Hk, Lk, d)
-    ptrs = []
-    for name, x, shape in (("Q", Q, Q.shape), ("K", K, kv), ("V", V, kv), ("O", O, Q.shape), ("dO", dO, Q.shape)):
-        ptrs += _heads(x, shape, dt, name)
-    dQ = torch.empty(Q.shape, device=Q.device, dtype=dt) if dQ is None else dQ
-    dK = torch.empty(kv, device=Q.device, dtype=dt) if dK is None else dK
-    dV = torch.empty(kv, device=Q.device, dtype=dt) if dV is None else dV
-    outs = []
-    for name, x, shape in (("dQ", dQ, Q.shape), ("dK", dK, kv), ("dV", dV, kv)):
-        outs += _heads(x, shape, dt, name)
+    dev, qshape, kshape, dt, code = _here(Q, "Q"), Q.shape, (B, Hk, Lk, d), Q.dtype, _code(Q)
+    qp, qs = _heads(Q, qshape, dt, dev, "Q")
+    kp, ks = _heads(K, kshape, dt, dev, "K")
+    vp, vs = _heads(V, kshape, dt, dev, "V")
+    op, os = _heads(O, qshape, dt, dev, "O")
+    gp, gs = _heads(dO, qshape, dt, dev, "dO")
+    if dQ is None:
+        dQ = Q.new_empty(qshape)
+    if dK is None:
+        dK = K.new_empty(kshape)
+    if dV is None:
+        dV = K.new_empty(kshape)
+    dqp, dqs = _heads(dQ, qshape, dt, dev, "dQ")
+    dkp, dks = _heads(dK, kshape, dt, dev, "dK")
+    dvp, dvs = _heads(dV, kshape, dt, dev, "dV")
     lib = _lib()
-    W, causal = int(W), int(bool(causal))
-    ws, n, keep = _workspace(workspace, lib.ska_softmax_attn_workspace_bytes(1, B, Hq, Hk, Lq, Lk, d, W, causal, code), Q.device)
+    W, causal, i32, u8 = int(W), 1 if causal else 0, torch.int32, torch.uint8
+    ws, n, keep = _workspace(workspace, lib.ska_softmax_attn_workspace_bytes(1, B, Hq, Hk, Lq, Lk, d, W, causal, code), Q, dev)
     _done(lib.ska_softmax_attn_bwd(
-        *ptrs, _plain(LSE, (B, Hq, Lq), torch.float32, "LSE"), *outs, _plain(start_q, (B,), torch.int32, "start_q"),
-        _plain(len_q, (B,), torch.int32, "len_q"), _plain(len_k, (B,), torch.int32, "len_k"), _plain(mask_q, (B, Lq), torch.uint8, "mask_q"),
-        _plain(mask_k, (B, Lk), torch.uint8, "mask_k"), B, Hq, Hk, Lq, Lk, d, W, causal, eps, code, ws, n, _stream()))
+        qp, qs, kp, ks, vp, vs, op, os, gp, gs, _plain(LSE, (B, Hq, Lq), torch.float32, dev, "LSE"), dqp, dqs, dkp, dks, dvp, dvs,
+        _plain(start_q, (B,), i32, dev, "start_q"), _plain(len_q, (B,), i32, dev, "len_q"), _plain(len_k, (B,), i32, dev, "len_k"),
+        _plain(mask_q, (B, Lq), u8, dev, "mask_q"), _plain(mask_k, (B, Lk), u8, dev, "mask_k"), B, Hq, Hk, Lq, Lk, d, W, causal, eps, code,
+        ws, n, _raw_stream(dev)))
     return dQ, dK, dV
