@@ -161,7 +161,14 @@ template <typename T, int D, int NW> struct SmActivity {
     }
     __device__ __forceinline__ unsigned long long bits() const { return __ballot(lane != 0); }
 };
-__device__ __forceinline__ void sm_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits for this wavefront's loads.  The builtin, not the instruction in text: the compiler must know that the owners' rows have
+// come as well, or it waits for them again inside the loop, and with them for the next tile's loads.
+__device__ __forceinline__ void sm_arrived()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    asm volatile("" ::: "memory");
+}
 __device__ __forceinline__ unsigned sm_lds(const void *p) { return (unsigned)(size_t)(__attribute__((address_space(3))) const unsigned char *)p; }
 // 64 floats at `p` + `at` (bytes, per lane) into LDS
 __device__ __forceinline__ void sm_load_words(unsigned lds, const float *p, unsigned at)
@@ -206,27 +213,68 @@ template <int D> __device__ __forceinline__ float sm_dot(const OwnerFrag<float, 
     return s + __shfl_xor(s, 32);
 }
 
-// s[f][t, o] = sum_k tile[t][k] own[f][o][k]: the tile's fragments are read once for all owners
+// Operands of one score tile, read from LDS: rows for the scores, columns (transposed) for the second product.  Reads are asked
+// for well before the products that take them (SM_READ_FIRST keeps the compiler from moving them there): a product that
+// waits for its own read costs a read's latency, and two or three wavefronts per SIMD do not hide that.  fp32 tiles are read where
+// they are used: their products take four times as long.
+#define SM_READ_FIRST() __builtin_amdgcn_sched_barrier(0)
+template <typename T, int D> struct SmRows {
+    bf16x8 a[D / 16];
+    __device__ __forceinline__ void read(const unsigned char *tile, int lane)
+    {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) a[k] = *reinterpret_cast<const bf16x8 *>(tile + bf16_chunk_off<D>(lane & 31, 2 * k + (lane >> 5)));
+    }
+};
+template <int D> struct SmRows<float, D> {
+    const unsigned char *tile;
+    __device__ __forceinline__ void read(const unsigned char *t, int) { tile = t; }
+};
+template <typename T, int D> struct SmCols {
+    bf16x8 a[2][D / 32];
+    __device__ __forceinline__ void read(const unsigned char *tile, int lane)
+    {
+        // transposing reads: within 16 lanes, lane i receives element (i & 3) of the 8-byte pieces addressed by lanes
+        // (i >> 2) + 4 e, e = 0..3
+        typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
+        const int row = 4 * (lane >> 5) + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        const unsigned char *sub = tile + (lane & 1) * 8;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int v = 0; v < D / 32; ++v) {
+                const bf16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4v __attribute__((address_space(3))) *)(
+                    sub + bf16_chunk_off<D>(row + 16 * m, ch + 4 * v)));
+                const bf16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4v __attribute__((address_space(3))) *)(
+                    sub + bf16_chunk_off<D>(row + 16 * m + 8, ch + 4 * v)));
+                a[m][v] = bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            }
+    }
+};
+template <int D> struct SmCols<float, D> {
+    const unsigned char *tile;
+    __device__ __forceinline__ void read(const unsigned char *t, int) { tile = t; }
+};
+
+// s[f][t, o] = sum_k tile[t][k] own[f][o][k]
 template <typename T, int D, int FR>
-__device__ __forceinline__ void sm_scores(f32x16 (&s)[FR], const unsigned char *tile, const OwnerFrag<T, D> (&own)[FR], int lane)
+__device__ __forceinline__ void sm_scores(f32x16 (&s)[FR], const SmRows<T, D> &rows, const OwnerFrag<T, D> (&own)[FR], int lane)
 {
-    using TL = SmTile<T, D>;
-    const int t = lane & 31, h = lane >> 5;
 #pragma unroll
     for (int f = 0; f < FR; ++f)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[f][e] = 0.f;
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            const bf16x8 a = *reinterpret_cast<const bf16x8 *>(tile + bf16_chunk_off<D>(t, 2 * k + h));
+        for (int k = 0; k < D / 16; ++k)
 #pragma unroll
-            for (int f = 0; f < FR; ++f) s[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, own[f].v[k], s[f], 0, 0, 0);
-        }
+            for (int f = 0; f < FR; ++f) s[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows.a[k], own[f].v[k], s[f], 0, 0, 0);
     } else {
+        using TL = SmTile<T, D>;
+        const int t = lane & 31, h = lane >> 5;
 #pragma unroll
         for (int q = 0; q < D / 8; ++q) {
-            const float4 a = *reinterpret_cast<const float4 *>(tile + t * TL::ROWB + ((h * (D / 8) + q) ^ TL::swz(t)) * 16);
+            const float4 a = *reinterpret_cast<const float4 *>(rows.tile + t * TL::ROWB + ((h * (D / 8) + q) ^ TL::swz(t)) * 16);
 #pragma unroll
             for (int f = 0; f < FR; ++f) {
                 s[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, own[f].v[4 * q + 0], s[f], 0, 0, 0);
@@ -239,43 +287,59 @@ __device__ __forceinline__ void sm_scores(f32x16 (&s)[FR], const unsigned char *
 }
 // out[f][v, o] += sum_t tile[t][v] p[f][t, o]
 template <typename T, int D, int FR>
-__device__ __forceinline__ void sm_accum(f32x16 (&out)[FR][D / 32], const unsigned char *tile, const float (&p)[FR][16], int lane)
+__device__ __forceinline__ void sm_accum(f32x16 (&out)[FR][D / 32], const SmCols<T, D> &cols, const float (&p)[FR][16], int lane)
 {
-    using TL = SmTile<T, D>;
-    const int c = lane & 31, h = lane >> 5;
     if constexpr (sizeof(T) == 2) {
-        // transposing reads: within 16 lanes, lane i receives element (i & 3) of the 8-byte pieces addressed by lanes
-        // (i >> 2) + 4 e, e = 0..3
-        typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
-        const int row = 4 * h + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        const unsigned char *sub = tile + (lane & 1) * 8;
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             bf16x8 pf[FR];
 #pragma unroll
             for (int f = 0; f < FR; ++f) pf[f] = pack8(&p[f][8 * m]);
 #pragma unroll
-            for (int v = 0; v < D / 32; ++v) {
-                bf16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4v __attribute__((address_space(3))) *)(
-                    sub + bf16_chunk_off<D>(row + 16 * m, ch + 4 * v)));
-                bf16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4v __attribute__((address_space(3))) *)(
-                    sub + bf16_chunk_off<D>(row + 16 * m + 8, ch + 4 * v)));
-                const bf16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            for (int v = 0; v < D / 32; ++v)
 #pragma unroll
-                for (int f = 0; f < FR; ++f) out[f][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[f], out[f][v], 0, 0, 0);
-            }
+                for (int f = 0; f < FR; ++f) out[f][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols.a[m][v], pf[f], out[f][v], 0, 0, 0);
         }
     } else {
+        using TL = SmTile<T, D>;
+        const int c = lane & 31, h = lane >> 5;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int t = 8 * (r >> 2) + 4 * h + (r & 3);
 #pragma unroll
             for (int v = 0; v < D / 32; ++v) {
-                const float a = *reinterpret_cast<const float *>(tile + t * TL::ROWB + ((8 * v + (c >> 2)) ^ TL::swz(t)) * 16 + (c & 3) * 4);
+                const float a = *reinterpret_cast<const float *>(cols.tile + t * TL::ROWB + ((8 * v + (c >> 2)) ^ TL::swz(t)) * 16 + (c & 3) * 4);
 #pragma unroll
                 for (int f = 0; f < FR; ++f) out[f][v] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[f][r], out[f][v], 0, 0, 0);
             }
         }
+    }
+}
+
+// The rows that a wavefront holds as accumulators (a lane has pieces of 4 features of row lane & 31), times scale, into memory:
+// across LDS (32 rows of the wavefront's own), so that a store instruction writes whole rows and not 16 bytes of each of 32.
+// row(i): where row i goes, null: nowhere.
+template <typename T, int D, typename Row>
+__device__ __forceinline__ void sm_store_rows(unsigned char *lds, const f32x16 (&x)[D / 32], float scale, bool live, int lane, Row row)
+{
+    using TL = SmTile<T, D>;
+    const int o = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int v = 0; v < D / 32; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = sizeof(T) == 2 ? 4 * v + e : 8 * v + 2 * e + h;   // 16-byte piece of features 32 v + 8 e + 4 h ...
+            T *at = reinterpret_cast<T *>(lds + o * TL::ROWB + (c ^ TL::swz(o)) * 16 + (sizeof(T) == 2 ? 8 * h : 0));
+            if (live) store4<T>(at, x[v][4 * e] * scale, x[v][4 * e + 1] * scale, x[v][4 * e + 2] * scale, x[v][4 * e + 3] * scale);
+            else store4<T>(at, 0.f, 0.f, 0.f, 0.f);
+        }
+    const int l = lane / TL::CPR, c = lane % TL::CPR;
+#pragma unroll
+    for (int k = 0; k < 32 / TL::RPI; ++k) {
+        const int i = k * TL::RPI + l;
+        const uint4 y = *reinterpret_cast<const uint4 *>(lds + i * TL::ROWB + (c ^ TL::swz(i)) * 16);
+        T *to = row(i);
+        if (to) *reinterpret_cast<uint4 *>(to + c * (16 / (int)sizeof(T))) = y;
     }
 }
 
@@ -406,8 +470,16 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
             if (j0 > w_hi || j0 + KT - 1 < w_lo) return;
             const bool whole = j0 >= all_lo && j0 + KT - 1 <= all_hi && here == ~0ull;
             f32x16 s[NS][FR];
+            SmRows<T, D> kr[NS];
+            SmCols<T, D> vc[NS];
 #pragma unroll
-            for (int n = 0; n < NS; ++n) sm_scores<T, D, FR>(s[n], lds[buf][0] + n * TL::SUB, q, lane);
+            for (int n = 0; n < NS; ++n) kr[n].read(lds[buf][0] + n * TL::SUB, lane);
+            SM_READ_FIRST();
+#pragma unroll
+            for (int n = 0; n < NS; ++n) sm_scores<T, D, FR>(s[n], kr[n], q, lane);
+#pragma unroll
+            for (int n = 0; n < NS; ++n) vc[n].read(lds[buf][1] + n * TL::SUB, lane);
+            SM_READ_FIRST();
             if (!whole) {
 #pragma unroll
                 for (int n = 0; n < NS; ++n)
@@ -457,7 +529,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                         p[f][e] = fast_exp2(fmaf(s[n][f][e], a.c2, -mu[f]));
                         sum[f] += p[f][e];
                     }
-                sm_accum<T, D, FR>(acc, lds[buf][1] + n * TL::SUB, p, lane);
+                sm_accum<T, D, FR>(acc, vc[n], p, lane);
             }
         } else {
 #pragma unroll
@@ -466,8 +538,15 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                 if (base > w_hi || base + 31 < w_lo) continue;
                 const bool whole = base >= all_lo && base + 31 <= all_hi && (unsigned)(here >> (32 * n)) == ~0u;
                 f32x16 s[FR], z[FR];
-                sm_scores<T, D, FR>(s, lds[buf][0] + n * TL::SUB, q, lane);
-                sm_scores<T, D, FR>(z, lds[buf][1] + n * TL::SUB, g, lane);
+                SmRows<T, D> kr, vr;
+                SmCols<T, D> kc;
+                kr.read(lds[buf][0] + n * TL::SUB, lane);
+                vr.read(lds[buf][1] + n * TL::SUB, lane);
+                SM_READ_FIRST();
+                sm_scores<T, D, FR>(s, kr, q, lane);
+                sm_scores<T, D, FR>(z, vr, g, lane);
+                kc.read(lds[buf][0] + n * TL::SUB, lane);
+                SM_READ_FIRST();
                 if (!whole) {
 #pragma unroll
                     for (int f = 0; f < FR; ++f) {
@@ -481,7 +560,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                 for (int f = 0; f < FR; ++f)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) p[f][e] = fast_exp2(fmaf(s[f][e], a.c2, -m[f])) * (z[f][e] - delta[f]);
-                sm_accum<T, D, FR>(acc, lds[buf][0] + n * TL::SUB, p, lane);
+                sm_accum<T, D, FR>(acc, kc, p, lane);
             }
         }
     };
@@ -491,6 +570,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
         if (t + 1 < tiles) step(std::integral_constant<int, 1>{}, t + 1);
     }
 
+    __syncthreads();   // (the tiles' LDS is used for the results)
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
         const int r = wr0 + 32 * f + (lane & 31), rc = min(r, R - 1), i = rc / a.G, hq = w.hk * a.G + (rc - i * a.G);
@@ -505,9 +585,9 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                 else a.lse[((long)w.b * a.G * a.Hk + hq) * a.Lq + i] = lse;
             }
         }
-        if (r >= R) continue;
         if (a.parts > 1) {
             float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * R + r) * D;
+            if (r >= R) continue;
 #pragma unroll
             for (int v = 0; v < D / 32; ++v)
 #pragma unroll
@@ -516,15 +596,11 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                         live[f] ? make_float4(acc[f][v][4 * e] * scale, acc[f][v][4 * e + 1] * scale, acc[f][v][4 * e + 2] * scale, acc[f][v][4 * e + 3] * scale)
                                 : make_float4(0.f, 0.f, 0.f, 0.f);
         } else {
-            T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + w.b * a.oq.b + hq * a.oq.h + i * a.oq.l;
-#pragma unroll
-            for (int v = 0; v < D / 32; ++v)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    T *at = out + 32 * v + 8 * e + 4 * h;
-                    if (live[f]) store4<T>(at, acc[f][v][4 * e] * scale, acc[f][v][4 * e + 1] * scale, acc[f][v][4 * e + 2] * scale, acc[f][v][4 * e + 3] * scale);
-                    else store4<T>(at, 0.f, 0.f, 0.f, 0.f);
-                }
+            T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + w.b * a.oq.b + (long)w.hk * a.G * a.oq.h;
+            sm_store_rows<T, D>(&lds[0][0][0] + (wv * FR + f) * TL::SUB, acc[f], scale, live[f], lane, [&](int x) -> T * {
+                const int rr = wr0 + 32 * f + x, ii = a.G == 1 ? rr : rr / a.G;
+                return rr < R ? out + (rr - ii * a.G) * a.oq.h + ii * a.oq.l : nullptr;
+            });
         }
     }
 }
@@ -624,8 +700,16 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
             if (p_last + up < w_first || p_first - a.W > w_last || 32 * n >= rows) continue;
             const bool whole = p_first + up >= w_last && p_last - a.W <= w_first;
             f32x16 s[FR], z[FR];
-            sm_scores<T, D, FR>(s, lds[buf][0] + n * TL::SUB, k, lane);
-            sm_scores<T, D, FR>(z, lds[buf][1] + n * TL::SUB, v, lane);
+            SmRows<T, D> qr, gr;
+            SmCols<T, D> qc, gc;
+            qr.read(lds[buf][0] + n * TL::SUB, lane);
+            gr.read(lds[buf][1] + n * TL::SUB, lane);
+            SM_READ_FIRST();
+            sm_scores<T, D, FR>(s, qr, k, lane);
+            sm_scores<T, D, FR>(z, gr, v, lane);
+            gc.read(lds[buf][1] + n * TL::SUB, lane);
+            qc.read(lds[buf][0] + n * TL::SUB, lane);
+            SM_READ_FIRST();
             float p[FR][16], ds[FR][16];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -654,8 +738,8 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
             for (int f = 0; f < FR; ++f)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) ds[f][e] *= p[f][e];
-            sm_accum<T, D, FR>(dv, lds[buf][1] + n * TL::SUB, p, lane);
-            sm_accum<T, D, FR>(dk, lds[buf][0] + n * TL::SUB, ds, lane);
+            sm_accum<T, D, FR>(dv, gc, p, lane);
+            sm_accum<T, D, FR>(dk, qc, ds, lane);
         }
         i0 = next;
     };
@@ -665,13 +749,14 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
         if (t + 1 < t1) step(std::integral_constant<int, NBUF - 1>{}, t + 1);
     }
 
+    __syncthreads();   // (the tiles' LDS is used for the results)
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
         const int j = w_first + 32 * f + (lane & 31);
-        if (j >= a.Lk) continue;
         bool live = j < lk;
         if (live && a.mask_k) live = a.mask_k[(long)w.b * a.Lk + j] != 0;
         if (a.parts > 1) {
+            if (j >= a.Lk) continue;
             float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * a.Lk + j) * 2 * D;
 #pragma unroll
             for (int x = 0; x < D / 32; ++x)
@@ -682,21 +767,18 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
                     *reinterpret_cast<float4 *>(o + D) = live ? make_float4(dv[f][x][4 * e], dv[f][x][4 * e + 1], dv[f][x][4 * e + 2], dv[f][x][4 * e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
         } else {
-            T *ok = reinterpret_cast<T *>(const_cast<void *>(a.ok.p)) + w.b * a.ok.b + w.hk * a.ok.h + j * a.ok.l;
-            T *ov = reinterpret_cast<T *>(const_cast<void *>(a.ov.p)) + w.b * a.ov.b + w.hk * a.ov.h + j * a.ov.l;
-#pragma unroll
-            for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int o = 32 * x + 8 * e + 4 * h;
-                    if (live) {
-                        store4<T>(ok + o, dk[f][x][4 * e] * a.cs, dk[f][x][4 * e + 1] * a.cs, dk[f][x][4 * e + 2] * a.cs, dk[f][x][4 * e + 3] * a.cs);
-                        store4<T>(ov + o, dv[f][x][4 * e], dv[f][x][4 * e + 1], dv[f][x][4 * e + 2], dv[f][x][4 * e + 3]);
-                    } else {
-                        store4<T>(ok + o, 0.f, 0.f, 0.f, 0.f);
-                        store4<T>(ov + o, 0.f, 0.f, 0.f, 0.f);
-                    }
+            T *ok = reinterpret_cast<T *>(const_cast<void *>(a.ok.p)) + w.b * a.ok.b + w.hk * a.ok.h;
+            T *ov = reinterpret_cast<T *>(const_cast<void *>(a.ov.p)) + w.b * a.ov.b + w.hk * a.ov.h;
+            // (where one buffer of tiles has not room for all wavefronts' rows: two of them after the other two)
+            constexpr bool ROOM = sizeof(lds) >= NW * FR * TL::SUB;
+            unsigned char *mine = &lds[0][0][0] + (ROOM ? wv * FR + f : wv & 1) * TL::SUB;
+            for (int turn = 0; turn < (ROOM ? 1 : 2); ++turn) {
+                if (ROOM || wv >> 1 == turn) {
+                    sm_store_rows<T, D>(mine, dk[f], a.cs, live, lane, [&](int x) -> T * { return w_first + 32 * f + x < a.Lk ? ok + (w_first + 32 * f + x) * a.ok.l : nullptr; });
+                    sm_store_rows<T, D>(mine, dv[f], 1.f, live, lane, [&](int x) -> T * { return w_first + 32 * f + x < a.Lk ? ov + (w_first + 32 * f + x) * a.ov.l : nullptr; });
                 }
+                if (!ROOM) __syncthreads();
+            }
         }
     }
 }
