@@ -18,6 +18,23 @@
 
 namespace {
 
+// Division of any 32-bit number by a number of the launch: the product with its reciprocal of 33 bits, of which m holds the lower
+// 32.  A dozen divisions stand at the start of every workgroup, where a wavefront is alone with their latency.
+struct SmDiv {
+    unsigned m;
+    int s1, s2;
+    __host__ static SmDiv by(unsigned d)
+    {
+        int l = 0;
+        while (l < 32 && (1ull << l) < d) ++l;
+        return {(unsigned)((((1ull << l) - d) << 32) / d) + 1, l < 1 ? l : 1, l > 1 ? l - 1 : 0};
+    }
+    __device__ __forceinline__ int operator()(int n) const
+    {
+        const unsigned t = __umulhi(m, (unsigned)n);
+        return (int)((t + (((unsigned)n - t) >> s1)) >> s2);
+    }
+};
 struct SmTensor {
     const void *p;
     long b, h, l;   // elements between items, heads, tokens
@@ -34,6 +51,7 @@ struct SmArgs {
     int blocks;                    // blocks of owners per problem
     int total;                     // blocks * parts * problems
     int order;                     // SmOrder
+    SmDiv by_g, by_hk, by_n, by_parts, by_blocks;   // G, Hk, problems, parts, blocks * parts
     float c2, cs;                  // log2(e) / (eps sqrt d), 1 / (eps sqrt d)
 };
 
@@ -50,18 +68,18 @@ __device__ __forceinline__ bool sm_place(const SmArgs &a, SmPlace &w)
     int n, x;
     if (a.order != SM_NEIGHBOURS) {
         if ((int)blockIdx.x >= a.total) return false;
-        x = blockIdx.x / N;
+        x = a.by_n(blockIdx.x);
         n = blockIdx.x - x * N;
         if (a.order == SM_LAST_FIRST) x = a.blocks * a.parts - 1 - x;
     } else {
         const int per = gridDim.x / 8, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
         if (at >= a.total) return false;
-        n = at / (a.blocks * a.parts);
+        n = a.by_blocks(at);
         x = at - n * a.blocks * a.parts;
     }
-    w.blk = x / a.parts;
+    w.blk = a.by_parts(x);
     w.part = x - w.blk * a.parts;
-    w.b = n / a.Hk;
+    w.b = a.by_hk(n);
     w.hk = n - w.b * a.Hk;
     return true;
 }
@@ -343,11 +361,19 @@ __device__ __forceinline__ void sm_store_rows(unsigned char *lds, const f32x16 (
     }
 }
 
-// x where bit `bit` of m is set, otherwise -inf
-__device__ __forceinline__ float sm_keep(float x, unsigned m, int bit)
+// A constant of the launch in a vector register: multiply-adds with a scalar operand issue at half the rate of those with
+// vector operands alone (4.9 against 2.7 cycles with four wavefronts per SIMD), as maxima, comparisons, selections and
+// conversions do; exponentials take 8.9.
+__device__ __forceinline__ float sm_vector(float x)
+{
+    asm("" : "+v"(x));
+    return x;
+}
+// x where bit `bit` of m is set, otherwise `other`
+__device__ __forceinline__ float sm_keep(float x, unsigned m, int bit, float other)
 {
     const int on = ((int)(m << (31 - bit))) >> 31;
-    return __int_as_float((__float_as_int(x) & on) | (~on & (int)0xff800000));
+    return __int_as_float((__float_as_int(x) & on) | (~on & __float_as_int(other)));
 }
 // bits [a, b] of 32 (none where b < a)
 __device__ __forceinline__ unsigned sm_bits(int a, int b)
@@ -382,15 +408,44 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
     const long prob = (long)w.b * a.Hk + w.hk;
     const int up = a.causal ? 0 : a.W;
 
+    const int wr0 = r0 + 32 * FR * wv;   // this wavefront's first row
+    // keys that the block's rows, and this wavefront's, can reach
+    const int i_last = a.by_g(max(0, min(min(r0 + BM, R), lq * a.G) - 1));   // (lq 0: no row, and no key below)
+    int j_lo = max(0, start + a.by_g(r0) - a.W), j_hi = min(lk - 1, start + i_last + up);
+    if (lq * a.G <= r0) j_hi = j_lo - 1;
+    const int w_first = start + a.by_g(min(wr0, R - 1)), w_last = start + a.by_g(min(wr0 + 32 * FR - 1, R - 1));
+    const int w_lo = w_first - a.W, w_hi = w_last + up;                        // any of its rows
+    const int all_lo = w_last - a.W, all_hi = min(min(w_first + up, lk - 1), j_hi);   // all of them
+    int tiles = (j_hi - j_lo + KT) / KT;
+    if (a.parts > 1) {
+        const int per = a.by_parts(max(0, tiles) + a.parts - 1);
+        j_lo += w.part * per * KT;
+        tiles = min(per, tiles - w.part * per);
+    }
+
+    const unsigned char *kb = reinterpret_cast<const unsigned char *>(reinterpret_cast<const T *>(a.k.p) + w.b * a.k.b + w.hk * a.k.h);
+    const unsigned char *vb = reinterpret_cast<const unsigned char *>(reinterpret_cast<const T *>(a.v.p) + w.b * a.v.b + w.hk * a.v.h);
+    const long ks = a.k.l * (long)sizeof(T), vs = a.v.l * (long)sizeof(T);
+    const unsigned char *mk = a.mask_k ? a.mask_k + (long)w.b * a.Lk : nullptr;
+    const SmLoader<T, D, NW> loader(lane, wv);
+    const unsigned lds_at = sm_lds(lds);
+    SmActivity<T, D, NW> act;
+    auto fetch = [&](int j0, int buf) {
+        const int rows = j_hi + 1 - j0;
+        loader.load(lds_at + buf * 2 * TL::BYTES, kb + j0 * ks, ks, rows);
+        loader.load(lds_at + (buf * 2 + 1) * TL::BYTES, vb + j0 * vs, vs, rows);
+        if (mk) act.load(loader, mk + j0, rows);
+    };
+    if (tiles > 0) fetch(j_lo, 0);   // (before the owners' rows: both are under way at a time)
+
     // this lane's rows
     OwnerFrag<T, D> q[FR], g[FR];
     bool live[FR];
     int my_lo[FR], my_hi[FR];
     float m[FR], sum[FR], delta[FR];   // BWD: m = LSE log2(e)
-    const int wr0 = r0 + 32 * FR * wv;
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
-        const int r = wr0 + 32 * f + (lane & 31), rc = min(r, R - 1), i = rc / a.G, hq = w.hk * a.G + (rc - i * a.G);
+        const int r = wr0 + 32 * f + (lane & 31), rc = min(r, R - 1), i = a.by_g(rc), hq = w.hk * a.G + (rc - i * a.G);
         live[f] = r < R && i < lq;
         if (live[f] && a.mask_q) live[f] = a.mask_q[(long)w.b * a.Lq + i] != 0;
         my_lo[f] = start + i - a.W;
@@ -415,20 +470,6 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
         }
     }
 
-    // keys that the block's rows, and this wavefront's, can reach
-    const int i_last = (min(min(r0 + BM, R), lq * a.G) - 1) / a.G;   // (lq 0: no row, and no key below)
-    int j_lo = max(0, start + r0 / a.G - a.W), j_hi = min(lk - 1, start + i_last + up);
-    if (lq * a.G <= r0) j_hi = j_lo - 1;
-    const int w_first = start + min(wr0, R - 1) / a.G, w_last = start + min(wr0 + 32 * FR - 1, R - 1) / a.G;
-    const int w_lo = w_first - a.W, w_hi = w_last + up;                        // any of its rows
-    const int all_lo = w_last - a.W, all_hi = min(min(w_first + up, lk - 1), j_hi);   // all of them
-    int tiles = (j_hi - j_lo + KT) / KT;
-    if (a.parts > 1) {
-        const int per = (tiles + a.parts - 1) / a.parts;
-        j_lo += w.part * per * KT;
-        tiles = min(per, tiles - w.part * per);
-    }
-
     f32x16 acc[FR][D / 32];
 #pragma unroll
     for (int f = 0; f < FR; ++f)
@@ -437,19 +478,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[f][v][e] = 0.f;
 
-    const unsigned char *kb = reinterpret_cast<const unsigned char *>(reinterpret_cast<const T *>(a.k.p) + w.b * a.k.b + w.hk * a.k.h);
-    const unsigned char *vb = reinterpret_cast<const unsigned char *>(reinterpret_cast<const T *>(a.v.p) + w.b * a.v.b + w.hk * a.v.h);
-    const long ks = a.k.l * (long)sizeof(T), vs = a.v.l * (long)sizeof(T);
-    const unsigned char *mk = a.mask_k ? a.mask_k + (long)w.b * a.Lk : nullptr;
-    const SmLoader<T, D, NW> loader(lane, wv);
-    const unsigned lds_at = sm_lds(lds);
-    SmActivity<T, D, NW> act;
-    auto fetch = [&](int j0, int buf) {
-        const int rows = j_hi + 1 - j0;
-        loader.load(lds_at + buf * 2 * TL::BYTES, kb + j0 * ks, ks, rows);
-        loader.load(lds_at + (buf * 2 + 1) * TL::BYTES, vb + j0 * vs, vs, rows);
-        if (mk) act.load(loader, mk + j0, rows);
-    };
+    const float c2 = sm_vector(a.c2), none = sm_vector(-INFINITY);
     auto step = [&](auto which, int t) {
         constexpr int buf = decltype(which)::value;   // (a constant: LDS addresses are offsets of the instructions)
         const int j0 = j_lo + t * KT;
@@ -488,7 +517,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                         const int base = j0 + 32 * n;
                         const unsigned keep = (sm_bits(my_lo[f] - base, min(my_hi[f], j_hi) - base) & (unsigned)(here >> (32 * n))) >> (4 * h);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) s[n][f][e] = sm_keep(s[n][f][e], keep, 8 * (e >> 2) + (e & 3));
+                        for (int e = 0; e < 16; ++e) s[n][f][e] = sm_keep(s[n][f][e], keep, 8 * (e >> 2) + (e & 3), none);
                     }
             }
             // Running maximum: sums stay relative to an older one until a score exceeds it by 2^SM_LAZY, so that the
@@ -502,7 +531,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                 for (int n = 0; n < NS; ++n)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) top[f] = fmaxf(top[f], s[n][f][e]);
-                top[f] = sm_max_halves(top[f]) * a.c2;
+                top[f] = sm_max_halves(top[f]) * c2;
                 grow = grow || top[f] > m[f] + SM_LAZY;
             }
             if (__any(grow)) {
@@ -526,7 +555,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                 for (int f = 0; f < FR; ++f)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        p[f][e] = fast_exp2(fmaf(s[n][f][e], a.c2, -mu[f]));
+                        p[f][e] = fast_exp2(fmaf(s[n][f][e], c2, -mu[f]));
                         sum[f] += p[f][e];
                     }
                 sm_accum<T, D, FR>(acc, vc[n], p, lane);
@@ -552,19 +581,18 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                     for (int f = 0; f < FR; ++f) {
                         const unsigned keep = (sm_bits(my_lo[f] - base, min(my_hi[f], j_hi) - base) & (unsigned)(here >> (32 * n))) >> (4 * h);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) s[f][e] = sm_keep(s[f][e], keep, 8 * (e >> 2) + (e & 3));
+                        for (int e = 0; e < 16; ++e) s[f][e] = sm_keep(s[f][e], keep, 8 * (e >> 2) + (e & 3), none);
                     }
                 }
                 float p[FR][16];
 #pragma unroll
                 for (int f = 0; f < FR; ++f)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) p[f][e] = fast_exp2(fmaf(s[f][e], a.c2, -m[f])) * (z[f][e] - delta[f]);
+                    for (int e = 0; e < 16; ++e) p[f][e] = fast_exp2(fmaf(s[f][e], c2, -m[f])) * (z[f][e] - delta[f]);
                 sm_accum<T, D, FR>(acc, kc, p, lane);
             }
         }
     };
-    if (tiles > 0) fetch(j_lo, 0);
     for (int t = 0; t < tiles; t += 2) {
         step(std::integral_constant<int, 0>{}, t);
         if (t + 1 < tiles) step(std::integral_constant<int, 1>{}, t + 1);
@@ -573,7 +601,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
     __syncthreads();   // (the tiles' LDS is used for the results)
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
-        const int r = wr0 + 32 * f + (lane & 31), rc = min(r, R - 1), i = rc / a.G, hq = w.hk * a.G + (rc - i * a.G);
+        const int r = wr0 + 32 * f + (lane & 31), rc = min(r, R - 1), i = a.by_g(rc), hq = w.hk * a.G + (rc - i * a.G);
         float scale = a.cs;
         if constexpr (!BWD) {
             sum[f] += __shfl_xor(sum[f], 32);
@@ -598,7 +626,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
         } else {
             T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + w.b * a.oq.b + (long)w.hk * a.G * a.oq.h;
             sm_store_rows<T, D>(&lds[0][0][0] + (wv * FR + f) * TL::SUB, acc[f], scale, live[f], lane, [&](int x) -> T * {
-                const int rr = wr0 + 32 * f + x, ii = a.G == 1 ? rr : rr / a.G;
+                const int rr = wr0 + 32 * f + x, ii = a.by_g(rr);
                 return rr < R ? out + (rr - ii * a.G) * a.oq.h + ii * a.oq.l : nullptr;
             });
         }
@@ -638,7 +666,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
     const int per_head = k_last < k0 || i_hi < i_lo ? 0 : (i_hi - i_lo + KT) / KT;
     int t0 = 0, t1 = per_head * a.G;
     if (a.parts > 1) {
-        const int per = (t1 + a.parts - 1) / a.parts;
+        const int per = a.by_parts(t1 + a.parts - 1);
         t0 = w.part * per;
         t1 = min(t1, t0 + per);
     }
@@ -674,6 +702,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
         if (++at == per_head) { at = 0; ++head; }
     };
     int i0 = i_lo + at * KT;   // first query of the tile at hand
+    const float c2 = sm_vector(a.c2);
     auto step = [&](auto which, int t) {
         constexpr int buf = decltype(which)::value;
         const int rows = i_hi + 1 - i0;
@@ -720,18 +749,18 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
                 for (int f = 0; f < FR; ++f)
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        p[f][4 * e + x] = fast_exp2(fmaf(s[f][4 * e + x], a.c2, -ls[x]));
+                        p[f][4 * e + x] = fast_exp2(fmaf(s[f][4 * e + x], c2, -ls[x]));
                         ds[f][4 * e + x] = z[f][4 * e + x] - dl[x];
                     }
             }
             if (!whole) {
 #pragma unroll
                 for (int f = 0; f < FR; ++f) {
-                    // pair (p, j): p - W <= j <= p + up, p = p_first + 8 (e >> 2) + 4 h + (e & 3)
-                    const int d = w_first + 32 * f + (lane & 31) - p_first - 4 * h + a.W;
+                    // pair (p, j): p - W <= j <= p + up; bits of the tile's rows p_first ...
+                    const int d = w_first + 32 * f + (lane & 31) - p_first;
+                    const unsigned keep = sm_bits(d - up, d + a.W) >> (4 * h);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if ((unsigned)(d - 8 * (e >> 2) - (e & 3)) > (unsigned)(a.W + up)) p[f][e] = 0.f;
+                    for (int e = 0; e < 16; ++e) p[f][e] = sm_keep(p[f][e], keep, 8 * (e >> 2) + (e & 3), 0.f);
                 }
             }
 #pragma unroll
@@ -835,13 +864,13 @@ template <typename T, int D, int WHAT> __global__ __launch_bounds__(NTHREADS) vo
         }
     }
     if (!have) return;
-    const int prob = (int)(row / R), r = (int)(row - (long)prob * R), b = prob / a.Hk, hk = prob - b * a.Hk;
+    const int prob = (int)(row / R), r = (int)(row - (long)prob * R), b = a.by_hk(prob), hk = prob - b * a.Hk;
     if constexpr (WHAT == SM_JOIN_DKV) {
         const SmTensor &t = f < D ? a.ok : a.ov;
         T *out = reinterpret_cast<T *>(const_cast<void *>(t.p)) + b * t.b + hk * t.h + r * t.l;
         store4<T>(out + (f < D ? f : f - D), x.x, x.y, x.z, x.w);
     } else {
-        const int i = r / a.G, hq = hk * a.G + (r - i * a.G);
+        const int i = a.by_g(r), hq = hk * a.G + (r - i * a.G);
         const float c = WHAT == SM_JOIN_O ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
         T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + b * a.oq.b + hq * a.oq.h + i * a.oq.l;
         store4<T>(out + f, x.x * c, x.y * c, x.z * c, x.w * c);

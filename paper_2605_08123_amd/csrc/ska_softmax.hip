@@ -93,6 +93,11 @@ int launch(int what, const SmProblem &p, const SmGrid &g, SmArgs a, hipStream_t 
     const long total = g.blocks * g.parts * p.N();
     if (total > 0x7ffffff0L) return SKA_EUNSUPPORTED;
     a.total = (int)total;
+    a.by_g = SmDiv::by(a.G);
+    a.by_hk = SmDiv::by(a.Hk);
+    a.by_n = SmDiv::by(a.B * a.Hk);
+    a.by_parts = SmDiv::by(a.parts);
+    a.by_blocks = SmDiv::by(a.blocks * a.parts);
     const long other = what == SM_DKV ? p.Lq : p.Lk;
     a.order = 2L * p.W + 1 < other / 2 ? SM_NEIGHBOURS : what == SM_DKV && p.causal ? SM_FIRST_FIRST : SM_LAST_FIRST;
     const auto f = p.dtype == SKA_F32 ? (p.d == 32 ? ska_launch_softmax_f32_32 : p.d == 64 ? ska_launch_softmax_f32_64 : ska_launch_softmax_f32_128)
