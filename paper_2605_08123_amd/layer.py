@@ -102,6 +102,11 @@ def _heads(x, shape, dtype, dev, name):
     return x.data_ptr(), ctypes.byref(Strides(b, h, l))   # (the reference keeps it alive)
 
 
+def _like(x):
+    """A contiguous tensor of x's shape and type."""
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+
+
 def _done(rc):
     if rc != SKA_OK:
         raise SinkhornAttnError(rc)
@@ -157,14 +162,14 @@ def ska_layer_norm_fwd(X, weight=None, bias=None, residual=None, eps=1e-5, Y=Non
     if w is not None:
         wp, bp = _plain(weight, (D,), w.dtype, dev, "weight"), _plain(bias, (D,), w.dtype, dev, "bias")
     if Y is None:
-        Y = X.new_empty(shape)
+        Y = _like(X)
     yp, ldy = _rows(Y, shape, dt, dev, "Y")
     rp = sp = None
     ldr = lds = 0
     if residual is not None:
         rp, ldr = _rows(residual, shape, dt, dev, "residual")
         if S is None:
-            S = X.new_empty(shape)
+            S = _like(X)
         sp, lds = _rows(S, shape, dt, dev, "S")
     elif S is not None:
         raise ValueError("S is the sum with a residual: there is none")
@@ -194,12 +199,12 @@ def ska_layer_norm_bwd(dY, S, weight, stats, dS=None, want_weight=True, want_bia
     wp = _plain(weight, (D,), wt, dev, "weight")
     rp, ldr = _rows(dS, shape, dt, dev, "dS") if dS is not None else (None, 0)
     if dX is None:
-        dX = S.new_empty(shape)
+        dX = _like(S)
     xp, ldx = _rows(dX, shape, dt, dev, "dX")
     if want_weight and dweight is None:
-        dweight = S.new_empty(D, dtype=wt)
+        dweight = S.new_empty(D, dtype=wt) if weight is None else torch.empty_like(weight)
     if want_bias and dbias is None:
-        dbias = S.new_empty(D, dtype=wt)
+        dbias = S.new_empty(D, dtype=wt) if weight is None else torch.empty_like(weight)
     dwp, dbp = _plain(dweight, (D,), wt, dev, "dweight"), _plain(dbias, (D,), wt, dev, "dbias")
     lib = _lib()
     ws, n, keep = _workspace(workspace, lib.ska_layer_norm_workspace_bytes(N, D) if dwp or dbp else 0, S, dev)
@@ -228,7 +233,7 @@ def _rope(call, Q, K, freq, amplitude, interleaved, start, positions, Qo, Ko, na
     B, Hq, L, d = shape
     qp, qs = _heads(Q, shape, dt, dev, names[0])
     if Qo is None:
-        Qo = Q.new_empty(shape)
+        Qo = _like(Q)
     op, os = _heads(Qo, shape, dt, dev, names[2])
     kp = kop = ks = kos = None
     Hk = 0
@@ -237,7 +242,7 @@ def _rope(call, Q, K, freq, amplitude, interleaved, start, positions, Qo, Ko, na
         kshape = (B, Hk, L, d)
         kp, ks = _heads(K, kshape, dt, dev, names[1])
         if Ko is None:
-            Ko = Q.new_empty(kshape)
+            Ko = _like(K)
         kop, kos = _heads(Ko, kshape, dt, dev, names[3])
     elif Ko is not None:
         raise ValueError(f"{names[3]} without {names[1]}")
@@ -285,7 +290,7 @@ def ska_softmax_attn_fwd(Q, K, V, W, causal=False, eps=1.0, len_q=None, len_k=No
     kp, ks = _heads(K, kshape, dt, dev, "K")
     vp, vs = _heads(V, kshape, dt, dev, "V")
     if O is None:
-        O = Q.new_empty(qshape)
+        O = _like(Q)
     op, os = _heads(O, qshape, dt, dev, "O")
     if LSE is None:
         LSE = Q.new_empty((B, Hq, Lq), dtype=torch.float32)
@@ -310,11 +315,11 @@ def ska_softmax_attn_bwd(Q, K, V, O, dO, LSE, W, causal=False, eps=1.0, len_q=No
     op, os = _heads(O, qshape, dt, dev, "O")
     gp, gs = _heads(dO, qshape, dt, dev, "dO")
     if dQ is None:
-        dQ = Q.new_empty(qshape)
+        dQ = _like(Q)
     if dK is None:
-        dK = K.new_empty(kshape)
+        dK = _like(K)
     if dV is None:
-        dV = K.new_empty(kshape)
+        dV = _like(V)
     dqp, dqs = _heads(dQ, qshape, dt, dev, "dQ")
     dkp, dks = _heads(dK, kshape, dt, dev, "dK")
     dvp, dvs = _heads(dV, kshape, dt, dev, "dV")
