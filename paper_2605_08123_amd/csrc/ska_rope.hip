@@ -56,6 +56,27 @@ template <typename T, int FORM, bool INTER> __global__ __launch_bounds__(NT) voi
     else if (FORM == ROPE_ADJACENT) f0 = f1 = slot * V;
     else if (INTER) { f0 = 2 * slot; f1 = f0 + 1; }
     else { f0 = slot * V; f1 = f0 + a.rot / 2; }
+    // heads BATCH at a time: their pieces are all asked for before the first is stored (an output may be its input, so the
+    // compiler cannot do that by itself), those of the first ones before the angles are found
+    constexpr int BATCH = 4;
+    constexpr bool TWO = FORM != ROPE_ADJACENT;   // a turned slot has a second piece
+    const int h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, a.q.H + a.k.H);
+    vec u[BATCH], v[BATCH];
+    T *out[BATCH];
+    auto ask = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (h + i >= h1) break;
+            const bool isq = h + i < a.q.H;
+            const RopeTensor &x = isq ? a.q : a.k;
+            const int hh = isq ? h + i : h + i - a.q.H;
+            const T *in = reinterpret_cast<const T *>(x.in) + b * x.ib + hh * x.ih + l * x.il;
+            out[i] = reinterpret_cast<T *>(x.out) + b * x.ob + hh * x.oh + l * x.ol;
+            u[i] = *reinterpret_cast<const vec *>(in + f0);
+            if (TWO && turned) v[i] = *reinterpret_cast<const vec *>(in + f1);
+        }
+    };
+    ask(h0);
     float c[PAIRS], s[PAIRS];
     if (turned) {
         const int p = a.pos ? a.pos[(long)b * a.L + l] : (a.start ? a.start[b] : 0) + l;
@@ -68,35 +89,28 @@ template <typename T, int FORM, bool INTER> __global__ __launch_bounds__(NT) voi
             s[i] *= a.back ? -a.amplitude : a.amplitude;
         }
     }
-    const int h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, a.q.H + a.k.H);
-#pragma unroll 2
-    for (int h = h0; h < h1; ++h) {
-        const bool isq = h < a.q.H;
-        const RopeTensor &x = isq ? a.q : a.k;
-        const int hh = isq ? h : h - a.q.H;
-        const T *in = reinterpret_cast<const T *>(x.in) + b * x.ib + hh * x.ih + l * x.il;
-        T *out = reinterpret_cast<T *>(x.out) + b * x.ob + hh * x.oh + l * x.ol;
-        vec u = *reinterpret_cast<const vec *>(in + f0);
-        if (!turned) {
-            *reinterpret_cast<vec *>(out + f0) = u;
-        } else if constexpr (FORM == ROPE_ADJACENT) {
+    for (int h = h0; h < h1; h += BATCH) {
+        if (h > h0) ask(h);
 #pragma unroll
-            for (int i = 0; i < PAIRS; ++i) {
-                const float x1 = (float)u[2 * i], x2 = (float)u[2 * i + 1];
-                u[2 * i] = (T)fmaf(x1, c[i], -(x2 * s[i]));   // (which product is rounded is said: every form gives the same bits)
-                u[2 * i + 1] = (T)fmaf(x2, c[i], x1 * s[i]);
-            }
-            *reinterpret_cast<vec *>(out + f0) = u;
-        } else {
-            vec v = *reinterpret_cast<const vec *>(in + f1);
+        for (int j = 0; j < BATCH; ++j) {
+            if (h + j >= h1) break;
+            if (turned) {
+                // (which product is rounded is said: every form gives the same bits)
 #pragma unroll
-            for (int i = 0; i < PAIRS; ++i) {
-                const float x1 = (float)u[i], x2 = (float)v[i];
-                u[i] = (T)fmaf(x1, c[i], -(x2 * s[i]));
-                v[i] = (T)fmaf(x2, c[i], x1 * s[i]);
+                for (int i = 0; i < PAIRS; ++i) {
+                    const float x1 = (float)(TWO ? u[j][i] : u[j][2 * i]), x2 = (float)(TWO ? v[j][i] : u[j][2 * i + 1]);
+                    const T y1 = (T)fmaf(x1, c[i], -(x2 * s[i])), y2 = (T)fmaf(x2, c[i], x1 * s[i]);
+                    if constexpr (TWO) {
+                        u[j][i] = y1;
+                        v[j][i] = y2;
+                    } else {
+                        u[j][2 * i] = y1;
+                        u[j][2 * i + 1] = y2;
+                    }
+                }
             }
-            *reinterpret_cast<vec *>(out + f0) = u;
-            *reinterpret_cast<vec *>(out + f1) = v;
+            *reinterpret_cast<vec *>(out[j] + f0) = u[j];
+            if (TWO && turned) *reinterpret_cast<vec *>(out[j] + f1) = v[j];
         }
     }
 }
