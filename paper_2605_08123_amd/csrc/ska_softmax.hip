@@ -27,47 +27,43 @@ int check(const SmProblem &p)
 
 // How one kernel of a call is launched: wavefronts per workgroup, blocks of owners, parts of a walk
 struct SmGrid { int nw; long blocks; int parts; };
-// owners: rows of the side that is kept; walk: rows of the other side that a block may meet, at most
-SmGrid sm_grid(const SmProblem &p, int what, long owners, long walk)
+// Rows of the walked side that a block of `rows` owners can meet, at most (dK, dV: of all heads of the group)
+long sm_walk(const SmProblem &p, int what, int rows)
+{
+    const bool keys = what == SM_DKV;
+    const long other = keys ? p.Lq : p.Lk, W = std::min<long>(p.W, other), own = keys ? std::min(rows, p.Lk) : std::min(rows / p.G() + 1, p.Lq);
+    return std::min(other, own + W + (p.causal ? 0 : W)) * (keys ? p.G() : 1);
+}
+SmGrid sm_grid(const SmProblem &p, int what)
 {
     SmGrid g{4, 0, 1};
+    const long owners = what == SM_DKV ? p.Lk : p.R();
     const int bytes = p.dtype == SKA_F32 ? 4 : 2;
     // One wavefront per workgroup where there are no more rows, or where workgroups of four would leave CUs without any and share
     // little (a band: two problems of 4 heads, L = 701, W = 64, fp32, forward and backward 12.6 and 30.6 us with four, 10.9 and
     // 25.4 with one; all of 8 heads, L = 2000, d = 128, fp32: 176 and 549 with four, 718 and 1290 with one)
-    if (owners <= 32 || ((owners + 127) / 128 * p.N() < 256 && walk <= 512)) g.nw = 1;
+    if (owners <= 32 || ((owners + 127) / 128 * p.N() < 256 && sm_walk(p, what, 128) <= 512)) g.nw = 1;
     const int rows = 32 * g.nw * sm_fr(what, bytes, p.d, g.nw);
     g.blocks = (owners + rows - 1) / rows;
     // Parts where there are fewer wavefronts than SIMDs: one per SIMD in all (forward: two problems of 8 heads, L = 1000, causal
     // 19 us, with two 25) or two (backward, whose walks are longer: 16 heads on 4, L = 4096, d = 128, causal 311 us, with one 430),
-    // but no fewer than four tiles each, since parts have to be joined by another launch.
-    const long tile = bytes == 2 && p.d < 128 ? 64 : 32, tiles = (walk + tile - 1) / tile, waves = g.blocks * p.N() * g.nw;
-    if (waves < 1024) g.parts = (int)std::max(1L, std::min({(what == SM_FWD ? 1024 : 2048) / waves, tiles / 4, 256L}));
+    // but no fewer than two tiles each, since parts have to be joined by another launch (4 heads, L = 512, d = 64, causal, backward:
+    // one tile 22.4 us, two 21.0, four 22.7).
+    const long tile = bytes == 2 && p.d < 128 ? 64 : 32, tiles = (sm_walk(p, what, rows) + tile - 1) / tile, waves = g.blocks * p.N() * g.nw;
+    if (waves < 1024) g.parts = (int)std::max(1L, std::min({(what == SM_FWD ? 1024 : 2048) / waves, tiles / 2, 256L}));
     return g;
 }
-long walk_of_rows(const SmProblem &p)
-{
-    const long W = std::min<long>(p.W, p.Lk);
-    return std::min<long>(p.Lk, std::min(p.Lq, 256) + W + (p.causal ? 0 : W));
-}
-long walk_of_keys(const SmProblem &p)
-{
-    const long W = std::min<long>(p.W, p.Lq);
-    return std::min<long>(p.Lq, std::min(p.Lk, 256) + W + (p.causal ? 0 : W)) * p.G();
-}
-SmGrid rows_grid(const SmProblem &p, int what) { return sm_grid(p, what, p.R(), walk_of_rows(p)); }
-SmGrid keys_grid(const SmProblem &p) { return sm_grid(p, SM_DKV, p.Lk, walk_of_keys(p)); }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 size_t delta_bytes(const SmProblem &p) { return up256((size_t)p.N() * p.R() * sizeof(float)); }
 size_t part_lse_bytes(const SmProblem &p, const SmGrid &g) { return g.parts > 1 ? up256((size_t)g.parts * p.N() * p.R() * sizeof(float)) : 0; }
 size_t ws_fwd(const SmProblem &p)
 {
-    const SmGrid g = rows_grid(p, SM_FWD);
+    const SmGrid g = sm_grid(p, SM_FWD);
     return g.parts > 1 ? part_lse_bytes(p, g) + (size_t)g.parts * p.N() * p.R() * p.d * sizeof(float) : 0;
 }
 size_t ws_bwd(const SmProblem &p)
 {
-    const SmGrid r = rows_grid(p, SM_DQ), k = keys_grid(p);
+    const SmGrid r = sm_grid(p, SM_DQ), k = sm_grid(p, SM_DKV);
     const size_t pr = r.parts > 1 ? (size_t)r.parts * p.N() * p.R() * p.d : 0, pk = k.parts > 1 ? (size_t)k.parts * p.N() * p.Lk * 2 * p.d : 0;
     return 2 * delta_bytes(p) + std::max(pr, pk) * sizeof(float);   // (one after the other)
 }
@@ -155,7 +151,7 @@ int ska_softmax_attn_fwd(const void *Q, const ska_strides *q_strides, const void
     const size_t need = ws_fwd(p);
     if (need && (!workspace || workspace_bytes < need)) return SKA_EWORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 15) return SKA_EINVAL;
-    const SmGrid g = rows_grid(p, SM_FWD);
+    const SmGrid g = sm_grid(p, SM_FWD);
     a.part_lse = static_cast<float *>(workspace);
     a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + part_lse_bytes(p, g));
     return launch(SM_FWD, p, g, a, static_cast<hipStream_t>(stream));
@@ -187,8 +183,8 @@ int ska_softmax_attn_bwd(const void *Q, const ska_strides *q_strides, const void
     a.delta = a.lse2 + delta_bytes(p) / sizeof(float);
     a.part = a.delta + delta_bytes(p) / sizeof(float);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    rc = launch(SM_DQ, p, rows_grid(p, SM_DQ), a, st);   // (writes delta, which dK reads)
-    return rc != SKA_OK ? rc : launch(SM_DKV, p, keys_grid(p), a, st);
+    rc = launch(SM_DQ, p, sm_grid(p, SM_DQ), a, st);   // (writes delta, which dK reads)
+    return rc != SKA_OK ? rc : launch(SM_DKV, p, sm_grid(p, SM_DKV), a, st);
 }
 
 }  // extern "C"
