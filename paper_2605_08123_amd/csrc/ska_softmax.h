@@ -11,6 +11,13 @@
 // of the second product (whose sum runs over the walked side in any order).  dQ apart from dK and dV means two score
 // evaluations (seven products, not five), but no atomics, so that results repeat, and no pass over dQ in fp32.
 //
+// What bounds them (MI355X, 2 heads, L = 262144, d = 64, W = 256, bf16; products of the band's pairs alone): forward 117 us,
+// 589 TFLOP/s; dQ 157 us, 658; dK and dV 205 us, 672.  The forward's HBM traffic is the least possible (200 MB read and 68 written
+// by the L2's counters, 2.3 TB/s).  The matrix cores are busy for 29 to 32 % of the cycles: a lone wavefront issues a vector
+// instruction every 8 cycles at most, and three wavefronts fit a SIMD's registers (dK, dV: two).  In the forward each lives 20 us,
+// of which 3.5 pass until its first tile is there, 12 in the arithmetic of nine tiles, 2.7 waiting for tiles and barriers, 1.9
+// storing.
+//
 // Query heads that share a key head are rows of the same problem: row r of problem (b, key head) is query r / G of head
 // r % G of the group, G = Hq / Hk.  Keys are read once for the group, and dK, dV sum over it by themselves.
 #pragma once
@@ -274,63 +281,49 @@ template <int D> struct SmCols<float, D> {
     __device__ __forceinline__ void read(const unsigned char *t, int) { tile = t; }
 };
 
-// s[f][t, o] = sum_k tile[t][k] own[f][o][k]
-template <typename T, int D, int FR>
-__device__ __forceinline__ void sm_scores(f32x16 (&s)[FR], const SmRows<T, D> &rows, const OwnerFrag<T, D> (&own)[FR], int lane)
+// s[t, o] = sum_k tile[t][k] own[o][k]
+template <typename T, int D>
+__device__ __forceinline__ void sm_scores(f32x16 &s, const SmRows<T, D> &rows, const OwnerFrag<T, D> &own, int lane)
 {
 #pragma unroll
-    for (int f = 0; f < FR; ++f)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[f][e] = 0.f;
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-            for (int f = 0; f < FR; ++f) s[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows.a[k], own[f].v[k], s[f], 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows.a[k], own.v[k], s, 0, 0, 0);
     } else {
         using TL = SmTile<T, D>;
         const int t = lane & 31, h = lane >> 5;
 #pragma unroll
         for (int q = 0; q < D / 8; ++q) {
             const float4 a = *reinterpret_cast<const float4 *>(rows.tile + t * TL::ROWB + ((h * (D / 8) + q) ^ TL::swz(t)) * 16);
-#pragma unroll
-            for (int f = 0; f < FR; ++f) {
-                s[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, own[f].v[4 * q + 0], s[f], 0, 0, 0);
-                s[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, own[f].v[4 * q + 1], s[f], 0, 0, 0);
-                s[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, own[f].v[4 * q + 2], s[f], 0, 0, 0);
-                s[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, own[f].v[4 * q + 3], s[f], 0, 0, 0);
-            }
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, own.v[4 * q + 0], s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, own.v[4 * q + 1], s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, own.v[4 * q + 2], s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, own.v[4 * q + 3], s, 0, 0, 0);
         }
     }
 }
-// out[f][v, o] += sum_t tile[t][v] p[f][t, o].  bf16: p is rounded to bf16 (half a step, 2^-8), or with EXACT taken as the sum of
+// out[v, o] += sum_t tile[t][v] p[t, o].  bf16: p is rounded to bf16 (half a step, 2^-8), or with EXACT taken as the sum of
 // what that gives and of the rest rounded likewise (2^-16).
-template <typename T, int D, int FR, bool EXACT = false>
-__device__ __forceinline__ void sm_accum(f32x16 (&out)[FR][D / 32], const SmCols<T, D> &cols, const float (&p)[FR][16], int lane)
+template <typename T, int D, bool EXACT = false>
+__device__ __forceinline__ void sm_accum(f32x16 (&out)[D / 32], const SmCols<T, D> &cols, const float (&p)[16], int lane)
 {
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            bf16x8 pf[FR];
-#pragma unroll
-            for (int f = 0; f < FR; ++f) pf[f] = pack8(&p[f][8 * m]);
+            const bf16x8 pf = pack8(&p[8 * m]);
 #pragma unroll
             for (int v = 0; v < D / 32; ++v)
-#pragma unroll
-                for (int f = 0; f < FR; ++f) out[f][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols.a[m][v], pf[f], out[f][v], 0, 0, 0);
+                out[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols.a[m][v], pf, out[v], 0, 0, 0);
             if constexpr (EXACT) {
-                bf16x8 rest[FR];
+                float x[8];
 #pragma unroll
-                for (int f = 0; f < FR; ++f) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = p[f][8 * m + e] - (float)pf[f][e];
-                    rest[f] = pack8(x);
-                }
+                for (int e = 0; e < 8; ++e) x[e] = p[8 * m + e] - (float)pf[e];
+                const bf16x8 rest = pack8(x);
 #pragma unroll
                 for (int v = 0; v < D / 32; ++v)
-#pragma unroll
-                    for (int f = 0; f < FR; ++f) out[f][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols.a[m][v], rest[f], out[f][v], 0, 0, 0);
+                    out[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols.a[m][v], rest, out[v], 0, 0, 0);
             }
         }
     } else {
@@ -342,8 +335,7 @@ __device__ __forceinline__ void sm_accum(f32x16 (&out)[FR][D / 32], const SmCols
 #pragma unroll
             for (int v = 0; v < D / 32; ++v) {
                 const float a = *reinterpret_cast<const float *>(cols.tile + t * TL::ROWB + ((8 * v + (c >> 2)) ^ TL::swz(t)) * 16 + (c & 3) * 4);
-#pragma unroll
-                for (int f = 0; f < FR; ++f) out[f][v] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[f][r], out[f][v], 0, 0, 0);
+                out[v] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[r], out[v], 0, 0, 0);
             }
         }
     }
@@ -401,18 +393,14 @@ __device__ __forceinline__ unsigned sm_bits(int a, int b)
 constexpr float SM_LAZY = 8.f;   // powers of two that a row's maximum may grow by before its sums are scaled to it
 
 enum { SM_FWD, SM_DQ, SM_DKV };
-// Fragments of 32 owners that a wavefront of a kernel holds (nw: wavefronts of the workgroup), and wavefronts per SIMD that its
-// registers are to allow
-constexpr int sm_fr(int what, int bytes, int d, int nw) { return 1; }
-constexpr int sm_waves(int what, int bytes, int d, int fr) { return 1; }
 
 // ------------------------------------------------------------------ queries as owners: forward, dQ
-// BWD: dQ instead of O.  NW wavefronts, 32 FR rows each.
-template <typename T, int D, int NW, int FR, bool BWD>
-__global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeof(T), D, FR))) void sm_rows_kernel(const SmArgs a)
+// BWD: dQ instead of O.  NW wavefronts, 32 rows each.
+template <typename T, int D, int NW, bool BWD>
+__global__ __launch_bounds__(64 * NW, 1) void sm_rows_kernel(const SmArgs a)
 {
     using TL = SmTile<T, D>;
-    constexpr int KT = TL::KT, NS = KT / 32, BM = 32 * NW * FR;
+    constexpr int KT = TL::KT, NS = KT / 32, BM = 32 * NW;
     __shared__ __align__(1024) unsigned char lds[2][2][TL::BYTES];
 
     SmPlace w;
@@ -423,12 +411,12 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
     const long prob = (long)w.b * a.Hk + w.hk;
     const int up = a.causal ? 0 : a.W;
 
-    const int wr0 = r0 + 32 * FR * wv;   // this wavefront's first row
+    const int wr0 = r0 + 32 * wv;   // this wavefront's first row
     // keys that the block's rows, and this wavefront's, can reach
     const int i_last = a.by_g(max(0, min(min(r0 + BM, R), lq * a.G) - 1));   // (lq 0: no row, and no key below)
     int j_lo = max(0, start + a.by_g(r0) - a.W), j_hi = min(lk - 1, start + i_last + up);
     if (lq * a.G <= r0) j_hi = j_lo - 1;
-    const int w_first = start + a.by_g(min(wr0, R - 1)), w_last = start + a.by_g(min(wr0 + 32 * FR - 1, R - 1));
+    const int w_first = start + a.by_g(min(wr0, R - 1)), w_last = start + a.by_g(min(wr0 + 31, R - 1));
     const int w_lo = w_first - a.W, w_hi = w_last + up;                        // any of its rows
     const int all_lo = w_last - a.W, all_hi = min(min(w_first + up, lk - 1), j_hi);   // all of them
     int tiles = (j_hi - j_lo + KT) / KT;
@@ -445,7 +433,9 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
     const SmLoader<T, D, NW> loader(lane, wv);
     const unsigned lds_at = sm_lds(lds);
     SmActivity<T, D, NW> act;
-    auto fetch = [&](int j0, int buf) {
+    // (inlined by order: where the compiler called fetch or step, fp32 at d = 128 kept its registers in memory, 661 us instead of 185 for a
+    // token of 4 sequences, 8 heads on 2, caches of 65536)
+    auto fetch = [&](int j0, int buf) __attribute__((always_inline)) {
         const int rows = j_hi + 1 - j0;
         loader.load(lds_at + buf * 2 * TL::BYTES, kb + j0 * ks, ks, rows);
         loader.load(lds_at + (buf * 2 + 1) * TL::BYTES, vb + j0 * vs, vs, rows);
@@ -454,47 +444,37 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
     if (tiles > 0) fetch(j_lo, 0);   // (before the owners' rows: both are under way at a time)
 
     // this lane's rows
-    OwnerFrag<T, D> q[FR], g[FR];
-    bool live[FR];
-    int my_lo[FR], my_hi[FR];
-    float m[FR], sum[FR], delta[FR];   // BWD: m = LSE log2(e)
-#pragma unroll
-    for (int f = 0; f < FR; ++f) {
-        const int r = wr0 + 32 * f + (lane & 31), rc = min(r, R - 1), i = a.by_g(rc), hq = w.hk * a.G + (rc - i * a.G);
-        live[f] = r < R && i < lq;
-        if (live[f] && a.mask_q) live[f] = a.mask_q[(long)w.b * a.Lq + i] != 0;
-        my_lo[f] = start + i - a.W;
-        my_hi[f] = min(start + i + up, lk - 1);
-        sm_frag<T, D>(q[f], reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + hq * a.q.h + i * a.q.l, h);
-        m[f] = -INFINITY;
-        sum[f] = delta[f] = 0.f;
-        if constexpr (BWD) {
-            OwnerFrag<T, D> o;
-            sm_frag<T, D>(g[f], reinterpret_cast<const T *>(a.g.p) + w.b * a.g.b + hq * a.g.h + i * a.g.l, h);
-            sm_frag<T, D>(o, reinterpret_cast<const T *>(a.o.p) + w.b * a.o.b + hq * a.o.h + i * a.o.l, h);
-            const long at = ((long)w.b * a.G * a.Hk + hq) * a.Lq + i;
-            const float lse = a.lse[at];
-            live[f] = live[f] && lse > -INFINITY;
-            m[f] = live[f] ? lse * LOG2E : INFINITY;      // (exp2(s - inf) = 0)
-            delta[f] = sm_dot<D>(g[f], o);
-            if (!live[f]) delta[f] = 0.f;
-            if (w.part == 0 && h == 0 && r < R) {
-                a.lse2[at] = m[f];
-                a.delta[at] = delta[f];
-            }
+    OwnerFrag<T, D> q, g;
+    const int r = wr0 + (lane & 31), rc = min(r, R - 1), i = a.by_g(rc), hq = w.hk * a.G + (rc - i * a.G);
+    bool live = r < R && i < lq;
+    if (live && a.mask_q) live = a.mask_q[(long)w.b * a.Lq + i] != 0;
+    const int my_lo = start + i - a.W, my_hi = min(start + i + up, lk - 1);
+    sm_frag<T, D>(q, reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + hq * a.q.h + i * a.q.l, h);
+    float m = -INFINITY, sum = 0.f, delta = 0.f;   // BWD: m = LSE log2(e)
+    if constexpr (BWD) {
+        OwnerFrag<T, D> o;
+        sm_frag<T, D>(g, reinterpret_cast<const T *>(a.g.p) + w.b * a.g.b + hq * a.g.h + i * a.g.l, h);
+        sm_frag<T, D>(o, reinterpret_cast<const T *>(a.o.p) + w.b * a.o.b + hq * a.o.h + i * a.o.l, h);
+        const long at = ((long)w.b * a.G * a.Hk + hq) * a.Lq + i;
+        const float lse = a.lse[at];
+        live = live && lse > -INFINITY;
+        m = live ? lse * LOG2E : INFINITY;      // (exp2(s - inf) = 0)
+        delta = sm_dot<D>(g, o);
+        if (!live) delta = 0.f;
+        if (w.part == 0 && h == 0 && r < R) {
+            a.lse2[at] = m;
+            a.delta[at] = delta;
         }
     }
 
-    f32x16 acc[FR][D / 32];
+    f32x16 acc[D / 32];
 #pragma unroll
-    for (int f = 0; f < FR; ++f)
+    for (int v = 0; v < D / 32; ++v)
 #pragma unroll
-        for (int v = 0; v < D / 32; ++v)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[f][v][e] = 0.f;
+        for (int e = 0; e < 16; ++e) acc[v][e] = 0.f;
 
     const float c2 = sm_vector(a.c2), none = sm_vector(-INFINITY);
-    auto step = [&](auto which, int t) {
+    auto step = [&](auto which, int t) __attribute__((always_inline)) {
         constexpr int buf = decltype(which)::value;   // (a constant: LDS addresses are offsets of the instructions)
         const int j0 = j_lo + t * KT;
         sm_arrived();
@@ -513,69 +493,55 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
         if constexpr (!BWD) {
             if (j0 > w_hi || j0 + KT - 1 < w_lo) return;
             const bool whole = j0 >= all_lo && j0 + KT - 1 <= all_hi && here == ~0ull;
-            f32x16 s[NS][FR];
+            f32x16 s[NS];
             SmRows<T, D> kr[NS];
             SmCols<T, D> vc[NS];
 #pragma unroll
             for (int n = 0; n < NS; ++n) kr[n].read(lds[buf][0] + n * TL::SUB, lane);
             SM_READ_FIRST();
 #pragma unroll
-            for (int n = 0; n < NS; ++n) sm_scores<T, D, FR>(s[n], kr[n], q, lane);
+            for (int n = 0; n < NS; ++n) sm_scores<T, D>(s[n], kr[n], q, lane);
 #pragma unroll
             for (int n = 0; n < NS; ++n) vc[n].read(lds[buf][1] + n * TL::SUB, lane);
             SM_READ_FIRST();
             if (!whole) {
 #pragma unroll
-                for (int n = 0; n < NS; ++n)
+                for (int n = 0; n < NS; ++n) {
+                    const int base = j0 + 32 * n;
+                    const unsigned keep = (sm_bits(my_lo - base, min(my_hi, j_hi) - base) & (unsigned)(here >> (32 * n))) >> (4 * h);
 #pragma unroll
-                    for (int f = 0; f < FR; ++f) {
-                        const int base = j0 + 32 * n;
-                        const unsigned keep = (sm_bits(my_lo[f] - base, min(my_hi[f], j_hi) - base) & (unsigned)(here >> (32 * n))) >> (4 * h);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) s[n][f][e] = sm_keep(s[n][f][e], keep, 8 * (e >> 2) + (e & 3), none);
-                    }
+                    for (int e = 0; e < 16; ++e) s[n][e] = sm_keep(s[n][e], keep, 8 * (e >> 2) + (e & 3), none);
+                }
             }
             // Running maximum: sums stay relative to an older one until a score exceeds it by 2^SM_LAZY, so that the
             // accumulators are scaled a few times per row and not once per tile; P up to 2^8 loses nothing in either type.
-            float top[FR], mu[FR];
-            bool grow = false;
+            float top = s[0][0];
 #pragma unroll
-            for (int f = 0; f < FR; ++f) {
-                top[f] = s[0][f][0];
+            for (int n = 0; n < NS; ++n)
 #pragma unroll
-                for (int n = 0; n < NS; ++n)
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[n][e]);
+            top = sm_max_halves(top) * c2;
+            if (__any(top > m + SM_LAZY)) {
+                const float mn = fmaxf(m, top), x = mn > -INFINITY ? fast_exp2(m - mn) : 1.f;
+                sum *= x;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) top[f] = fmaxf(top[f], s[n][f][e]);
-                top[f] = sm_max_halves(top[f]) * c2;
-                grow = grow || top[f] > m[f] + SM_LAZY;
+                for (int v = 0; v < D / 32; ++v)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[v][e] *= x;
+                m = mn;
             }
-            if (__any(grow)) {
-#pragma unroll
-                for (int f = 0; f < FR; ++f) {
-                    const float mn = fmaxf(m[f], top[f]), x = mn > -INFINITY ? fast_exp2(m[f] - mn) : 1.f;
-                    sum[f] *= x;
-#pragma unroll
-                    for (int v = 0; v < D / 32; ++v)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) acc[f][v][e] *= x;
-                    m[f] = mn;
-                }
-            }
-#pragma unroll
-            for (int f = 0; f < FR; ++f) mu[f] = m[f] > -INFINITY ? m[f] : 0.f;
+            const float mu = m > -INFINITY ? m : 0.f;
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
-                float p[FR][16];
+                float p[16];
 #pragma unroll
-                for (int f = 0; f < FR; ++f)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        p[f][e] = fast_exp2(fmaf(s[n][f][e], c2, -mu[f]));
-                        sum[f] += p[f][e];
-                    }
+                for (int e = 0; e < 16; ++e) {
+                    p[e] = fast_exp2(fmaf(s[n][e], c2, -mu));
+                    sum += p[e];
+                }
                 // (few rows wait for the cache and not for products, so that their P need not be rounded: four sequences of one
                 // token on caches of 65536, d = 64, 26.0 us against 25.6, and O as near as its type allows)
-                sm_accum<T, D, FR, NW == 1>(acc, vc[n], p, lane);
+                sm_accum<T, D, NW == 1>(acc, vc[n], p, lane);
             }
         } else {
 #pragma unroll
@@ -583,30 +549,25 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
                 const int base = j0 + 32 * n;
                 if (base > w_hi || base + 31 < w_lo) continue;
                 const bool whole = base >= all_lo && base + 31 <= all_hi && (unsigned)(here >> (32 * n)) == ~0u;
-                f32x16 s[FR], z[FR];
+                f32x16 s, z;
                 SmRows<T, D> kr, vr;
                 SmCols<T, D> kc;
                 kr.read(lds[buf][0] + n * TL::SUB, lane);
                 vr.read(lds[buf][1] + n * TL::SUB, lane);
                 SM_READ_FIRST();
-                sm_scores<T, D, FR>(s, kr, q, lane);
-                sm_scores<T, D, FR>(z, vr, g, lane);
+                sm_scores<T, D>(s, kr, q, lane);
+                sm_scores<T, D>(z, vr, g, lane);
                 kc.read(lds[buf][0] + n * TL::SUB, lane);
                 SM_READ_FIRST();
                 if (!whole) {
+                    const unsigned keep = (sm_bits(my_lo - base, min(my_hi, j_hi) - base) & (unsigned)(here >> (32 * n))) >> (4 * h);
 #pragma unroll
-                    for (int f = 0; f < FR; ++f) {
-                        const unsigned keep = (sm_bits(my_lo[f] - base, min(my_hi[f], j_hi) - base) & (unsigned)(here >> (32 * n))) >> (4 * h);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) s[f][e] = sm_keep(s[f][e], keep, 8 * (e >> 2) + (e & 3), none);
-                    }
+                    for (int e = 0; e < 16; ++e) s[e] = sm_keep(s[e], keep, 8 * (e >> 2) + (e & 3), none);
                 }
-                float p[FR][16];
+                float p[16];
 #pragma unroll
-                for (int f = 0; f < FR; ++f)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) p[f][e] = fast_exp2(fmaf(s[f][e], c2, -m[f])) * (z[f][e] - delta[f]);
-                sm_accum<T, D, FR>(acc, kc, p, lane);
+                for (int e = 0; e < 16; ++e) p[e] = fast_exp2(fmaf(s[e], c2, -m)) * (z[e] - delta);
+                sm_accum<T, D>(acc, kc, p, lane);
             }
         }
     };
@@ -616,47 +577,43 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(BWD ? SM_DQ : SM_FWD, (int)sizeo
     }
 
     __syncthreads();   // (the tiles' LDS is used for the results)
-#pragma unroll
-    for (int f = 0; f < FR; ++f) {
-        const int r = wr0 + 32 * f + (lane & 31), rc = min(r, R - 1), i = a.by_g(rc), hq = w.hk * a.G + (rc - i * a.G);
-        float scale = a.cs;
-        if constexpr (!BWD) {
-            sum[f] += __shfl_xor(sum[f], 32);
-            live[f] = live[f] && sum[f] > 0.f;
-            scale = live[f] ? 1.f / sum[f] : 0.f;
-            const float lse = live[f] ? (m[f] + fast_log2(sum[f])) * LN2 : -INFINITY;
-            if (h == 0 && r < R) {
-                if (a.parts > 1) a.part_lse[((long)w.part * a.B * a.Hk + prob) * R + r] = lse;
-                else a.lse[((long)w.b * a.G * a.Hk + hq) * a.Lq + i] = lse;
-            }
+    float scale = a.cs;
+    if constexpr (!BWD) {
+        sum += __shfl_xor(sum, 32);
+        live = live && sum > 0.f;
+        scale = live ? 1.f / sum : 0.f;
+        const float lse = live ? (m + fast_log2(sum)) * LN2 : -INFINITY;
+        if (h == 0 && r < R) {
+            if (a.parts > 1) a.part_lse[((long)w.part * a.B * a.Hk + prob) * R + r] = lse;
+            else a.lse[((long)w.b * a.G * a.Hk + hq) * a.Lq + i] = lse;
         }
-        if (a.parts > 1) {
-            float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * R + r) * D;
-            if (r >= R) continue;
+    }
+    if (a.parts > 1) {
+        float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * R + r) * D;
+        if (r >= R) return;
 #pragma unroll
-            for (int v = 0; v < D / 32; ++v)
+        for (int v = 0; v < D / 32; ++v)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    *reinterpret_cast<float4 *>(out + 32 * v + 8 * e + 4 * h) =
-                        live[f] ? make_float4(acc[f][v][4 * e] * scale, acc[f][v][4 * e + 1] * scale, acc[f][v][4 * e + 2] * scale, acc[f][v][4 * e + 3] * scale)
-                                : make_float4(0.f, 0.f, 0.f, 0.f);
-        } else {
-            T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + w.b * a.oq.b + (long)w.hk * a.G * a.oq.h;
-            sm_store_rows<T, D>(&lds[0][0][0] + (wv * FR + f) * TL::SUB, acc[f], scale, live[f], lane, [&](int x) -> T * {
-                const int rr = wr0 + 32 * f + x, ii = a.by_g(rr);
-                return rr < R ? out + (rr - ii * a.G) * a.oq.h + ii * a.oq.l : nullptr;
-            });
-        }
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<float4 *>(out + 32 * v + 8 * e + 4 * h) =
+                    live ? make_float4(acc[v][4 * e] * scale, acc[v][4 * e + 1] * scale, acc[v][4 * e + 2] * scale, acc[v][4 * e + 3] * scale)
+                         : make_float4(0.f, 0.f, 0.f, 0.f);
+    } else {
+        T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + w.b * a.oq.b + (long)w.hk * a.G * a.oq.h;
+        sm_store_rows<T, D>(&lds[0][0][0] + wv * TL::SUB, acc, scale, live, lane, [&](int x) -> T * {
+            const int rr = wr0 + x, ii = a.by_g(rr);
+            return rr < R ? out + (rr - ii * a.G) * a.oq.h + ii * a.oq.l : nullptr;
+        });
     }
 }
 
 // ------------------------------------------------------------------ keys as owners: dK, dV
 // The queries of one head after another: each is a walk of its own over the same positions.
-template <typename T, int D, int NW, int FR>
-__global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR))) void sm_keys_kernel(const SmArgs a)
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void sm_keys_kernel(const SmArgs a)
 {
     using TL = SmTile<T, D>;
-    constexpr int KT = TL::KT, NS = KT / 32, BM = 32 * NW * FR;
+    constexpr int KT = TL::KT, NS = KT / 32, BM = 32 * NW;
     constexpr int NBUF = 4 * TL::BYTES + 1024 <= 65536 ? 2 : 1;   // (fp32, d = 128: one, and other workgroups while it is filled)
     __shared__ __align__(1024) unsigned char lds[NBUF][2][TL::BYTES];
     __shared__ __align__(256) float vec[2][2][64];   // of the tile's rows: LSE log2(e) (inf: no such row), delta
@@ -668,14 +625,11 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const long prob = (long)w.b * a.Hk + w.hk;
     const int up = a.causal ? 0 : a.W;
-    OwnerFrag<T, D> k[FR], v[FR];
-    const int w_first = k0 + 32 * FR * wv, w_last = w_first + 32 * FR - 1;
-#pragma unroll
-    for (int f = 0; f < FR; ++f) {
-        const int jc = min(w_first + 32 * f + (lane & 31), a.Lk - 1);
-        sm_frag<T, D>(k[f], reinterpret_cast<const T *>(a.k.p) + w.b * a.k.b + w.hk * a.k.h + jc * a.k.l, h);
-        sm_frag<T, D>(v[f], reinterpret_cast<const T *>(a.v.p) + w.b * a.v.b + w.hk * a.v.h + jc * a.v.l, h);
-    }
+    OwnerFrag<T, D> k, v;
+    const int w_first = k0 + 32 * wv, w_last = w_first + 31;
+    const int jc = min(w_first + (lane & 31), a.Lk - 1);
+    sm_frag<T, D>(k, reinterpret_cast<const T *>(a.k.p) + w.b * a.k.b + w.hk * a.k.h + jc * a.k.l, h);
+    sm_frag<T, D>(v, reinterpret_cast<const T *>(a.v.p) + w.b * a.v.b + w.hk * a.v.h + jc * a.v.l, h);
 
     // queries that reach the block's keys: p - W <= j <= p + up
     const int k_last = min(min(k0 + BM, a.Lk), lk) - 1;
@@ -688,13 +642,11 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
         t1 = min(t1, t0 + per);
     }
 
-    f32x16 dk[FR][D / 32], dv[FR][D / 32];
+    f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
-    for (int f = 0; f < FR; ++f)
+    for (int x = 0; x < D / 32; ++x)
 #pragma unroll
-        for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) dk[f][x][e] = dv[f][x][e] = 0.f;
+        for (int e = 0; e < 16; ++e) dk[x][e] = dv[x][e] = 0.f;
 
     const long head0 = (long)w.b * a.G * a.Hk + w.hk * a.G;
     const T *qb = reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + (long)w.hk * a.G * a.q.h;
@@ -705,7 +657,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
     const unsigned lds_at = sm_lds(lds), vec_at = sm_lds(vec);
     SmActivity<T, D, NW> act;
     int head = t0 < t1 ? t0 / per_head : 0, at = t0 - head * per_head;   // of the next tile to fetch
-    auto fetch = [&](int buf) {
+    auto fetch = [&](int buf) __attribute__((always_inline)) {
         const int i0 = i_lo + at * KT, rows = i_hi + 1 - i0;
         loader.load(lds_at + buf * 2 * TL::BYTES, reinterpret_cast<const unsigned char *>(qb + head * a.q.h) + i0 * qs, qs, rows);
         loader.load(lds_at + (buf * 2 + 1) * TL::BYTES, reinterpret_cast<const unsigned char *>(gb + head * a.g.h) + i0 * gs, gs, rows);
@@ -720,7 +672,7 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
     };
     int i0 = i_lo + at * KT;   // first query of the tile at hand
     const float c2 = sm_vector(a.c2);
-    auto step = [&](auto which, int t) {
+    auto step = [&](auto which, int t) __attribute__((always_inline)) {
         constexpr int buf = decltype(which)::value;
         const int rows = i_hi + 1 - i0;
         if (NBUF == 1) {
@@ -745,47 +697,40 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
             const int p_first = start + i0 + 32 * n, p_last = p_first + 31;   // positions of the score tile's rows
             if (p_last + up < w_first || p_first - a.W > w_last || 32 * n >= rows) continue;
             const bool whole = p_first + up >= w_last && p_last - a.W <= w_first;
-            f32x16 s[FR], z[FR];
+            f32x16 s, z;
             SmRows<T, D> qr, gr;
             SmCols<T, D> qc, gc;
             qr.read(lds[buf][0] + n * TL::SUB, lane);
             gr.read(lds[buf][1] + n * TL::SUB, lane);
             SM_READ_FIRST();
-            sm_scores<T, D, FR>(s, qr, k, lane);
-            sm_scores<T, D, FR>(z, gr, v, lane);
+            sm_scores<T, D>(s, qr, k, lane);
+            sm_scores<T, D>(z, gr, v, lane);
             gc.read(lds[buf][1] + n * TL::SUB, lane);
             qc.read(lds[buf][0] + n * TL::SUB, lane);
             SM_READ_FIRST();
-            float p[FR][16], ds[FR][16];
+            float p[16], ds[16];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float4 l4 = *reinterpret_cast<const float4 *>(&vec[buf][0][32 * n + 8 * e + 4 * h]);
                 const float4 d4 = *reinterpret_cast<const float4 *>(&vec[buf][1][32 * n + 8 * e + 4 * h]);
                 const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-                for (int f = 0; f < FR; ++f)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        p[f][4 * e + x] = fast_exp2(fmaf(s[f][4 * e + x], c2, -ls[x]));
-                        ds[f][4 * e + x] = z[f][4 * e + x] - dl[x];
-                    }
-            }
-            if (!whole) {
-#pragma unroll
-                for (int f = 0; f < FR; ++f) {
-                    // pair (p, j): p - W <= j <= p + up; bits of the tile's rows p_first ...
-                    const int d = w_first + 32 * f + (lane & 31) - p_first;
-                    const unsigned keep = sm_bits(d - up, d + a.W) >> (4 * h);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) p[f][e] = sm_keep(p[f][e], keep, 8 * (e >> 2) + (e & 3), 0.f);
+                for (int x = 0; x < 4; ++x) {
+                    p[4 * e + x] = fast_exp2(fmaf(s[4 * e + x], c2, -ls[x]));
+                    ds[4 * e + x] = z[4 * e + x] - dl[x];
                 }
             }
+            if (!whole) {
+                // pair (p, j): p - W <= j <= p + up; bits of the tile's rows p_first ...
+                const int d = w_first + (lane & 31) - p_first;
+                const unsigned keep = sm_bits(d - up, d + a.W) >> (4 * h);
 #pragma unroll
-            for (int f = 0; f < FR; ++f)
+                for (int e = 0; e < 16; ++e) p[e] = sm_keep(p[e], keep, 8 * (e >> 2) + (e & 3), 0.f);
+            }
 #pragma unroll
-                for (int e = 0; e < 16; ++e) ds[f][e] *= p[f][e];
-            sm_accum<T, D, FR>(dv, gc, p, lane);
-            sm_accum<T, D, FR>(dk, qc, ds, lane);
+            for (int e = 0; e < 16; ++e) ds[e] *= p[e];
+            sm_accum<T, D>(dv, gc, p, lane);
+            sm_accum<T, D>(dk, qc, ds, lane);
         }
         i0 = next;
     };
@@ -796,35 +741,32 @@ __global__ __launch_bounds__(64 * NW, (sm_waves(SM_DKV, (int)sizeof(T), D, FR)))
     }
 
     __syncthreads();   // (the tiles' LDS is used for the results)
+    const int j = w_first + (lane & 31);
+    bool live = j < lk;
+    if (live && a.mask_k) live = a.mask_k[(long)w.b * a.Lk + j] != 0;
+    if (a.parts > 1) {
+        if (j >= a.Lk) return;
+        float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * a.Lk + j) * 2 * D;
 #pragma unroll
-    for (int f = 0; f < FR; ++f) {
-        const int j = w_first + 32 * f + (lane & 31);
-        bool live = j < lk;
-        if (live && a.mask_k) live = a.mask_k[(long)w.b * a.Lk + j] != 0;
-        if (a.parts > 1) {
-            if (j >= a.Lk) continue;
-            float *out = a.part + (((long)w.part * a.B * a.Hk + prob) * a.Lk + j) * 2 * D;
+        for (int x = 0; x < D / 32; ++x)
 #pragma unroll
-            for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float *o = out + 32 * x + 8 * e + 4 * h;
-                    *reinterpret_cast<float4 *>(o) = live ? make_float4(dk[f][x][4 * e] * a.cs, dk[f][x][4 * e + 1] * a.cs, dk[f][x][4 * e + 2] * a.cs, dk[f][x][4 * e + 3] * a.cs) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    *reinterpret_cast<float4 *>(o + D) = live ? make_float4(dv[f][x][4 * e], dv[f][x][4 * e + 1], dv[f][x][4 * e + 2], dv[f][x][4 * e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-        } else {
-            T *ok = reinterpret_cast<T *>(const_cast<void *>(a.ok.p)) + w.b * a.ok.b + w.hk * a.ok.h;
-            T *ov = reinterpret_cast<T *>(const_cast<void *>(a.ov.p)) + w.b * a.ov.b + w.hk * a.ov.h;
-            // (where one buffer of tiles has not room for all wavefronts' rows: two of them after the other two)
-            constexpr bool ROOM = sizeof(lds) >= NW * FR * TL::SUB;
-            unsigned char *mine = &lds[0][0][0] + (ROOM ? wv * FR + f : wv & 1) * TL::SUB;
-            for (int turn = 0; turn < (ROOM ? 1 : 2); ++turn) {
-                if (ROOM || wv >> 1 == turn) {
-                    sm_store_rows<T, D>(mine, dk[f], a.cs, live, lane, [&](int x) -> T * { return w_first + 32 * f + x < a.Lk ? ok + (w_first + 32 * f + x) * a.ok.l : nullptr; });
-                    sm_store_rows<T, D>(mine, dv[f], 1.f, live, lane, [&](int x) -> T * { return w_first + 32 * f + x < a.Lk ? ov + (w_first + 32 * f + x) * a.ov.l : nullptr; });
-                }
-                if (!ROOM) __syncthreads();
+            for (int e = 0; e < 4; ++e) {
+                float *o = out + 32 * x + 8 * e + 4 * h;
+                *reinterpret_cast<float4 *>(o) = live ? make_float4(dk[x][4 * e] * a.cs, dk[x][4 * e + 1] * a.cs, dk[x][4 * e + 2] * a.cs, dk[x][4 * e + 3] * a.cs) : make_float4(0.f, 0.f, 0.f, 0.f);
+                *reinterpret_cast<float4 *>(o + D) = live ? make_float4(dv[x][4 * e], dv[x][4 * e + 1], dv[x][4 * e + 2], dv[x][4 * e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
+    } else {
+        T *ok = reinterpret_cast<T *>(const_cast<void *>(a.ok.p)) + w.b * a.ok.b + w.hk * a.ok.h;
+        T *ov = reinterpret_cast<T *>(const_cast<void *>(a.ov.p)) + w.b * a.ov.b + w.hk * a.ov.h;
+        // (where one buffer of tiles has not room for all wavefronts' rows: two of them after the other two)
+        constexpr bool ROOM = sizeof(lds) >= NW * TL::SUB;
+        unsigned char *mine = &lds[0][0][0] + (ROOM ? wv : wv & 1) * TL::SUB;
+        for (int turn = 0; turn < (ROOM ? 1 : 2); ++turn) {
+            if (ROOM || wv >> 1 == turn) {
+                sm_store_rows<T, D>(mine, dk, a.cs, live, lane, [&](int x) -> T * { return w_first + x < a.Lk ? ok + (w_first + x) * a.ok.l : nullptr; });
+                sm_store_rows<T, D>(mine, dv, 1.f, live, lane, [&](int x) -> T * { return w_first + x < a.Lk ? ov + (w_first + x) * a.ov.l : nullptr; });
+            }
+            if (!ROOM) __syncthreads();
         }
     }
 }

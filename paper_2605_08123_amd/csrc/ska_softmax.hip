@@ -38,18 +38,17 @@ SmGrid sm_grid(const SmProblem &p, int what)
 {
     SmGrid g{4, 0, 1};
     const long owners = what == SM_DKV ? p.Lk : p.R();
-    const int bytes = p.dtype == SKA_F32 ? 4 : 2;
     // One wavefront per workgroup where there are no more rows, or where workgroups of four would leave CUs without any and share
     // little (a band: two problems of 4 heads, L = 701, W = 64, fp32, forward and backward 12.6 and 30.6 us with four, 10.9 and
     // 25.4 with one; all of 8 heads, L = 2000, d = 128, fp32: 176 and 549 with four, 718 and 1290 with one)
     if (owners <= 32 || ((owners + 127) / 128 * p.N() < 256 && sm_walk(p, what, 128) <= 512)) g.nw = 1;
-    const int rows = 32 * g.nw * sm_fr(what, bytes, p.d, g.nw);
+    const int rows = 32 * g.nw;
     g.blocks = (owners + rows - 1) / rows;
     // Parts where there are fewer wavefronts than SIMDs: one per SIMD in all (forward: two problems of 8 heads, L = 1000, causal
     // 19 us, with two 25) or two (backward, whose walks are longer: 16 heads on 4, L = 4096, d = 128, causal 311 us, with one 430),
     // but no fewer than two tiles each, since parts have to be joined by another launch (4 heads, L = 512, d = 64, causal, backward:
     // one tile 22.4 us, two 21.0, four 22.7).
-    const long tile = bytes == 2 && p.d < 128 ? 64 : 32, tiles = (sm_walk(p, what, rows) + tile - 1) / tile, waves = g.blocks * p.N() * g.nw;
+    const long tile = p.dtype == SKA_BF16 && p.d < 128 ? 64 : 32, tiles = (sm_walk(p, what, rows) + tile - 1) / tile, waves = g.blocks * p.N() * g.nw;
     if (waves < 1024) g.parts = (int)std::max(1L, std::min({(what == SM_FWD ? 1024 : 2048) / waves, tiles / 2, 256L}));
     return g;
 }

@@ -6,19 +6,18 @@ namespace {
 template <typename T, int D> int launch(int what, int nw, const SmArgs &a, hipStream_t st)
 {
     const dim3 grid((unsigned)((a.total + 7) / 8 * 8));
-    constexpr int E = (int)sizeof(T);
     switch (what) {
     case SM_FWD:
-        if (nw == 1) hipLaunchKernelGGL((sm_rows_kernel<T, D, 1, sm_fr(SM_FWD, E, D, 1), false>), grid, dim3(64), 0, st, a);
-        else hipLaunchKernelGGL((sm_rows_kernel<T, D, 4, sm_fr(SM_FWD, E, D, 4), false>), grid, dim3(256), 0, st, a);
+        if (nw == 1) hipLaunchKernelGGL((sm_rows_kernel<T, D, 1, false>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((sm_rows_kernel<T, D, 4, false>), grid, dim3(256), 0, st, a);
         break;
     case SM_DQ:
-        if (nw == 1) hipLaunchKernelGGL((sm_rows_kernel<T, D, 1, sm_fr(SM_DQ, E, D, 1), true>), grid, dim3(64), 0, st, a);
-        else hipLaunchKernelGGL((sm_rows_kernel<T, D, 4, sm_fr(SM_DQ, E, D, 4), true>), grid, dim3(256), 0, st, a);
+        if (nw == 1) hipLaunchKernelGGL((sm_rows_kernel<T, D, 1, true>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((sm_rows_kernel<T, D, 4, true>), grid, dim3(256), 0, st, a);
         break;
     default:
-        if (nw == 1) hipLaunchKernelGGL((sm_keys_kernel<T, D, 1, sm_fr(SM_DKV, E, D, 1)>), grid, dim3(64), 0, st, a);
-        else hipLaunchKernelGGL((sm_keys_kernel<T, D, 4, sm_fr(SM_DKV, E, D, 4)>), grid, dim3(256), 0, st, a);
+        if (nw == 1) hipLaunchKernelGGL((sm_keys_kernel<T, D, 1>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((sm_keys_kernel<T, D, 4>), grid, dim3(256), 0, st, a);
     }
     if (hipGetLastError() != hipSuccess) return SKA_EHIP;
     if (a.parts > 1) {
