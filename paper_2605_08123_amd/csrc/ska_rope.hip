@@ -1,10 +1,12 @@
 // Rotary positions of queries and keys, forward and gradient, in one launch (sinkhorn_attn_layer.h).
 //
 //   (x1, x2) -> a (x1 cos t - x2 sin t, x2 cos t + x1 sin t),  t = position * freq[k]; the gradient is the same with -t.
-// Bound by memory: each feature is read and written once.  A thread owns one slot of a token (16 bytes of each half, or
-// 16 bytes of adjacent pairs, or 16 bytes that are copied) and takes it through several heads, so that an angle's cosine and
-// sine, which cost about 40 instructions a pair, are found once for them.  Far positions make angles of 10^5 radians and
-// more, of which fp32 holds two decimals: the product and its reduction to a turn are in 64 bits, the rest in fp32.
+// Bound by memory: each feature is read and written once (MI355X: queries and keys of 2 heads, L = 262144, d = 64, bf16, 52 us on
+// tensors that no cache holds, 5.1 TB/s, 40 on the same ones again; with one head's pieces asked for at a time 60 and 44).
+// A thread owns one slot of a token (16 bytes of each half, or 16 bytes of adjacent pairs, or 16 bytes that are copied) and
+// takes it through several heads, so that an angle's cosine and sine, which cost about 40 instructions a pair, are found once
+// for them.  Far positions make angles of 10^5 radians and more, of which fp32 holds two decimals: the product and its
+// reduction to a turn are in 64 bits, the rest in fp32.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
