@@ -38,18 +38,45 @@ SmGrid sm_grid(const SmProblem &p, int what)
 {
     SmGrid g{4, 0, 1};
     const long owners = what == SM_DKV ? p.Lk : p.R();
+    const long problems = p.N(), alone = (owners + 31) / 32 * problems;   // alone: wavefronts, 32 owners each
+    const long other = what == SM_DKV ? p.Lq : p.Lk;
+    const bool band = 2L * p.W + 1 < other / 2, triangle = !band && p.causal && p.Lq > p.Lk / 2;
     // One wavefront per workgroup where there are no more rows, or where workgroups of four would leave CUs without any and share
     // little (a band: two problems of 4 heads, L = 701, W = 64, fp32, forward and backward 12.6 and 30.6 us with four, 10.9 and
-    // 25.4 with one; all of 8 heads, L = 2000, d = 128, fp32: 176 and 549 with four, 718 and 1290 with one)
-    if (owners <= 32 || ((owners + 127) / 128 * p.N() < 256 && sm_walk(p, what, 128) <= 512)) g.nw = 1;
+    // 25.4 with one; all of 8 heads, L = 2000, d = 128, fp32: 176 and 549 with four, 718 and 1290 with one).
+    if (owners <= 32 || ((owners + 127) / 128 * problems < 256 && sm_walk(p, what, 128) <= 512)) g.nw = 1;
+    // dK, dV of a band in fp32 as well: its products take eight times as long as bf16's, and a wavefront of four sits through the
+    // tiles that only the other three reach (backward of 8 heads on 2, d = 64, L = 43748, W = 32: 353 us with one, 496 with four;
+    // W = 256: 1474, 1621; bf16, 4 on 2, L = 65536, W = 256: 249, 174).  Not where that makes less than one wavefront per
+    // SIMD and more than one per two, since at d = 32 a CU has room for eight and takes them: 8 on 2, L = 14400, W = 256: 391, 311.
+    if (what == SM_DKV && band && p.dtype == SKA_F32 && (p.d > 32 || alone <= 512 || alone >= 1024)) g.nw = 1;
     const int rows = 32 * g.nw;
     g.blocks = (owners + rows - 1) / rows;
-    // Parts where there are fewer wavefronts than SIMDs: one per SIMD in all (forward: two problems of 8 heads, L = 1000, causal
-    // 19 us, with two 25) or two (backward, whose walks are longer: 16 heads on 4, L = 4096, d = 128, causal 311 us, with one 430),
-    // but no fewer than two tiles each, since parts have to be joined by another launch (4 heads, L = 512, d = 64, causal, backward:
-    // one tile 22.4 us, two 21.0, four 22.7).
-    const long tile = p.dtype == SKA_BF16 && p.d < 128 ? 64 : 32, tiles = (sm_walk(p, what, rows) + tile - 1) / tile, waves = g.blocks * p.N() * g.nw;
-    if (waves < 1024) g.parts = (int)std::max(1L, std::min({(what == SM_FWD ? 1024 : 2048) / waves, tiles / 2, 256L}));
+    // Parts where there are fewer wavefronts than SIMDs, to make it one each, but no fewer than two tiles to a part, since parts
+    // have to be joined by another launch (4 heads, L = 512, d = 64, causal, backward: one tile 22.4 us, two 21.0, four 22.7).
+    const long tile = p.dtype == SKA_BF16 && p.d < 128 ? 64 : 32, tiles = (sm_walk(p, what, rows) + tile - 1) / tile;
+    const long waves = g.blocks * problems * g.nw;
+    const auto parts = [&](long each, long least) { return std::max(1L, std::min({1024 * each / waves, tiles / least, 256L})); };
+    g.parts = (int)parts(1, 2);
+    if (triangle) {
+        // Where a causal mask makes walks of every length, two each, which also evens them out, and where there are up to two
+        // anyhow (8 heads, L = 4096, d = 128, forward and backward 69 and 200 us, without 91 and 262; fp32 347 and 1092, without
+        // 604 and 1923); in the forward if a part has 512 keys (fp32: 256; 4 heads, L = 2048, d = 64: 19.9 us with parts of 512,
+        // 25.0 with 256; fp32 43.7 with 256, 49.6 with 512).
+        g.parts = std::max(g.parts, (int)parts(2, what != SM_FWD ? 2 : p.dtype == SKA_F32 ? 8 : 512 / tile));
+    } else if (!band) {
+        // Two each if that takes less by this count: tiles of a part one after the other, and its start, end and joining, about
+        // four tiles' time (fp32: one); two wavefronts of a SIMD take twice as long, or 1.8 times in bf16 at d <= 64, where they
+        // fill each other's waits.  Backward, all of it: 16 heads on 4, L = 4096, d = 64, 264 us with two, 298 with one; 8 heads,
+        // L = 1400, d = 128, fp32, 331, 370; 8 heads, L = 2048, d = 128, 117, 104; 4 heads, L = 2048, d = 64, 55, 50.  Forward: 6
+        // heads on 2, L = 3270, d = 128, 57, 74; four sequences' 64 tokens on caches of 40000, 4 heads, d = 64, 36, 44.
+        const auto time = [&](long n) {
+            const long each = (waves * n + 1023) / 1024, start = p.dtype == SKA_F32 ? 1 : 4;
+            return (each == 2 && p.dtype == SKA_BF16 && p.d <= 64 ? 18 : 10 * each) * ((tiles + n - 1) / n + start);
+        };
+        const long two = parts(2, 2);
+        if (time(two) < time(g.parts)) g.parts = (int)two;
+    }
     return g;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
