@@ -191,6 +191,16 @@ def test_attention_sizes(Hq, Hk, L, W, causal, dtype, d):
     attn_case(1 + L % 2, Hq, Hk, L, L, d, W, causal, eps=0.5 if W else 1.0, dtype=dtype)
 
 
+@pytest.mark.parametrize("B,Hq,Hk,L,W,causal,dtype,d", [
+    (2, 16, 16, 1030, 1030, True, BF16, 64), (2, 16, 16, 1030, 1030, True, F32, 32),   # between one and two wavefronts per SIMD, walks of every length
+    (1, 16, 16, 1030, 2000, False, F32, 64), (1, 16, 16, 1030, 2000, False, BF16, 32),   # more than half of one, walks of one length
+    (2, 16, 16, 1030, 20, False, F32, 128), (2, 32, 16, 1030, 40, True, F32, 64),   # a band of many rows, single wavefronts for the keys in fp32
+    (1, 6, 2, 1600, 1600, False, BF16, 128), (1, 8, 2, 900, 900, True, F32, 128)])
+def test_attention_many_rows(B, Hq, Hk, L, W, causal, dtype, d):
+    """Enough rows for the other choices of workgroups and of parts of a walk."""
+    attn_case(B, Hq, Hk, L, L, d, W, causal, dtype=dtype)
+
+
 @pytest.mark.parametrize("dtype,d", [(F32, 32), (F32, 128), (BF16, 64), (BF16, 128)])
 @pytest.mark.parametrize("Hq,Hk,Lq,Lk,W", [(8, 2, 1, 1000, 1 << 30), (1, 1, 1, 1, 0), (4, 4, 1, 3000, 100), (6, 2, 17, 900, 1 << 25), (2, 1, 5, 5, 7),
                                            (2, 1, 40, 2500, 5000), (4, 1, 1, 20000, 1 << 20), (1, 1, 300, 2, 400), (2, 2, 1500, 3, 1 << 20)])
