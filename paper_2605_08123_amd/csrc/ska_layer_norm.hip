@@ -6,7 +6,7 @@
 //             registers until the block's last row, go to memory once per block and are added up by a second launch
 // Both are bound by memory (MI355X, where a copy of 4 GB reaches 4.8 TB/s): forward with a residual, 262144 rows of 512, bf16,
 // 190 us, 5.7 TB/s; backward, 30011 rows of 1283, fp32, 88 + 5 us, 5.3 TB/s in the first launch; 16384 rows of 512, bf16,
-// 16.5 + 3.9 us, 4.1 TB/s.  Of the last, with twice the blocks (more partial sums) 19.8 + 5.4, with rows asked for one ahead 17.2.
+// 16.5 + 3.9 us, 4.1 TB/s; 48828 rows of 4096, bf16, 233 us in all, 5.1 TB/s.
 // A row is dealt to TPR threads (a power of two) in NV pieces of 16 bytes, piece t + k TPR to thread t.  Rows of up to 256
 // pieces (backward: 128) are a wavefront's or several in one, so that their sums need no barrier; wider ones are a block's.
 #include <hip/hip_runtime.h>
@@ -21,7 +21,7 @@ namespace {
 
 constexpr int NT = 256;          // threads of a block whose rows stay in registers
 constexpr int NT_LOOP = 1024;    // threads of a block whose row does not
-constexpr int MAX_BLOCKS = 1024; // blocks (of partial sums) of the backward: four a CU, which its registers allow
+constexpr int MAX_BLOCKS = 1024; // blocks (of partial sums) of the backward: four a CU
 
 struct NormArgs {
     const void *x, *r, *w, *b;   // backward: x = dY, r = dS
@@ -50,6 +50,15 @@ template <int V, typename T> __device__ __forceinline__ void load_piece(const T 
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) f[i] = i < n ? (float)p[i] : 0.f;
+    }
+}
+// the same, as it lies in memory
+template <typename T> __device__ __forceinline__ void load_piece(const T *p, int n, Vec<T> &v)
+{
+    if (n >= VEC<T>) v = *reinterpret_cast<const Vec<T> *>(p);
+    else {
+#pragma unroll
+        for (int i = 0; i < VEC<T>; ++i) v[i] = i < n ? p[i] : (T)0.f;
     }
 }
 template <int V, typename T> __device__ __forceinline__ void store_piece(T *p, int n, const float (&f)[V])
@@ -217,6 +226,9 @@ template <typename T, typename TW> __global__ __launch_bounds__(NT_LOOP) void no
 template <typename T, typename TW, int NV> __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a)
 {
     constexpr int V = VEC<T>;
+    // Rows asked for one ahead in bf16 where the registers hold another (both launches for 262144 rows of 512 165 us, without 183;
+    // 110926 of 1803 377, 561; with NV = 4, 33333 of 6000, 540, 437).  fp32 rows are twice as long: 77942 of 1283 243, 236.
+    constexpr bool AHEAD = sizeof(T) == 2 && NV <= 2;
     __shared__ float red[2][NT / 64][2];
     extern __shared__ float sums[];   // with partial sums and rows of at most 64 threads: [wavefronts][tpr NV V]
     const int t = threadIdx.x & (a.tpr - 1), rows = NT / a.tpr;
@@ -232,26 +244,43 @@ template <typename T, typename TW, int NV> __global__ __launch_bounds__(NT) void
             dw[k][i] = db[k][i] = 0.f;
         }
     }
-    int turn = 0;
-    for (long first = (long)blockIdx.x * rows; first < a.N; first += (long)gridDim.x * rows, turn ^= 1) {
-        const long row = first + threadIdx.x / a.tpr;
-        const bool have = row < a.N;
-        const long at = have ? row : a.N - 1;
-        const float mean = a.stats[at], rstd = a.stats[a.N + at];
+    const long stride = (long)gridDim.x * rows;
+    Vec<T> ng[NV], nh[NV];   // the row at hand, or with AHEAD the next one
+    float mean, rstd;
+    auto ask = [&](long first) __attribute__((always_inline)) {
+        const long at = min(first + threadIdx.x / a.tpr, a.N - 1);
+        mean = a.stats[at];
+        rstd = a.stats[a.N + at];
         const T *gp = reinterpret_cast<const T *>(a.x) + at * a.ldx, *sp = reinterpret_cast<const T *>(a.s) + at * a.lds;
-        float g[NV][V], h[NV][V], sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (t + k * a.tpr) * V;
-            load_piece<V>(gp + c, a.D - c, g[k]);
-            load_piece<V>(sp + c, a.D - c, h[k]);
+            load_piece(gp + c, a.D - c, ng[k]);
+            load_piece(sp + c, a.D - c, nh[k]);
         }
+    };
+    if (AHEAD) ask((long)blockIdx.x * rows);
+    int turn = 0;
+    for (long first = (long)blockIdx.x * rows; first < a.N; first += stride, turn ^= 1) {
+        const long row = first + threadIdx.x / a.tpr;
+        const bool have = row < a.N;
+        if (!AHEAD) ask(first);
+        const float mu = mean, rs = rstd;
+        float g[NV][V], h[NV][V], sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                g[k][i] = (float)ng[k][i];
+                h[k][i] = (float)nh[k][i];
+            }
+        if (AHEAD && first + stride < a.N) ask(first + stride);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int n = a.D - (t + k * a.tpr) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                h[k][i] = i < n ? (h[k][i] - mean) * rstd : 0.f;
+                h[k][i] = i < n ? (h[k][i] - mu) * rs : 0.f;
                 if (have) {
                     dw[k][i] = fmaf(g[k][i], h[k][i], dw[k][i]);
                     db[k][i] += g[k][i];
@@ -272,7 +301,7 @@ template <typename T, typename TW, int NV> __global__ __launch_bounds__(NT) void
             float r[V], y[V];
             if (a.r) load_piece<V>(rp + c, a.D - c, r);
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = fmaf(rstd, g[k][i] - m0 - h[k][i] * m1, a.r ? r[i] : 0.f);
+            for (int i = 0; i < V; ++i) y[i] = fmaf(rs, g[k][i] - m0 - h[k][i] * m1, a.r ? r[i] : 0.f);
             store_piece<V>(yp + c, a.D - c, y);
         }
     }
@@ -416,7 +445,8 @@ inline RowShape row_shape(int pieces, int wave_nv, int most_nv)
     const int nv = pow2_at_least((pieces + NT - 1) / NT);
     return {NT, nv <= most_nv ? nv : 0};
 }
-constexpr int FWD_WAVE_NV = 4, FWD_NV = 8, BWD_WAVE_NV = 2, BWD_NV = 4;
+constexpr int FWD_WAVE_NV = 4, FWD_NV = 8, BWD_WAVE_NV = 2;
+template <typename T> constexpr int BWD_NV = 32 / VEC<T>;   // five arrays of 32 values in registers (fp32 rows of 6000: 237 us for 16666, by memory 420)
 
 inline bool type_ok(int dtype) { return dtype == SKA_F32 || dtype == SKA_BF16; }
 int check_rows(long long N, int D, int dtype, int wdtype)
@@ -457,7 +487,7 @@ template <typename T, typename TW> int norm_fwd(NormArgs a, hipStream_t st)
 
 template <typename T, typename TW> int norm_bwd(NormArgs a, TW *dw, TW *db, hipStream_t st)
 {
-    const RowShape sh = row_shape((a.D + VEC<T> - 1) / VEC<T>, BWD_WAVE_NV, BWD_NV);
+    const RowShape sh = row_shape((a.D + VEC<T> - 1) / VEC<T>, BWD_WAVE_NV, BWD_NV<T>);
     int parts = 0;
     if (a.N && !sh.nv) {
         if (a.part) {
@@ -470,12 +500,17 @@ template <typename T, typename TW> int norm_bwd(NormArgs a, TW *dw, TW *db, hipS
         a.tpr = sh.tpr;
         const int rows = NT / sh.tpr;
         const long blocks = (a.N + rows - 1) / rows;
-        parts = (int)(blocks < MAX_BLOCKS ? blocks : MAX_BLOCKS);
+        // as many as are there at a time, four a CU or what the registers allow (59808 rows of 3344, bf16, three a CU: 275 us, four:
+        // 341; 39062 of 2560, fp32, 227, 267)
+        const int values = sh.nv * VEC<T>, most = values <= 8 ? MAX_BLOCKS : values == 16 ? MAX_BLOCKS / 4 * 3 : MAX_BLOCKS / 2;
+        parts = (int)(blocks < most ? blocks : most);
         const int lds = a.part && sh.tpr <= 64 ? NT / 64 * sh.tpr * sh.nv * VEC<T> * 4 : 0;
         switch (sh.nv) {
         case 1: hipLaunchKernelGGL((norm_bwd_kernel<T, TW, 1>), dim3(parts), dim3(NT), lds, st, a); break;
         case 2: hipLaunchKernelGGL((norm_bwd_kernel<T, TW, 2>), dim3(parts), dim3(NT), lds, st, a); break;
-        default: hipLaunchKernelGGL((norm_bwd_kernel<T, TW, 4>), dim3(parts), dim3(NT), lds, st, a); break;
+        case 4: hipLaunchKernelGGL((norm_bwd_kernel<T, TW, 4>), dim3(parts), dim3(NT), lds, st, a); break;
+        default:
+            if constexpr (BWD_NV<T> == 8) hipLaunchKernelGGL((norm_bwd_kernel<T, TW, 8>), dim3(parts), dim3(NT), lds, st, a);
         }
     }
     if (dw || db)

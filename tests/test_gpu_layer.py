@@ -49,6 +49,24 @@ def test_layer_norm(rows, D, dtype, wdtype):
             ref.check(name, t, want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,D", [(40003, 40), (9001, 512), (5003, 1283), (3001, 2100), (2051, 4200), (1601, 8192), (700, 9000)])
+def test_layer_norm_many_rows(rows, D, dtype):
+    """More rows than a launch has room for at a time, also in place."""
+    say("layer norm, many rows", rows, D, dtype)
+    g = torch.Generator().manual_seed(rows + D)
+    s, dy, ds = (rnd(g, rows, D, dtype=dtype) for _ in range(3))
+    w = rnd(g, D, scale=0.3, shift=1.0)
+    _, _, mean, rstd = ref.norm_fwd(s, None, None, None, 1e-5)
+    st = torch.stack([mean[0], rstd[0]]).float()
+    x = dy.cuda()
+    got = ska.ska_layer_norm_bwd(x, s.cuda(), w.cuda(), st.cuda(), dS=ds.cuda())
+    for name, t, want in zip(("dX", "dweight", "dbias"), got, ref.norm_bwd(dy, s, w, st, ds, F32)):
+        ref.check(name, t, want)
+    again = ska.ska_layer_norm_bwd(x, s.cuda(), w.cuda(), st.cuda(), dS=ds.cuda(), dX=x)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
 @pytest.mark.parametrize("D", [96, 1000, 20000])
 def test_layer_norm_strides_and_places(D):
     """Rows apart, rows that start on any element, results in the inputs' place, no weights, only some of the results."""
