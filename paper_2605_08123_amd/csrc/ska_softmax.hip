@@ -44,7 +44,11 @@ SmGrid sm_grid(const SmProblem &p, int what)
     // One wavefront per workgroup where there are no more rows, or where workgroups of four would leave CUs without any and share
     // little (a band: two problems of 4 heads, L = 701, W = 64, fp32, forward and backward 12.6 and 30.6 us with four, 10.9 and
     // 25.4 with one; all of 8 heads, L = 2000, d = 128, fp32: 176 and 549 with four, 718 and 1290 with one).
-    if (owners <= 32 || ((owners + 127) / 128 * problems < 256 && sm_walk(p, what, 128) <= 512)) g.nw = 1;
+    // Two buffers of a pair of fp32 tiles of d = 128 are 64 KB, two workgroups a CU: single wavefronts only where there are half as
+    // many as that (8 heads on 4, L = 2000, W = 306, causal, forward and backward 81 and 184 us with one, 50 and 143 with four;
+    // 4 heads, L = 2000, W = 20, causal: 19 and 51, 30 and 66).
+    const bool large = what != SM_DKV && p.dtype == SKA_F32 && p.d == 128;
+    if (owners <= 32 || ((owners + 127) / 128 * problems < 256 && sm_walk(p, what, 128) <= 512 && !(large && alone > 256))) g.nw = 1;
     // dK, dV of a band in fp32 as well: its products take eight times as long as bf16's, and a wavefront of four sits through the
     // tiles that only the other three reach (backward of 8 heads on 2, d = 64, L = 43748, W = 32: 353 us with one, 496 with four;
     // W = 256: 1474, 1621; bf16, 4 on 2, L = 65536, W = 256: 249, 174).  Not where that makes less than one wavefront per
@@ -56,7 +60,8 @@ SmGrid sm_grid(const SmProblem &p, int what)
     // have to be joined by another launch (4 heads, L = 512, d = 64, causal, backward: one tile 22.4 us, two 21.0, four 22.7).
     const long tile = p.dtype == SKA_BF16 && p.d < 128 ? 64 : 32, tiles = (sm_walk(p, what, rows) + tile - 1) / tile;
     const long waves = g.blocks * problems * g.nw;
-    const auto parts = [&](long each, long least) { return std::max(1L, std::min({1024 * each / waves, tiles / least, 256L})); };
+    const long room = large && g.nw == 1 ? 512 : 1024;   // (4 heads' 8 tokens on a cache of 16384: 33 us, 38 with 1024)
+    const auto parts = [&](long each, long least) { return std::max(1L, std::min({room * each / waves, tiles / least, 256L})); };
     g.parts = (int)parts(1, 2);
     if (triangle) {
         // Where a causal mask makes walks of every length, two each, which also evens them out, and where there are up to two
@@ -71,7 +76,7 @@ SmGrid sm_grid(const SmProblem &p, int what)
         // L = 1400, d = 128, fp32, 331, 370; 8 heads, L = 2048, d = 128, 117, 104; 4 heads, L = 2048, d = 64, 55, 50.  Forward: 6
         // heads on 2, L = 3270, d = 128, 57, 74; four sequences' 64 tokens on caches of 40000, 4 heads, d = 64, 36, 44.
         const auto time = [&](long n) {
-            const long each = (waves * n + 1023) / 1024, start = p.dtype == SKA_F32 ? 1 : 4;
+            const long each = (waves * n + room - 1) / room, start = p.dtype == SKA_F32 ? 1 : 4;
             return (each == 2 && p.dtype == SKA_BF16 && p.d <= 64 ? 18 : 10 * each) * ((tiles + n - 1) / n + start);
         };
         const long two = parts(2, 2);
