@@ -27,19 +27,19 @@ int check(const SmProblem &p)
 
 // How one kernel of a call is launched: wavefronts per workgroup, blocks of owners, parts of a walk
 struct SmGrid { int nw; long blocks; int parts; };
-// Rows of the walked side that a block of `rows` owners can meet, at most (dK, dV: of all heads of the group)
+// Rows of the walked side that a block of `rows` owners can meet, at most (dK, dV: of one head of the group)
 long sm_walk(const SmProblem &p, int what, int rows)
 {
     const bool keys = what == SM_DKV;
     const long other = keys ? p.Lq : p.Lk, W = std::min<long>(p.W, other), own = keys ? std::min(rows, p.Lk) : std::min(rows / p.G() + 1, p.Lq);
-    return std::min(other, own + W + (p.causal ? 0 : W)) * (keys ? p.G() : 1);
+    return std::min(other, own + W + (p.causal ? 0 : W));
 }
 SmGrid sm_grid(const SmProblem &p, int what)
 {
     SmGrid g{4, 0, 1};
     const long owners = what == SM_DKV ? p.Lk : p.R();
     const long problems = p.N(), alone = (owners + 31) / 32 * problems;   // alone: wavefronts, 32 owners each
-    const long other = what == SM_DKV ? p.Lq : p.Lk;
+    const long other = what == SM_DKV ? p.Lq : p.Lk, heads = what == SM_DKV ? p.G() : 1;   // heads: walks of a block
     const bool band = 2L * p.W + 1 < other / 2, triangle = !band && p.causal && p.Lq > p.Lk / 2;
     // One wavefront per workgroup where there are no more rows, or where workgroups of four would leave CUs without any and share
     // little (a band: two problems of 4 heads, L = 701, W = 64, fp32, forward and backward 12.6 and 30.6 us with four, 10.9 and
@@ -48,7 +48,7 @@ SmGrid sm_grid(const SmProblem &p, int what)
     // many as that (8 heads on 4, L = 2000, W = 306, causal, forward and backward 81 and 184 us with one, 50 and 143 with four;
     // 4 heads, L = 2000, W = 20, causal: 19 and 51, 30 and 66).
     const bool large = what != SM_DKV && p.dtype == SKA_F32 && p.d == 128;
-    if (owners <= 32 || ((owners + 127) / 128 * problems < 256 && sm_walk(p, what, 128) <= 512 && !(large && alone > 256))) g.nw = 1;
+    if (owners <= 32 || ((owners + 127) / 128 * problems < 256 && sm_walk(p, what, 128) * heads <= 512 && !(large && alone > 256))) g.nw = 1;
     // dK, dV of a band in fp32 as well: its products take eight times as long as bf16's, and a wavefront of four sits through the
     // tiles that only the other three reach (backward of 8 heads on 2, d = 64, L = 43748, W = 32: 353 us with one, 496 with four;
     // W = 256: 1474, 1621; bf16, 4 on 2, L = 65536, W = 256: 249, 174).  Not where that makes less than one wavefront per
@@ -57,12 +57,14 @@ SmGrid sm_grid(const SmProblem &p, int what)
     const int rows = 32 * g.nw;
     g.blocks = (owners + rows - 1) / rows;
     // Parts where there are fewer wavefronts than SIMDs, to make it one each, but no fewer than two tiles to a part, since parts
-    // have to be joined by another launch (4 heads, L = 512, d = 64, causal, backward: one tile 22.4 us, two 21.0, four 22.7).
-    const long tile = p.dtype == SKA_BF16 && p.d < 128 ? 64 : 32, tiles = (sm_walk(p, what, rows) + tile - 1) / tile;
+    // have to be joined by another launch (4 heads, L = 512, d = 64, causal, backward: one tile 22.4 us, two 21.0, four 22.7); wide
+    // fp32 tiles of few rows take longer than that (4 heads on 1, L = 100, backward: d = 128, one tile 35 us, two 50; d = 64, 22, 29;
+    // not of many: 4 heads, L = 3000, W = 60, causal, d = 64: 46, 36).
+    const long tile = p.dtype == SKA_BF16 && p.d < 128 ? 64 : 32, tiles = (sm_walk(p, what, rows) + tile - 1) / tile * heads;
     const long waves = g.blocks * problems * g.nw;
     const long room = large && g.nw == 1 ? 512 : 1024;   // (4 heads' 8 tokens on a cache of 16384: 33 us, 38 with 1024)
     const auto parts = [&](long each, long least) { return std::max(1L, std::min({room * each / waves, tiles / least, 256L})); };
-    g.parts = (int)parts(1, 2);
+    g.parts = (int)parts(1, p.dtype == SKA_F32 && p.d >= 64 && waves <= 128 ? 1 : 2);
     if (triangle) {
         // Where a causal mask makes walks of every length, two each, which also evens them out, and where there are up to two
         // anyhow (8 heads, L = 4096, d = 128, forward and backward 69 and 200 us, without 91 and 262; fp32 347 and 1092, without
@@ -82,6 +84,11 @@ SmGrid sm_grid(const SmProblem &p, int what)
         const long two = parts(2, 2);
         if (time(two) < time(g.parts)) g.parts = (int)two;
     }
+    // (joining takes longer than a few tiles where there are many rows: 8 heads' gradient of one query on 2 heads' 8192 keys, d = 128,
+    // 27 us, 39 in two parts of two tiles)
+    if (p.dtype == SKA_BF16 && tiles < 8 && waves > 128) g.parts = 1;
+    const long per = std::max(1L, (tiles + g.parts - 1) / g.parts);
+    g.parts = (int)std::max(1L, (tiles + per - 1) / per);   // (none that would be empty)
     return g;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
