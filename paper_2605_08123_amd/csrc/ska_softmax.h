@@ -390,6 +390,7 @@ __device__ __forceinline__ unsigned sm_bits(int a, int b)
     return hi & lo;
 }
 
+constexpr float SM_NOTHING = -3.402823466e38f;   // LSE of a part whose scores are all -inf (one without keys: -inf)
 constexpr float SM_LAZY = 8.f;   // powers of two that a row's maximum may grow by before its sums are scaled to it
 
 enum { SM_FWD, SM_DQ, SM_DKV };
@@ -451,13 +452,14 @@ __global__ __launch_bounds__(64 * NW, 1) void sm_rows_kernel(const SmArgs a)
     const int my_lo = start + i - a.W, my_hi = min(start + i + up, lk - 1);
     sm_frag<T, D>(q, reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + hq * a.q.h + i * a.q.l, h);
     float m = -INFINITY, sum = 0.f, delta = 0.f;   // BWD: m = LSE log2(e)
+    unsigned keys = 0;                             // forward: not 0 where the row has met a key of its own
     if constexpr (BWD) {
         OwnerFrag<T, D> o;
         sm_frag<T, D>(g, reinterpret_cast<const T *>(a.g.p) + w.b * a.g.b + hq * a.g.h + i * a.g.l, h);
         sm_frag<T, D>(o, reinterpret_cast<const T *>(a.o.p) + w.b * a.o.b + hq * a.o.h + i * a.o.l, h);
         const long at = ((long)w.b * a.G * a.Hk + hq) * a.Lq + i;
         const float lse = a.lse[at];
-        live = live && lse > -INFINITY;
+        live = live && lse != -INFINITY;        // (NaN is a poisoned row's and goes on)
         m = live ? lse * LOG2E : INFINITY;      // (exp2(s - inf) = 0)
         delta = sm_dot<D>(g, o);
         if (!live) delta = 0.f;
@@ -493,6 +495,7 @@ __global__ __launch_bounds__(64 * NW, 1) void sm_rows_kernel(const SmArgs a)
         if constexpr (!BWD) {
             if (j0 > w_hi || j0 + KT - 1 < w_lo) return;
             const bool whole = j0 >= all_lo && j0 + KT - 1 <= all_hi && here == ~0ull;
+            if (whole) keys = 1;
             f32x16 s[NS];
             SmRows<T, D> kr[NS];
             SmCols<T, D> vc[NS];
@@ -508,7 +511,9 @@ __global__ __launch_bounds__(64 * NW, 1) void sm_rows_kernel(const SmArgs a)
 #pragma unroll
                 for (int n = 0; n < NS; ++n) {
                     const int base = j0 + 32 * n;
-                    const unsigned keep = (sm_bits(my_lo - base, min(my_hi, j_hi) - base) & (unsigned)(here >> (32 * n))) >> (4 * h);
+                    const unsigned own = sm_bits(my_lo - base, min(my_hi, j_hi) - base) & (unsigned)(here >> (32 * n));
+                    const unsigned keep = own >> (4 * h);
+                    keys |= own;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) s[n][e] = sm_keep(s[n][e], keep, 8 * (e >> 2) + (e & 3), none);
                 }
@@ -580,10 +585,13 @@ __global__ __launch_bounds__(64 * NW, 1) void sm_rows_kernel(const SmArgs a)
     __syncthreads();   // (the tiles' LDS is used for the results)
     float scale = a.cs;
     if constexpr (!BWD) {
+        // A row without a key is zeros, one that a NaN or an infinite score has poisoned is NaN: no comparison may take the second
+        // for the first.  Scores of -inf alone sum to 0 and are 0 / 0 too; in a part of a walk they weigh nothing (SM_NOTHING).
         sum += __shfl_xor(sum, 32);
-        live = live && sum > 0.f;
-        scale = live ? 1.f / sum : 0.f;
-        const float lse = live ? (m + fast_log2(sum)) * LN2 : -INFINITY;
+        live = live && keys != 0;
+        const bool nothing = sum == 0.f;
+        scale = nothing && a.parts > 1 ? 0.f : 1.f / sum;
+        const float lse = !live ? -INFINITY : !nothing ? (m + fast_log2(sum)) * LN2 : a.parts > 1 ? SM_NOTHING : NAN;
         if (h == 0 && r < R) {
             if (a.parts > 1) a.part_lse[((long)w.part * a.B * a.Hk + prob) * R + r] = lse;
             else a.lse[((long)w.b * a.G * a.Hk + hq) * a.Lq + i] = lse;
@@ -793,9 +801,10 @@ template <typename T, int D, int WHAT> __global__ __launch_bounds__(NTHREADS) vo
             const float4 y = *reinterpret_cast<const float4 *>(a.part + (s * rows + row) * F + f);
             float c = 1.f;
             if constexpr (WHAT == SM_JOIN_O) {
+                // (fmaxf passes over a NaN, so that m never is one; c is, and l and x from there on)
                 const float lse = a.part_lse[s * rows + row], mn = fmaxf(m, lse);
-                const float old = mn > -INFINITY ? fast_exp2((m - mn) * LOG2E) : 0.f;
-                c = mn > -INFINITY ? fast_exp2((lse - mn) * LOG2E) : 0.f;
+                const float old = m > -INFINITY ? fast_exp2((m - mn) * LOG2E) : 0.f;
+                c = lse != -INFINITY ? fast_exp2((lse - mn) * LOG2E) : 0.f;
                 l = fmaf(l, old, c);
                 x.x *= old; x.y *= old; x.z *= old; x.w *= old;
                 m = mn;
@@ -815,8 +824,8 @@ template <typename T, int D, int WHAT> __global__ __launch_bounds__(NTHREADS) vo
             float c = 1.f, old = 1.f;
             if constexpr (WHAT == SM_JOIN_O) {
                 const float mn = fmaxf(m, sm[o]);
-                old = mn > -INFINITY ? fast_exp2((m - mn) * LOG2E) : 0.f;
-                c = mn > -INFINITY ? fast_exp2((sm[o] - mn) * LOG2E) : 0.f;
+                old = m > -INFINITY ? fast_exp2((m - mn) * LOG2E) : 0.f;
+                c = sm[o] > -INFINITY ? fast_exp2((sm[o] - mn) * LOG2E) : 0.f;
                 l = l * old + sl[o] * c;
                 m = mn;
             }
@@ -831,10 +840,11 @@ template <typename T, int D, int WHAT> __global__ __launch_bounds__(NTHREADS) vo
         store4<T>(out + (f < D ? f : f - D), x.x, x.y, x.z, x.w);
     } else {
         const int i = a.by_g(r), hq = hk * a.G + (r - i * a.G);
-        const float c = WHAT == SM_JOIN_O ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+        if (WHAT == SM_JOIN_O && m == SM_NOTHING) l = NAN;   // (keys, whose scores are all -inf)
+        const float c = WHAT == SM_JOIN_O ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
         T *out = reinterpret_cast<T *>(const_cast<void *>(a.oq.p)) + b * a.oq.b + hq * a.oq.h + i * a.oq.l;
         store4<T>(out + f, x.x * c, x.y * c, x.z * c, x.w * c);
-        if (WHAT == SM_JOIN_O && f == 0) a.lse[((long)b * a.Hk * a.G + hq) * a.Lq + i] = l > 0.f ? m + fast_log2(l) * LN2 : -INFINITY;
+        if (WHAT == SM_JOIN_O && f == 0) a.lse[((long)b * a.Hk * a.G + hq) * a.Lq + i] = l == 0.f ? -INFINITY : m + fast_log2(l) * LN2;
     }
 }
 
