@@ -107,8 +107,9 @@ int ska_rope_bwd(const void *dQr, const ska_strides *dqr_strides, void *dQ, cons
  *   LSE [B,Hq,Lq] fp32.
  *   start_q, len_q, len_k: int32 device arrays [B] or NULL (0, Lq, Lk); starts are clamped to [0, 2^24], lengths to
  *   [0, Lq], [0, Lk].  mask_q [B,Lq], mask_k [B,Lk]: uint8 device arrays, nonzero = active, or NULL.
- *   Rows of inactive tokens and beyond the lengths may hold anything; a key that some query of its item can reach must be
- *   finite to leave the item's other queries alone.
+ *   Rows of inactive tokens and beyond the lengths may hold anything, and so may keys that no query, and queries that no key,
+ *   of their item reaches by position (|p - j| <= W, j <= p if `causal`, within the lengths; inactive ones reach as well).  An
+ *   active token that is reached must be finite to leave the item's others alone: products with a probability of 0 are formed.
  *   W >= 0 (W >= max(Lq, Lk) with starts of 0 is the dense problem); eps > 0 and finite.
  *   d in {32, 64, 128}; 1 <= Lq, Lk <= 2^24; B * Hk <= 65535, Lq * (Hq / Hk) <= 2^27.
  *   Pointers and strides in bytes: multiples of 16, tokens less than 128 MiB apart (SKA_EUNSUPPORTED otherwise).

@@ -730,11 +730,15 @@ __global__ __launch_bounds__(64 * NW, 1) void sm_keys_kernel(const SmArgs a)
                 }
             }
             if (!whole) {
-                // pair (p, j): p - W <= j <= p + up; bits of the tile's rows p_first ...
+                // pair (p, j): p - W <= j <= p + up; bits of the tile's rows p_first ... that exist.  dS is selected as well: a key that
+                // no query reaches may hold anything, and 0 times its dP is NaN where it does
                 const int d = w_first + (lane & 31) - p_first;
-                const unsigned keep = sm_bits(d - up, d + a.W) >> (4 * h);
+                const unsigned keep = sm_bits(d - up, min(d + a.W, rows - 1 - 32 * n)) >> (4 * h);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) p[e] = sm_keep(p[e], keep, 8 * (e >> 2) + (e & 3), 0.f);
+                for (int e = 0; e < 16; ++e) {
+                    p[e] = sm_keep(p[e], keep, 8 * (e >> 2) + (e & 3), 0.f);
+                    ds[e] = sm_keep(ds[e], keep, 8 * (e >> 2) + (e & 3), 0.f);
+                }
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) ds[e] *= p[e];

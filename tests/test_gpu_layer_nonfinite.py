@@ -130,3 +130,35 @@ def test_minus_infinity_alone_among_masked_keys(Lq, Lk, dtype):
 def test_the_last_shapes_are_in_parts():
     """(what the shapes above rely on)"""
     assert all(ska.ska_softmax_attn_workspace_bytes(False, B, Hq, Hk, Lq, Lk, d, W, c) > 0 for B, Hq, Hk, Lq, Lk, d, W, c in SHAPES[4:6])
+
+
+# B, Hq, Hk, Lq, Lk, d, W, causal, starts: keys past the causal end, beside the band on either side, queries past all keys
+UNREACHED = [(1, 2, 1, 1, 1024, 64, 1 << 20, True, [1000]), (2, 4, 2, 1, 1024, 128, 50, False, [1000, 300]), (2, 2, 2, 17, 900, 32, 40, True, [500, 0]),
+             (1, 4, 4, 300, 1500, 64, 25, False, [610]), (1, 2, 2, 400, 130, 32, 33, False, [0]), (1, 16, 16, 1100, 4000, 64, 70, True, [1501]),
+             (1, 8, 2, 40, 2600, 64, 1 << 20, True, [2000]), (2, 16, 16, 900, 1024, 128, 300, False, [0, 700])]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("fill", [math.nan, math.inf])
+@pytest.mark.parametrize("B,Hq,Hk,Lq,Lk,d,W,causal,start", UNREACHED)
+def test_what_nothing_reaches_may_hold_anything(B, Hq, Hk, Lq, Lk, d, W, causal, start, fill, dtype):
+    """Active keys that lie within no query's band, and queries within no key's, without lengths or masks: an unfilled cache."""
+    print("\n[case]", B, Hq, Hk, Lq, Lk, d, W, causal, start, fill, dtype, flush=True)
+    q, k, v, do = (x.cpu() for x in make(B, Hq, Hk, Lq, Lk, d, dtype, seed=9))
+    at = torch.tensor(start, dtype=torch.int32)
+    ok = ref.pairs(B, Lq, Lk, W, causal, start=at)
+    want = ref.attn(q, k, v, ok, 1.0, do)
+    assert not ok.any(1).all() or not ok.any(2).all()
+    for x, dead in ((q, ~ok.any(2)), (do, ~ok.any(2)), (k, ~ok.any(1)), (v, ~ok.any(1))):
+        x[dead[:, None].expand(x.shape[:3])] = fill
+    kw = dict(causal=causal, start_q=at.cuda())
+    q, k, v, do = (x.cuda() for x in (q, k, v, do))
+    O, LSE = ska.ska_softmax_attn_fwd(q, k, v, W, **kw)
+    ref.check("O", O, want["O"])
+    ref.check("LSE", LSE, want["LSE"])
+    grads = ska.ska_softmax_attn_bwd(q, k, v, want["O"][0].to(dtype).cuda(), do, want["LSE"][0].float().cuda(), W, **kw)
+    torch.cuda.synchronize()
+    for name, x in zip(("dQ", "dK", "dV"), grads):
+        ref.check(name, x, want[name])
+    dead = ~ok.any(1)[:, None].expand(B, Hk, Lk).cuda()
+    assert not grads[1][dead].any() and not grads[2][dead].any()
