@@ -1,4 +1,4 @@
-// Rotary positions of queries and keys, forward and gradient, in one launch (sinkhorn_attn_layer.h).
+// Rotary positions of queries and keys, forward and gradient, in one launch (several beyond 2^32 threads; sinkhorn_attn_layer.h).
 //
 //   (x1, x2) -> a (x1 cos t - x2 sin t, x2 cos t + x1 sin t),  t = position * freq[k]; the gradient is the same with -t.
 // Bound by memory: each feature is read and written once (MI355X: queries and keys of 2 heads, L = 262144, d = 64, bf16, 52 us on
@@ -10,6 +10,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "sinkhorn_attn_layer.h"
 
@@ -29,7 +31,7 @@ struct RopeArgs {
     const int *start, *pos;
     float amplitude;
     int back, L, d, rot, slots, heads;   // heads a thread takes, of the q.H + k.H
-    int wide;                            // slots of an item do not fit 32 bits
+    int l0, l1;                          // tokens of this launch
 };
 enum { ROPE_ONE = 0, ROPE_HALVES = 1, ROPE_ADJACENT = 2 };   // a slot: one pair or feature; 16 bytes of either half; 16 bytes of pairs
 
@@ -39,17 +41,9 @@ template <typename T, int FORM, bool INTER> __global__ __launch_bounds__(NT) voi
     constexpr int PAIRS = FORM == ROPE_ADJACENT ? V / 2 : V;                 // pairs of a slot
     typedef T vec __attribute__((ext_vector_type(V)));
     const int b = blockIdx.z;
-    int l, slot;
-    if (a.wide) {
-        const long at = (long)blockIdx.x * NT + threadIdx.x;
-        l = (int)(at / a.slots);
-        slot = (int)(at - (long)l * a.slots);
-    } else {
-        const unsigned at = blockIdx.x * NT + threadIdx.x;
-        l = (int)(at / (unsigned)a.slots);
-        slot = (int)(at - (unsigned)l * a.slots);
-    }
-    if (l >= a.L) return;
+    const unsigned at = blockIdx.x * NT + threadIdx.x, token = at / (unsigned)a.slots;
+    const int l = a.l0 + (int)token, slot = (int)(at - token * (unsigned)a.slots);
+    if (l >= a.l1) return;
     const int npair = a.rot / 2 / PAIRS;                                      // slots that are turned
     const bool turned = slot < npair;
     // features of the slot: at f0 and, where a second piece belongs to it, at f1
@@ -154,15 +148,19 @@ template <typename T> int launch_rope(RopeArgs a, int B, int interleaved, hipStr
     const long threads = (long)B * a.L * a.slots;
     a.heads = H;
     while (a.heads > 1 && threads * ((H + a.heads - 1) / a.heads) < (1 << 19)) a.heads = (a.heads + 1) / 2;
-    const long blocks = ((long)a.L * a.slots + NT - 1) / NT;
-    a.wide = blocks * NT > 0xffffffffL;
-    const dim3 grid((unsigned)blocks, (H + a.heads - 1) / a.heads, B);
-    if (!pieces) {
-        if (interleaved) hipLaunchKernelGGL((rope_kernel<T, ROPE_ONE, true>), grid, dim3(NT), 0, st, a);
-        else hipLaunchKernelGGL((rope_kernel<T, ROPE_ONE, false>), grid, dim3(NT), 0, st, a);
-    } else if (interleaved) hipLaunchKernelGGL((rope_kernel<T, ROPE_ADJACENT, true>), grid, dim3(NT), 0, st, a);
-    else hipLaunchKernelGGL((rope_kernel<T, ROPE_HALVES, false>), grid, dim3(NT), 0, st, a);
-    return hipGetLastError() == hipSuccess ? SKA_OK : SKA_EHIP;
+    const long most = (0xffffffffL / NT) * NT / a.slots;   // tokens of a launch, which has fewer than 2^32 threads in a dimension
+    for (long l0 = 0; l0 < a.L; l0 += most) {
+        a.l0 = (int)l0;
+        a.l1 = (int)std::min<long>(a.L, l0 + most);
+        const dim3 grid((unsigned)(((long)(a.l1 - a.l0) * a.slots + NT - 1) / NT), (H + a.heads - 1) / a.heads, B);
+        if (!pieces) {
+            if (interleaved) hipLaunchKernelGGL((rope_kernel<T, ROPE_ONE, true>), grid, dim3(NT), 0, st, a);
+            else hipLaunchKernelGGL((rope_kernel<T, ROPE_ONE, false>), grid, dim3(NT), 0, st, a);
+        } else if (interleaved) hipLaunchKernelGGL((rope_kernel<T, ROPE_ADJACENT, true>), grid, dim3(NT), 0, st, a);
+        else hipLaunchKernelGGL((rope_kernel<T, ROPE_HALVES, false>), grid, dim3(NT), 0, st, a);
+        if (hipGetLastError() != hipSuccess) return SKA_EHIP;
+    }
+    return SKA_OK;
 }
 
 int rope(int back, const void *Q, const ska_strides *qs, void *Qr, const ska_strides *qrs, const void *K, const ska_strides *ks, void *Kr,
