@@ -29,6 +29,7 @@ struct NormArgs {
     long ldx, ldr, lds, ldy;
     float *stats;
     long N;
+    long first;                  // row of the launch's first block (kernels with blocks for all rows)
     int D;
     float eps;
     int tpr;                     // threads per row
@@ -103,7 +104,7 @@ template <typename T, typename TW, int NV> __global__ __launch_bounds__(NT) void
     constexpr int V = VEC<T>;
     __shared__ float red[2][NT / 64][1];
     const int t = threadIdx.x & (a.tpr - 1);
-    const long row = (long)blockIdx.x * (NT / a.tpr) + threadIdx.x / a.tpr;
+    const long row = a.first + (long)blockIdx.x * (NT / a.tpr) + threadIdx.x / a.tpr;
     const bool have = row < a.N;
     const long at = have ? row : a.N - 1;
     float x[NV][V];
@@ -172,7 +173,7 @@ template <typename T, typename TW> __global__ __launch_bounds__(NT_LOOP) void no
 {
     constexpr int V = VEC<T>;
     __shared__ float red[2][NT_LOOP / 64][1];
-    const long row = blockIdx.x;
+    const long row = a.first + blockIdx.x;
     const T *xp = reinterpret_cast<const T *>(a.x) + row * a.ldx;
     const int first = threadIdx.x * V;
     constexpr int step = NT_LOOP * V;
@@ -344,7 +345,7 @@ template <typename T, typename TW> __global__ __launch_bounds__(NT_LOOP) void no
 {
     constexpr int V = VEC<T>;
     __shared__ float red[NT_LOOP / 64][2];
-    const long row = blockIdx.x;
+    const long row = a.first + blockIdx.x;
     const T *gp = reinterpret_cast<const T *>(a.x) + row * a.ldx, *sp = reinterpret_cast<const T *>(a.s) + row * a.lds;
     const float mean = a.stats[row], rstd = a.stats[a.N + row];
     const int first = threadIdx.x * V;
@@ -459,6 +460,16 @@ int check_rows(long long N, int D, int dtype, int wdtype)
 inline bool in_ok(long long ld) { return ld >= 0; }
 inline bool out_ok(long long ld, long long N, int D) { return ld >= 0 && (N <= 1 || ld >= D); }
 inline int launched() { return hipGetLastError() == hipSuccess ? SKA_OK : SKA_EHIP; }
+// launches a kernel with `rows` rows to a block of `threads` for all rows: several times where that takes 2^32 threads or more (a launch is accepted with more, and runs their number modulo 2^32)
+template <typename K> int for_all_rows(K kernel, NormArgs a, int rows, int threads, hipStream_t st)
+{
+    const long most = 0xffffffffL / threads;   // blocks of a launch
+    for (long left = (a.N + rows - 1) / rows; left > 0; left -= most, a.first += most * rows) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(left < most ? left : most)), dim3(threads), 0, st, a);
+        if (hipGetLastError() != hipSuccess) return SKA_EHIP;
+    }
+    return SKA_OK;
+}
 
 template <typename F> int with_types(int dtype, int wdtype, F f)
 {
@@ -469,20 +480,15 @@ template <typename F> int with_types(int dtype, int wdtype, F f)
 template <typename T, typename TW> int norm_fwd(NormArgs a, hipStream_t st)
 {
     const RowShape sh = row_shape((a.D + VEC<T> - 1) / VEC<T>, FWD_WAVE_NV, FWD_NV);
-    if (!sh.nv) {
-        hipLaunchKernelGGL((norm_fwd_loop_kernel<T, TW>), dim3((unsigned)a.N), dim3(NT_LOOP), 0, st, a);
-        return launched();
-    }
+    if (!sh.nv) return for_all_rows(norm_fwd_loop_kernel<T, TW>, a, 1, NT_LOOP, st);
     a.tpr = sh.tpr;
     const int rows = NT / sh.tpr;
-    const dim3 grid((unsigned)((a.N + rows - 1) / rows));
     switch (sh.nv) {
-    case 1: hipLaunchKernelGGL((norm_fwd_kernel<T, TW, 1>), grid, dim3(NT), 0, st, a); break;
-    case 2: hipLaunchKernelGGL((norm_fwd_kernel<T, TW, 2>), grid, dim3(NT), 0, st, a); break;
-    case 4: hipLaunchKernelGGL((norm_fwd_kernel<T, TW, 4>), grid, dim3(NT), 0, st, a); break;
-    default: hipLaunchKernelGGL((norm_fwd_kernel<T, TW, 8>), grid, dim3(NT), 0, st, a); break;
+    case 1: return for_all_rows(norm_fwd_kernel<T, TW, 1>, a, rows, NT, st);
+    case 2: return for_all_rows(norm_fwd_kernel<T, TW, 2>, a, rows, NT, st);
+    case 4: return for_all_rows(norm_fwd_kernel<T, TW, 4>, a, rows, NT, st);
+    default: return for_all_rows(norm_fwd_kernel<T, TW, 8>, a, rows, NT, st);
     }
-    return launched();
 }
 
 template <typename T, typename TW> int norm_bwd(NormArgs a, TW *dw, TW *db, hipStream_t st)
@@ -495,7 +501,8 @@ template <typename T, typename TW> int norm_bwd(NormArgs a, TW *dw, TW *db, hipS
             parts = (int)(a.N < MAX_BLOCKS / 4 ? a.N : MAX_BLOCKS / 4);
             hipLaunchKernelGGL((norm_columns_kernel<T>), dim3(cols, parts), dim3(NT), 0, st, a);   // (before dX, which may be dY)
         }
-        hipLaunchKernelGGL((norm_bwd_loop_kernel<T, TW>), dim3((unsigned)a.N), dim3(NT_LOOP), 0, st, a);
+        const int rc = for_all_rows(norm_bwd_loop_kernel<T, TW>, a, 1, NT_LOOP, st);
+        if (rc != SKA_OK) return rc;
     } else if (a.N) {
         a.tpr = sh.tpr;
         const int rows = NT / sh.tpr;
@@ -531,7 +538,7 @@ int ska_layer_norm_fwd(const void *X, long long ldx, const void *R, long long ld
     if (rc != SKA_OK) return rc;
     if (!in_ok(ldx) || !out_ok(ldy, N, D) || (R && (!in_ok(ldr) || !out_ok(lds, N, D)))) return SKA_EINVAL;
     if (N == 0) return SKA_OK;
-    const NormArgs a{X, R, weight, bias, S, Y, (long)ldx, (long)ldr, (long)lds, (long)ldy, stats, (long)N, D, ln_eps, 0, nullptr};
+    const NormArgs a{X, R, weight, bias, S, Y, (long)ldx, (long)ldr, (long)lds, (long)ldy, stats, (long)N, 0, D, ln_eps, 0, nullptr};
     return with_types(dtype, wdtype, [&](auto t, auto w) { return norm_fwd<decltype(t), decltype(w)>(a, static_cast<hipStream_t>(stream)); });
 }
 
@@ -556,7 +563,7 @@ int ska_layer_norm_bwd(const void *dY, long long lddy, const void *S, long long 
     }
     if (N == 0 && !sums) return SKA_OK;
     const NormArgs a{dY, dS, weight, nullptr, const_cast<void *>(S), dX, (long)lddy, (long)ldds, (long)lds, (long)lddx,
-                     const_cast<float *>(stats), (long)N, D, 0.f, 0, sums ? static_cast<float *>(workspace) : nullptr};
+                     const_cast<float *>(stats), (long)N, 0, D, 0.f, 0, sums ? static_cast<float *>(workspace) : nullptr};
     return with_types(dtype, wdtype, [&](auto t, auto w) {
         using TW = decltype(w);
         return norm_bwd<decltype(t), TW>(a, static_cast<TW *>(dweight), static_cast<TW *>(dbias), static_cast<hipStream_t>(stream));
