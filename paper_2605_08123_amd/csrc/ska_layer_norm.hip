@@ -460,7 +460,8 @@ int check_rows(long long N, int D, int dtype, int wdtype)
 inline bool in_ok(long long ld) { return ld >= 0; }
 inline bool out_ok(long long ld, long long N, int D) { return ld >= 0 && (N <= 1 || ld >= D); }
 inline int launched() { return hipGetLastError() == hipSuccess ? SKA_OK : SKA_EHIP; }
-// launches a kernel with `rows` rows to a block of `threads` for all rows: several times where that takes 2^32 threads or more (a launch is accepted with more, and runs their number modulo 2^32)
+// Launches a kernel with `rows` rows to a block of `threads` for all rows, several times where that takes 2^32 threads or more: a
+// launch is accepted with more, and runs their number modulo 2^32.
 template <typename K> int for_all_rows(K kernel, NormArgs a, int rows, int threads, hipStream_t st)
 {
     const long most = 0xffffffffL / threads;   // blocks of a launch

@@ -16,12 +16,16 @@ struct SmProblem {
     long R() const { return (long)Lq * G(); }
     long N() const { return (long)B * Hk; }
 };
-int check(const SmProblem &p)
+int check(const SmProblem &p, bool backward)
 {
     if (p.B < 1 || p.Hq < 1 || p.Hk < 1 || p.Lq < 1 || p.Lk < 1 || p.W < 0 || p.Hq % p.Hk) return SKA_EINVAL;
     if (p.d != 32 && p.d != 64 && p.d != 128) return SKA_EUNSUPPORTED;
     if (p.dtype != SKA_F32 && p.dtype != SKA_BF16) return SKA_EUNSUPPORTED;
     if (p.Lq > 1 << 24 || p.Lk > 1 << 24 || p.N() > 65535 || p.R() > 1 << 27) return SKA_EUNSUPPORTED;
+    // Two threads a row in whole workgroups of 128 rows, or four times as many of 32: fewer than 2^32 threads with the grid's
+    // rounding up to 8 workgroups (a launch is accepted with more, and runs their number modulo 2^32)
+    const long owners = backward ? std::max<long>(p.R(), p.Lk) : p.R();
+    if ((owners + 127) / 128 * p.N() > (1 << 24) - 8) return SKA_EUNSUPPORTED;
     return SKA_OK;
 }
 
@@ -131,9 +135,7 @@ int launch(int what, const SmProblem &p, const SmGrid &g, SmArgs a, hipStream_t 
 {
     a.parts = g.parts;
     a.blocks = (int)g.blocks;
-    const long total = g.blocks * g.parts * p.N();
-    if (total > 0x7ffffff0L) return SKA_EUNSUPPORTED;
-    a.total = (int)total;
+    a.total = (int)(g.blocks * g.parts * p.N());   // (check: below 2^26; parts only where there are few)
     a.by_g = SmDiv::by(a.G);
     a.by_hk = SmDiv::by(a.Hk);
     a.by_n = SmDiv::by(a.B * a.Hk);
@@ -167,7 +169,7 @@ extern "C" {
 size_t ska_softmax_attn_workspace_bytes(int backward, int B, int Hq, int Hk, int Lq, int Lk, int d, int W, int causal, int dtype)
 {
     const SmProblem p{B, Hq, Hk, Lq, Lk, d, W, causal, dtype};
-    if (check(p) != SKA_OK) return 0;
+    if (check(p, backward) != SKA_OK) return 0;
     return backward ? ws_bwd(p) : ws_fwd(p);
 }
 
@@ -179,7 +181,7 @@ int ska_softmax_attn_fwd(const void *Q, const ska_strides *q_strides, const void
 {
     const SmProblem p{B, Hq, Hk, Lq, Lk, d, W, causal, dtype};
     if (!LSE || !eps_ok(eps)) return SKA_EINVAL;
-    int rc = check(p);
+    int rc = check(p, false);
     if (rc != SKA_OK) return rc;
     SmArgs a = args_of(p, eps, LSE, start_q, len_q, len_k, mask_q, mask_k);
     if ((rc = tensor_of(a.q, Q, q_strides, B, Hq, Lq, d, dtype, false)) != SKA_OK) return rc;
@@ -204,7 +206,7 @@ int ska_softmax_attn_bwd(const void *Q, const ska_strides *q_strides, const void
 {
     const SmProblem p{B, Hq, Hk, Lq, Lk, d, W, causal, dtype};
     if (!LSE || !eps_ok(eps)) return SKA_EINVAL;
-    int rc = check(p);
+    int rc = check(p, true);
     if (rc != SKA_OK) return rc;
     SmArgs a = args_of(p, eps, const_cast<float *>(LSE), start_q, len_q, len_k, mask_q, mask_k);
     if ((rc = tensor_of(a.q, Q, q_strides, B, Hq, Lq, d, dtype, false)) != SKA_OK) return rc;

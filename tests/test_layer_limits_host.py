@@ -1,0 +1,20 @@
+"""Limits of the layer operators' sizes and arguments that hold before anything is launched (no GPU)."""
+import paper_2605_08123_amd as ska
+from paper_2605_08123_amd import binding, layer
+
+
+def test_softmax_sizes_fit_a_launch():
+    """2^24 - 8 blocks of 128 rows: a refused size has no workspace and its calls are SKA_EUNSUPPORTED."""
+    most, rows = (1 << 24) - 8, 1 << 24
+    need = lambda n, Lq, Lk=1, G=1, back=True, W=8: ska.ska_softmax_attn_workspace_bytes(back, 1, n * G, n, Lq, Lk, 32, W)   # noqa: E731
+    full = most // (rows // 128)      # 127 problems of 2^24 rows, and one more
+    assert need(full, rows) > 0 and need(full, 1, rows) > 0 and need(full, rows // 4, 1, 4) > 0
+    assert need(full + 1, rows) == 0 and need(full + 1, 1, rows) == 0 and need(full + 1, rows // 4, 1, 4) == 0
+    assert need(65535, 128 * 256) > 0 and need(65535, 128 * 256 + 1) == 0
+    # the forward's blocks are the queries' alone: one token against a cache of any documented size
+    assert need(full + 1, 1, rows, back=False, W=rows) > 0 and need(full + 1, 1, rows, W=rows) == 0
+    lib, P = layer._lib(), 1 << 20   # (not read: the size is refused first)
+    args = [1, full + 1, full + 1, rows, 1, 32, 8, 0, 1.0, binding.SKA_BF16]
+    assert lib.ska_softmax_attn_fwd(P, None, P, None, P, None, P, None, P, *[None] * 5, *args, P, 1 << 60, None) == binding.SKA_EUNSUPPORTED
+    assert lib.ska_softmax_attn_bwd(P, None, P, None, P, None, P, None, P, None, P, P, None, P, None, P, *[None] * 6, *args, P, 1 << 60,
+                                    None) == binding.SKA_EUNSUPPORTED
