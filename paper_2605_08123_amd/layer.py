@@ -60,7 +60,13 @@ def _code(t: torch.Tensor) -> int:
 
 # (A call of a microsecond's work is bound by what follows here: sizes are compared as they are, contiguous tensors pass no
 # strides, and the device and its stream are asked for once.)
-_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+_device = torch.cuda.current_device
+
+
+def _raw_stream(dev):
+    # (looked for when a call needs it: not every build of torch has it, and host-side calls need none)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream(dev).cuda_stream if raw is None else raw(dev)
 
 
 def _here(x: torch.Tensor, name: str) -> int:

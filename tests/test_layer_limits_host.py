@@ -1,6 +1,14 @@
-"""Limits of the layer operators' sizes and arguments that hold before anything is launched (no GPU)."""
+"""The layer operators' binding and the limits of their sizes and arguments that hold before anything is launched (no GPU)."""
+import os
+import subprocess
+import sys
+
+import torch
+
 import paper_2605_08123_amd as ska
 from paper_2605_08123_amd import binding, layer
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def test_softmax_sizes_fit_a_launch():
@@ -18,3 +26,18 @@ def test_softmax_sizes_fit_a_launch():
     assert lib.ska_softmax_attn_fwd(P, None, P, None, P, None, P, None, P, *[None] * 5, *args, P, 1 << 60, None) == binding.SKA_EUNSUPPORTED
     assert lib.ska_softmax_attn_bwd(P, None, P, None, P, None, P, None, P, None, P, P, None, P, None, P, *[None] * 6, *args, P, 1 << 60,
                                     None) == binding.SKA_EUNSUPPORTED
+
+
+def test_import_without_the_raw_stream():
+    """A build of torch without its function for the raw stream: the package is imported, host-side calls work."""
+    code = ("import torch; del torch._C._cuda_getCurrentRawStream\n"
+            "import paper_2605_08123_amd as ska\n"
+            "assert ska.ska_rope_frequencies(8)[0].numel() == 4 and ska.ska_layer_norm_workspace_bytes(8, 64) > 0\n")
+    res = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, res.stderr
+
+
+def test_the_stream_without_the_raw_function(monkeypatch):
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev: type("Stream", (), {"cuda_stream": 40 + dev}))
+    assert layer._raw_stream(2) == 42
