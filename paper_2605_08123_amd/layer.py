@@ -69,6 +69,12 @@ def _raw_stream(dev):
     return torch.cuda.current_stream(dev).cuda_stream if raw is None else raw(dev)
 
 
+def _int32(x) -> int:
+    """The nearest 32-bit integer: ctypes keeps the lower bits of what does not fit, and W = 2**32 would be 0."""
+    x = int(x)
+    return x if -0x80000000 <= x <= 0x7fffffff else 0x7fffffff if x > 0 else -0x80000000
+
+
 def _here(x: torch.Tensor, name: str) -> int:
     """The current device's number, which x must live on."""
     if not x.is_cuda:
@@ -227,7 +233,7 @@ def ska_rope_frequencies(rot, base=10000.0, scaling="none", factor=1.0, trained_
         raise ValueError(f"scaling: one of {sorted(ROPE_SCALINGS)}, got {scaling!r}")
     freq = torch.empty(max(int(rot), 0) // 2, dtype=torch.float64)
     amplitude = _d()
-    _done(_lib().ska_rope_frequencies(int(rot), float(base), ROPE_SCALINGS[scaling], float(factor), int(trained_length),
+    _done(_lib().ska_rope_frequencies(_int32(rot), float(base), ROPE_SCALINGS[scaling], float(factor), _int32(trained_length),
                                       freq.data_ptr() if freq.numel() else None, ctypes.addressof(amplitude)))
     return freq, amplitude.value
 
@@ -275,7 +281,7 @@ def ska_rope_bwd(dQr, dKr, freq, amplitude=1.0, interleaved=False, start=None, p
 
 # ------------------------------------------------------------------ softmax attention on a band
 def ska_softmax_attn_workspace_bytes(backward, B, Hq, Hk, Lq, Lk, d, W, causal=False, dtype=SKA_BF16) -> int:
-    return int(_lib().ska_softmax_attn_workspace_bytes(int(bool(backward)), B, Hq, Hk, Lq, Lk, d, W, int(bool(causal)), dtype))
+    return int(_lib().ska_softmax_attn_workspace_bytes(int(bool(backward)), B, Hq, Hk, Lq, Lk, d, _int32(W), int(bool(causal)), dtype))
 
 
 def _sizes(Q, K):
@@ -301,7 +307,7 @@ def ska_softmax_attn_fwd(Q, K, V, W, causal=False, eps=1.0, len_q=None, len_k=No
     if LSE is None:
         LSE = Q.new_empty((B, Hq, Lq), dtype=torch.float32)
     lib = _lib()
-    W, causal, i32, u8 = int(W), 1 if causal else 0, torch.int32, torch.uint8
+    W, causal, i32, u8 = _int32(W), 1 if causal else 0, torch.int32, torch.uint8
     ws, n, keep = _workspace(workspace, lib.ska_softmax_attn_workspace_bytes(0, B, Hq, Hk, Lq, Lk, d, W, causal, code), Q, dev)
     _done(lib.ska_softmax_attn_fwd(
         qp, qs, kp, ks, vp, vs, op, os, _plain(LSE, (B, Hq, Lq), torch.float32, dev, "LSE"), _plain(start_q, (B,), i32, dev, "start_q"),
@@ -330,7 +336,7 @@ def ska_softmax_attn_bwd(Q, K, V, O, dO, LSE, W, causal=False, eps=1.0, len_q=No
     dkp, dks = _heads(dK, kshape, dt, dev, "dK")
     dvp, dvs = _heads(dV, kshape, dt, dev, "dV")
     lib = _lib()
-    W, causal, i32, u8 = int(W), 1 if causal else 0, torch.int32, torch.uint8
+    W, causal, i32, u8 = _int32(W), 1 if causal else 0, torch.int32, torch.uint8
     ws, n, keep = _workspace(workspace, lib.ska_softmax_attn_workspace_bytes(1, B, Hq, Hk, Lq, Lk, d, W, causal, code), Q, dev)
     _done(lib.ska_softmax_attn_bwd(
         qp, qs, kp, ks, vp, vs, op, os, gp, gs, _plain(LSE, (B, Hq, Lq), torch.float32, dev, "LSE"), dqp, dqs, dkp, dks, dvp, dvs,

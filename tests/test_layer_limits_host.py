@@ -41,3 +41,15 @@ def test_the_stream_without_the_raw_function(monkeypatch):
     monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
     monkeypatch.setattr(torch.cuda, "current_stream", lambda dev: type("Stream", (), {"cuda_stream": 40 + dev}))
     assert layer._raw_stream(2) == 42
+
+
+def test_numbers_beyond_32_bits():
+    """A band as wide as can be said is everything, not what its lower 32 bits say; below 0 it is refused."""
+    need = lambda W, back=False: ska.ska_softmax_attn_workspace_bytes(back, 1, 4, 2, 1, 65536, 64, W)   # noqa: E731
+    assert need(1 << 20) > need(0) == 0
+    for W in (2 ** 31, 2 ** 32, 2 ** 32 + 5, sys.maxsize, 2 ** 80):
+        assert need(W) == need(1 << 20), W
+    for W in (-1, -2 ** 31 - 1, -2 ** 32, -2 ** 32 + 7):
+        assert need(W) == 0 and need(W, True) == 0 < need(0, True), W
+    far = ska.ska_rope_frequencies(64, scaling="yarn", factor=4.0, trained_length=2 ** 31 - 1)[0]
+    assert torch.equal(ska.ska_rope_frequencies(64, scaling="yarn", factor=4.0, trained_length=2 ** 32 + 4096)[0], far)
