@@ -202,12 +202,14 @@ def ska_layer_norm_workspace_bytes(N, D) -> int:
 def ska_layer_norm_bwd(dY, S, weight, stats, dS=None, want_weight=True, want_bias=True, dX=None, dweight=None, dbias=None,
                        workspace=None):
     """Gradient of ska_layer_norm_fwd: S, stats as it returned them, dS the gradient that reaches S on the residual's way.
-    Returns (dX, dweight, dbias): dX is that of X and of the residual; the others are None where they are not wanted."""
+    Returns (dX, dweight, dbias): dX is that of X and of the residual; the others are None where they are not wanted, and of the
+    weight's type, without a weight of that of the dweight or dbias given, else float32."""
     dev, shape, dt, D = _here(S, "S"), S.shape, S.dtype, _features(S, "S")
     gp, ldg = _rows(dY, shape, dt, dev, "dY")
     sp, lds = _rows(S, shape, dt, dev, "S")
     N = S.numel() // D
-    wt = torch.float32 if weight is None else weight.dtype
+    w = weight if weight is not None else dweight if dweight is not None else dbias
+    wt = torch.float32 if w is None else w.dtype
     wp = _plain(weight, (D,), wt, dev, "weight")
     rp, ldr = _rows(dS, shape, dt, dev, "dS") if dS is not None else (None, 0)
     if dX is None:
@@ -221,7 +223,7 @@ def ska_layer_norm_bwd(dY, S, weight, stats, dS=None, want_weight=True, want_bia
     lib = _lib()
     ws, n, keep = _workspace(workspace, lib.ska_layer_norm_workspace_bytes(N, D) if dwp or dbp else 0, S, dev)
     _done(lib.ska_layer_norm_bwd(gp, ldg, sp, lds, wp, _plain(stats, (2,) + shape[:-1], torch.float32, dev, "stats"), rp, ldr, xp, ldx,
-                                 dwp, dbp, N, D, _code(S), SKA_F32 if weight is None else _code(weight), ws, n, _raw_stream(dev)))
+                                 dwp, dbp, N, D, _code(S), SKA_F32 if w is None else _code(w), ws, n, _raw_stream(dev)))
     return dX, dweight, dbias
 
 
