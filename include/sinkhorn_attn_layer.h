@@ -110,7 +110,8 @@ int ska_rope_bwd(const void *dQr, const ska_strides *dqr_strides, void *dQ, cons
  *   Rows of inactive tokens and beyond the lengths may hold anything, and so may keys that no query, and queries that no key,
  *   of their item reaches by position (|p - j| <= W, j <= p if `causal`, within the lengths; inactive ones reach as well).  An
  *   active token that is reached must be finite to leave the item's others alone: products with a probability of 0 are formed.
- *   W >= 0 (W >= max(Lq, Lk) with starts of 0 is the dense problem); eps > 0 and finite.
+ *   W >= 0 (W >= max(Lq, Lk) with starts of 0 is the dense problem); eps > 0 and finite, and 1 / (eps sqrt d) a
+ *   normal fp32 number, log2(e) times which is finite (SKA_EUNSUPPORTED otherwise).  Scores are formed in fp32.
  *   d in {32, 64, 128}; 1 <= Lq, Lk <= 2^24; B * Hk <= 65535, Lq * (Hq / Hk) <= 2^27, and at most 2^24 - 8 blocks of
  *   128 rows: B * Hk times Lq * (Hq / Hk) rows, in the gradient also times Lk (SKA_EUNSUPPORTED otherwise).
  *   Pointers and strides in bytes: multiples of 16, tokens less than 128 MiB apart (SKA_EUNSUPPORTED otherwise).

@@ -161,6 +161,8 @@ SmArgs args_of(const SmProblem &p, float eps, float *lse, const int *start_q, co
     return a;
 }
 bool eps_ok(float eps) { return eps > 0.f && isfinite(eps); }
+// the scores' factor: at 0 a masked score would be 0 times -inf, at infinity an ordinary one 0 times that
+bool scale_ok(const SmArgs &a) { return isnormal(a.cs) && isnormal(a.c2); }
 
 }  // namespace
 
@@ -184,6 +186,7 @@ int ska_softmax_attn_fwd(const void *Q, const ska_strides *q_strides, const void
     int rc = check(p, false);
     if (rc != SKA_OK) return rc;
     SmArgs a = args_of(p, eps, LSE, start_q, len_q, len_k, mask_q, mask_k);
+    if (!scale_ok(a)) return SKA_EUNSUPPORTED;
     if ((rc = tensor_of(a.q, Q, q_strides, B, Hq, Lq, d, dtype, false)) != SKA_OK) return rc;
     if ((rc = tensor_of(a.k, K, k_strides, B, Hk, Lk, d, dtype, false)) != SKA_OK) return rc;
     if ((rc = tensor_of(a.v, V, v_strides, B, Hk, Lk, d, dtype, false)) != SKA_OK) return rc;
@@ -209,6 +212,7 @@ int ska_softmax_attn_bwd(const void *Q, const ska_strides *q_strides, const void
     int rc = check(p, true);
     if (rc != SKA_OK) return rc;
     SmArgs a = args_of(p, eps, const_cast<float *>(LSE), start_q, len_q, len_k, mask_q, mask_k);
+    if (!scale_ok(a)) return SKA_EUNSUPPORTED;
     if ((rc = tensor_of(a.q, Q, q_strides, B, Hq, Lq, d, dtype, false)) != SKA_OK) return rc;
     if ((rc = tensor_of(a.k, K, k_strides, B, Hk, Lk, d, dtype, false)) != SKA_OK) return rc;
     if ((rc = tensor_of(a.v, V, v_strides, B, Hk, Lk, d, dtype, false)) != SKA_OK) return rc;

@@ -53,3 +53,18 @@ def test_numbers_beyond_32_bits():
         assert need(W) == 0 and need(W, True) == 0 < need(0, True), W
     far = ska.ska_rope_frequencies(64, scaling="yarn", factor=4.0, trained_length=2 ** 31 - 1)[0]
     assert torch.equal(ska.ska_rope_frequencies(64, scaling="yarn", factor=4.0, trained_length=2 ** 32 + 4096)[0], far)
+
+
+def test_softmax_scale_is_a_number():
+    """1 / (eps sqrt d) of 0 or beyond fp32 made masked scores 0 times -inf.  (Without the workspace that both need: nothing is launched.)"""
+    lib, P = layer._lib(), 1 << 20
+
+    def calls(eps, d):
+        args = [1, 2, 2, 1, 65536, d, 1 << 20, 0, eps, binding.SKA_BF16, None, 0, None]
+        return [lib.ska_softmax_attn_fwd(P, None, P, None, P, None, P, None, P, *[None] * 5, *args),
+                lib.ska_softmax_attn_bwd(P, None, P, None, P, None, P, None, P, None, P, P, None, P, None, P, *[None] * 6, *args)]
+    for d in (32, 64, 128):
+        for eps in (3e38, 2e37, 1e-40, 1e-45):
+            assert calls(eps, d) == [binding.SKA_EUNSUPPORTED] * 2, (eps, d)
+        for eps in (1e36, 1.0, 1e-30, 1e-37):
+            assert calls(eps, d) == [binding.SKA_EWORKSPACE] * 2, (eps, d)
