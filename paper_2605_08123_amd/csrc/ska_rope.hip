@@ -75,7 +75,7 @@ template <typename T, int FORM, bool INTER> __global__ __launch_bounds__(NT) voi
     ask(h0);
     float c[PAIRS], s[PAIRS];
     if (turned) {
-        const int p = a.pos ? a.pos[(long)b * a.L + l] : (a.start ? a.start[b] : 0) + l;
+        const long p = a.pos ? a.pos[(long)b * a.L + l] : (long)(a.start ? a.start[b] : 0) + l;   // (may lie beyond 2^31)
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) {
             double turns = (double)p * a.freq[slot * PAIRS + i] * 0.15915494309189535;   // 1 / 2 pi

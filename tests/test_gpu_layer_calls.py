@@ -48,3 +48,16 @@ def test_gradient_of_a_bias_without_a_weight(rows, D, dtype):
     ref.check("dbias", db, want[2])
     _, dw, db = ska.ska_layer_norm_bwd(dy.cuda(), s.cuda(), None, st.cuda())
     assert dw.dtype == db.dtype == F32
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("start", [2 ** 31 - 1, 2 ** 31 - 3, -2 ** 31])
+def test_rope_starts_at_the_ends_of_32_bits(start, dtype):
+    """Tokens that follow a start near 2^31 stand beyond it."""
+    print("\n[case] rope start", start, dtype, flush=True)
+    B, H, L, d = 2, 2, 9, 64
+    q = torch.randn(B, H, L, d, generator=torch.Generator().manual_seed(3)).to(dtype)
+    freq, amp = ska.ska_rope_frequencies(d)
+    at = torch.tensor([start, 5], dtype=torch.int32)
+    got, _ = ska.ska_rope_fwd(q.cuda(), None, freq.cuda(), amp, start=at.cuda())
+    ref.check("Q", got, ref.rope(q, freq, amp, torch.arange(L) + at.long()[:, None], False))
