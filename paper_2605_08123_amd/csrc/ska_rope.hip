@@ -75,10 +75,11 @@ template <typename T, int FORM, bool INTER> __global__ __launch_bounds__(NT) voi
     ask(h0);
     float c[PAIRS], s[PAIRS];
     if (turned) {
-        const long p = a.pos ? a.pos[(long)b * a.L + l] : (long)(a.start ? a.start[b] : 0) + l;   // (may lie beyond 2^31)
+        // (the sum in 64 bits: it may lie beyond 2^31)
+        const double p = a.pos ? (double)a.pos[(long)b * a.L + l] : (double)(a.start ? a.start[b] : 0) + (double)l;
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) {
-            double turns = (double)p * a.freq[slot * PAIRS + i] * 0.15915494309189535;   // 1 / 2 pi
+            double turns = p * a.freq[slot * PAIRS + i] * 0.15915494309189535;   // 1 / 2 pi
             turns -= rint(turns);
             sincospif(2.f * (float)turns, &s[i], &c[i]);
             c[i] *= a.amplitude;
