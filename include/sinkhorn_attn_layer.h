@@ -6,7 +6,8 @@
  * Conventions are those of sinkhorn_attn.h: device pointers owned by the caller, work enqueued on `stream`, asynchronous,
  * nothing allocated, freed or kept; arguments are checked before anything is launched; SKA_OK or a negative ska_status.
  * All kernels of a call run on `stream` itself; the calls take no lock and may be captured into a graph (they record
- * kernels only).  Results are the same bits from call to call.  Sums, statistics and softmax run in fp32.
+ * kernels only).  Results are the same bits from call to call.  Sums, statistics and softmax run in fp32; what is rounded to fewer
+ * bits on the way is said below.
  */
 #ifndef SINKHORN_ATTN_LAYER_H
 #define SINKHORN_ATTN_LAYER_H
@@ -117,6 +118,11 @@ int ska_rope_bwd(const void *dQr, const ska_strides *dqr_strides, void *dQ, cons
  *   Pointers and strides in bytes: multiples of 16, tokens less than 128 MiB apart (SKA_EUNSUPPORTED otherwise).
  *   workspace: ska_softmax_attn_workspace_bytes(...) bytes (may be 0: then NULL is fine), 16-byte aligned; scratch.
  * Few queries on many keys (an answer's next token; W >= Lk for a whole cache) are split over the keys, and the parts joined.
+ * bf16: scores, maxima, sums and P are fp32; for the product with V, P is rounded to bf16 (2^-8 relative, half a step), or where
+ * the call has few rows taken as the sum of two bf16 parts (2^-16): always with Lq * (Hq / Hk) <= 32, else where that launches
+ * workgroups of one wavefront, which depends on B * Hk, Lq, Lk and W.  The same query can therefore differ by roundings of P and
+ * by the order of its sums between a batch and a call of its own, or between a token's call and the whole sequence's; the same
+ * call repeats its bits.
  */
 size_t ska_softmax_attn_workspace_bytes(int backward, int B, int Hq, int Hk, int Lq, int Lk, int d, int W, int causal,
                                         int dtype);
@@ -131,7 +137,8 @@ int ska_softmax_attn_fwd(const void *Q, const ska_strides *q_strides, const void
  *   delta_i = <dO_i, O_i>,  dS = P (dO V^T - delta),  dV = P^T dO,  dQ = dS K / (eps sqrt d),  dK = dS^T Q / (eps sqrt d),
  * dK and dV summed over the query heads that share a key head, in a fixed order.
  *   O, LSE: of the forward with the same arguments.  Results of keys without any query are zeros.
- * fp32 storage: products in fp32.  bf16: P and dS are rounded to bf16 for the second products (accumulated in fp32).
+ * fp32 storage: products in fp32.  bf16: P and dS are rounded to bf16 for the second products (accumulated in fp32), or taken in two
+ * parts where the call has few rows, as in the forward (queries for dQ, keys for dK and dV).
  */
 int ska_softmax_attn_bwd(const void *Q, const ska_strides *q_strides, const void *K, const ska_strides *k_strides,
                          const void *V, const ska_strides *v_strides, const void *O, const ska_strides *o_strides,

@@ -544,9 +544,12 @@ __global__ __launch_bounds__(64 * NW, 1) void sm_rows_kernel(const SmArgs a)
                     p[e] = fast_exp2(fmaf(s[n][e], c2, -mu));
                     sum += p[e];
                 }
-                // (few rows wait for the cache and not for products, so that their P, and in the backward P and dS, need not be
+                // bf16: few rows wait for the cache and not for products, so that their P, and in the backward P and dS, need not be
                 // rounded: four sequences of one token on caches of 65536, d = 64, 26.0 us against 25.6, and O as near as its type
-                // allows; backward of 4 heads, L = 256, d = 64, 18.2 against 17.3.  In sums over few keys a rounding is not averaged.)
+                // allows (1.7e-3 in the 2-norm); backward of 4 heads, L = 256, d = 64, 18.2 against 17.3.  In sums over few keys a
+                // rounding is not averaged.  Many rows pay for it with a fifth to a half of their time, so that theirs are rounded
+                // once (O 2.4e-3 off): 2 heads, L = 262144, d = 64, W = 256, forward 109 us, in two parts 155, backward 345, 460;
+                // 16 heads on 4, L = 4096, d = 128, causal, backward 312, 382; 8 heads, L = 4096, causal, d = 64, forward 44, 52.
                 sm_accum<T, D, NW == 1>(acc, vc[n], p, lane);
             }
         } else {
@@ -738,7 +741,7 @@ __global__ __launch_bounds__(64 * NW, 1) void sm_keys_kernel(const SmArgs a)
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) ds[e] *= p[e];
-            sm_accum<T, D, NW == 1>(dv, gc, p, lane);
+            sm_accum<T, D, NW == 1>(dv, gc, p, lane);   // (rounded as the other kernel's are)
             sm_accum<T, D, NW == 1>(dk, qc, ds, lane);
         }
         i0 = next;
