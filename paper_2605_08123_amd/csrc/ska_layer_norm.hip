@@ -6,7 +6,8 @@
 //             registers until the block's last row, go to memory once per block and are added up by a second launch
 // Both are bound by memory (MI355X, where a copy of 4 GB reaches 4.8 TB/s): forward with a residual, 262144 rows of 512, bf16,
 // 190 us, 5.7 TB/s; backward, 30011 rows of 1283, fp32, 88 + 5 us, 5.3 TB/s in the first launch; 16384 rows of 512, bf16,
-// 16.5 + 3.9 us, 4.1 TB/s; 48828 rows of 4096, bf16, 233 us in all, 5.1 TB/s.
+// 16.5 + 3.9 us, 4.1 TB/s; 48828 rows of 4096, bf16, 221 us in all, 5.4 TB/s.  Rows that leave the registers: 20000 of 20000, bf16,
+// forward 426 us, 3.8 TB/s; backward, whose two launches read S and dY three times, 951 us, 2.5 TB/s of what it cannot do without.
 // A row is dealt to TPR threads (a power of two) in NV pieces of 16 bytes, piece t + k TPR to thread t.  Rows of up to 256
 // pieces (backward: 128) are a wavefront's or several in one, so that their sums need no barrier; wider ones are a block's.
 #include <hip/hip_runtime.h>
@@ -227,8 +228,9 @@ template <typename T, typename TW> __global__ __launch_bounds__(NT_LOOP) void no
 template <typename T, typename TW, int NV> __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a)
 {
     constexpr int V = VEC<T>;
-    // Rows asked for one ahead in bf16 where the registers hold another (both launches for 262144 rows of 512 165 us, without 183;
-    // 110926 of 1803 377, 561; with NV = 4, 33333 of 6000, 540, 437).  fp32 rows are twice as long: 77942 of 1283 243, 236.
+    // Rows asked for one ahead in bf16 where the registers hold another (both launches for 110926 rows of 1803 368 us, without 403;
+    // 59808 of 3344 273, 299; with NV = 4, 33333 of 6000, 576, 329).  Rows of a wavefront, which no barrier holds up, are the other
+    // way about, by less: 262144 of 512 162, 152; 195312 of 1024 233, 232.  fp32 rows are twice as long: 77942 of 1283 238, 225.
     constexpr bool AHEAD = sizeof(T) == 2 && NV <= 2;
     __shared__ float red[2][NT / 64][2];
     extern __shared__ float sums[];   // with partial sums and rows of at most 64 threads: [wavefronts][tpr NV V]
