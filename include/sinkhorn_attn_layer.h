@@ -102,8 +102,8 @@ int ska_rope_bwd(const void *dQr, const ska_strides *dqr_strides, void *dQ, cons
  * pair where |p - j| <= W, j <= p if `causal`, i < len_q[b], j < len_k[b], and mask_q[b][i], mask_k[b][j] are not 0.
  *   S_ij = <Q_i, K_j> / (eps sqrt d),  LSE_i = log sum_j exp(S_ij),  O_i = sum_j exp(S_ij - LSE_i) V_j  over the pairs.
  * A query without any key has O_i = 0 and LSE_i = -inf, and its gradients are zeros.
- * NaN goes on: a query that meets one, in itself or in a key or value of its pairs, or a score of +inf, or that has keys but scores
- * of -inf alone, has NaN in O_i and LSE_i (O_i alone for a value's), and so have the gradients of its pairs.
+ * NaN goes on: a query that meets one, in itself or in a key of its pairs, or a score of +inf, or that has keys but scores of -inf
+ * alone, has NaN in O_i and LSE_i, and so have the gradients of its pairs.  One in a value is in O_i, and in dQ and dK of its pairs.
  *   Q, O [B,Hq,Lq,d]; K, V [B,Hk,Lk,d]; Hq a multiple of Hk: query head h reads key head h / (Hq / Hk).
  *   LSE [B,Hq,Lq] fp32.
  *   start_q, len_q, len_k: int32 device arrays [B] or NULL (0, Lq, Lk); starts are clamped to [0, 2^24], lengths to

@@ -162,3 +162,27 @@ def test_what_nothing_reaches_may_hold_anything(B, Hq, Hk, Lq, Lk, d, W, causal,
         ref.check(name, x, want[name])
     dead = ~ok.any(1)[:, None].expand(B, Hk, Lk).cuda()
     assert not grads[1][dead].any() and not grads[2][dead].any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,Hq,Hk,Lq,Lk,d,W,causal", SHAPES)
+def test_a_nan_in_a_value(B, Hq, Hk, Lq, Lk, d, W, causal, dtype):
+    """It is in O of the queries that read it and in the dQ and dK of their pairs; LSE and dV do not depend on it."""
+    print("\n[case]", B, Hq, Hk, Lq, Lk, d, W, causal, dtype, flush=True)
+    start = torch.tensor([Lk - Lq] * B, dtype=torch.int32)
+    kw = dict(causal=causal, start_q=start.cuda())
+    ok = ref.pairs(B, Lq, Lk, W, causal, start=start)[0]
+    q, k, v, do = make(B, Hq, Hk, Lq, Lk, d, dtype, seed=3)
+    clean = both(q, k, v, do, W, **kw)
+    at = Lk // 2 if Lq > 17 else Lk - Lq
+    v[0, 0, at, 5] = math.nan
+    O, LSE, dQ, dK, dV = both(q, k, v, do, W, **kw)
+    hit = ok[:, at]
+    reached = ok[hit].any(0)
+    heads = slice(0, Hq // Hk)
+    assert torch.isnan(O[0, heads][:, hit.cuda(), 5]).all() and torch.isnan(dQ[0, heads][:, hit.cuda()]).all()
+    assert torch.isnan(dK[0, :1][:, reached.cuda()]).all()
+    assert torch.equal(LSE, clean[1]) and torch.equal(dV, clean[4])
+    assert torch.equal(O[0, heads][..., :5], clean[0][0, heads][..., :5])   # (another feature is another sum)
+    for t, c, n in zip((O, dQ, dK), (clean[0], clean[2], clean[3]), (heads.stop, heads.stop, 1)):
+        assert torch.equal(t[0, n:], c[0, n:]) and torch.equal(t[1:], c[1:])
