@@ -1,7 +1,8 @@
 """MI355X-native banded Sinkhorn attention (forward + exact surrogate backward).
 
 `binding` is the thin ctypes layer over the C ABI of include/sinkhorn_attn.h, `layer` over
-that of include/sinkhorn_attn_layer.h (layer norm, rotary positions, softmax attention on the band);
+that of include/sinkhorn_attn_layer.h (layer norm, rotary positions, softmax attention on the band),
+`cache` over that of include/sinkhorn_attn_cache.h (caches in 8 bits, attention on them and on shared prefixes);
 `workloads` holds the seeded synthetic inputs; `build` compiles the library.
 """
 from .binding import (SinkhornAttnError, sinkhorn_attn_base_vjp, sinkhorn_attn_bwd,
@@ -16,3 +17,5 @@ from .binding import (SinkhornAttnError, sinkhorn_attn_base_vjp, sinkhorn_attn_b
 from .layer import (ska_layer_norm_bwd, ska_layer_norm_fwd, ska_layer_norm_workspace_bytes, ska_rope_bwd,  # noqa: F401
                     ska_rope_frequencies, ska_rope_fwd, ska_softmax_attn_bwd, ska_softmax_attn_fwd,
                     ska_softmax_attn_workspace_bytes)
+from .cache import (KVCache, ska_cache_attn_fwd, ska_cache_attn_workspace_bytes, ska_cache_empty, ska_cache_read,  # noqa: F401
+                    ska_cache_write, ska_prefix_attn_fwd, ska_prefix_attn_workspace_bytes)

@@ -26,7 +26,11 @@ UNITS = [("sinkhorn_attn", "sinkhorn_attn.hip", [])] + [
     for name, t in (("bf16", "__bf16"), ("f32", "float")) for d in (64, 32, 128)] + [
     ("layer_norm", "ska_layer_norm.hip", []), ("rope", "ska_rope.hip", []), ("softmax", "ska_softmax.hip", [])] + [
     (f"softmax_{name}_{d}", "ska_softmax_launch.hip", [f"-DSKA_T={t}", f"-DSKA_D={d}", f"-DSKA_NAME=ska_launch_softmax_{name}_{d}"])
-    for name, t in (("bf16", "__bf16"), ("f32", "float")) for d in (64, 32, 128)]
+    for name, t in (("bf16", "__bf16"), ("f32", "float")) for d in (64, 32, 128)] + [("cache", "ska_cache.hip", [])] + [
+    (f"cache_{store}_{name}_{d}", "ska_cache_launch.hip", [f"-DSKA_S={s}", f"-DSKA_T={t}", f"-DSKA_D={d}", f"-DSKA_NAME=ska_launch_cache_{store}_{name}_{d}"])
+    for store, s, name, t in (("f32", "float", "f32", "float"), ("bf16", "__bf16", "bf16", "__bf16"), ("e4m3", "E4M3", "f32", "float"),
+                              ("e4m3", "E4M3", "bf16", "__bf16"), ("int8", "INT8", "f32", "float"), ("int8", "INT8", "bf16", "__bf16"))
+    for d in (64, 32, 128)]
 
 
 def build_library(verbose: bool = False) -> str:

@@ -1,0 +1,411 @@
+// Caches in 8 bits (written, read back) and softmax attention on caches and shared prefixes: the host side of the attention
+// (sinkhorn_attn_cache.h; kernels in ska_cache.h), and the kernels that write and read.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "sinkhorn_attn_cache.h"
+#include "ska_cache_launch.h"
+
+namespace {
+
+bool scaled(int store) { return store == SKA_E4M3 || store == SKA_INT8; }
+int bytes_of(int type) { return type == SKA_F32 ? 4 : type == SKA_BF16 ? 2 : 1; }
+
+// A tensor's pointer and strides; SKA_EINVAL where they cannot be strides, SKA_EUNSUPPORTED where the kernels cannot use them.
+int tensor_of(SmTensor &t, const void *p, const ska_strides *s, int B, int H, long L, int d, int type, int align, bool out)
+{
+    if (!p) return SKA_EINVAL;
+    t.p = p;
+    if (s) {
+        t.b = (long)s->b; t.h = (long)s->h; t.l = (long)s->l;
+        if (t.b < 0 || t.h < 0 || t.l < 0) return SKA_EINVAL;
+        if (out && ((B > 1 && !t.b) || (H > 1 && !t.h) || (L > 1 && !t.l))) return SKA_EINVAL;
+        if (B == 1) t.b = 0;   // (never stepped over, whatever it says)
+        if (H == 1) t.h = 0;
+        if (L == 1) t.l = 0;
+    } else {
+        t.l = d; t.h = L * d; t.b = t.h * H;
+    }
+    const long e = bytes_of(type);
+    if (t.l * e >= 1L << 27) return SKA_EUNSUPPORTED;   // (32 tokens lie within 32 bits)
+    const unsigned long off = (unsigned long)reinterpret_cast<uintptr_t>(p) | (unsigned long)((t.b | t.h | t.l) * e);
+    return off & (unsigned long)(align - 1) ? SKA_EUNSUPPORTED : SKA_OK;
+}
+struct Scales { const float *p; long b, h; };
+int scales_of(Scales &t, const float *p, const ska_scale_strides *s, int B, int H, long L, bool out)
+{
+    if (!p) return SKA_EINVAL;
+    t = {p, s ? (long)s->b : L * H, s ? (long)s->h : L};
+    if (t.b < 0 || t.h < 0 || (out && ((B > 1 && !t.b) || (H > 1 && !t.h)))) return SKA_EINVAL;
+    if (B == 1) t.b = 0;
+    if (H == 1) t.h = 0;
+    return reinterpret_cast<uintptr_t>(p) & 3 ? SKA_EUNSUPPORTED : SKA_OK;
+}
+
+// ------------------------------------------------------------------ writing and reading
+// A thread takes 8 features of a key's row and of the value's: D / 8 threads a row, one exchange between them for its largest
+// feature.  Memory bounds both; what a row reads and writes is asked for before anything waits.
+struct MoveArgs {
+    SmTensor k, v, kc, vc;
+    Scales ks, vs;
+    const int *start, *len;
+    int B, Hk, L, Lc;
+    SmDiv by_hk;
+};
+constexpr int MOVE_ROWS = 4;   // of a thread
+
+template <typename T> __device__ __forceinline__ void load8(float (&f)[8], const T *p)
+{
+    load4<T>(p, reinterpret_cast<float(&)[4]>(f[0]));
+    load4<T>(p + 4, reinterpret_cast<float(&)[4]>(f[4]));
+}
+template <> __device__ __forceinline__ void load8<__bf16>(float (&f)[8], const __bf16 *p)
+{
+    const bf16x8 x = *reinterpret_cast<const bf16x8 *>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (float)x[i];
+}
+
+// Scale of a row whose largest feature has the bits `a` (as an unsigned number, so that infinities and NaN are the largest)
+template <typename S> __device__ __forceinline__ float move_scale(unsigned a)
+{
+    if (a >= 0x7f800000u) return NAN;
+    if constexpr (std::is_same<S, E4M3>::value)
+        // a = 1.m 2^e: 448 = 1.75 2^8, so that the power is e - 8, and one more where 1.m is more than 1.75
+        return __uint_as_float((unsigned)max((int)(a >> 23) - 8 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0), 1) << 23);
+    else return fminf(fmaxf(__uint_as_float(a) / 127.f, 0x1p-126f), 0x1.020406p+121f);   // (127 times the next number is infinite)
+}
+// 8 features as codes
+template <typename S> __device__ __forceinline__ uint2 move_codes(const float (&f)[8], float scale)
+{
+    unsigned w[2] = {0, 0};
+    if (!(scale > 0.f)) return make_uint2(0, 0);   // (NaN)
+    if constexpr (std::is_same<S, E4M3>::value) {
+        const float inv = __uint_as_float((254u << 23) - __float_as_uint(scale));   // a power of two: exact
+        const float most = scale == 0x1p120f ? 240.f : 448.f;                       // (256 2^120 would be infinite)
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(f[i] * inv, -most), most);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int x = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i], y[4 * i + 1], 0, false);
+            w[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], x, true);
+        }
+    } else {
+        const float inv = 1.f / scale, half = 0.5f * scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // the nearest integer to a rounded quotient, put right by the remainder, which is exact near a border
+            float n = rintf(f[i] * inv);
+            const float rest = fmaf(-n, scale, f[i]);
+            const bool odd = (int)n & 1;
+            if (rest > half || (rest == half && odd)) n += 1.f;
+            else if (rest < -half || (rest == -half && odd)) n -= 1.f;
+            w[i >> 2] |= ((unsigned)(int)fminf(fmaxf(n, -127.f), 127.f) & 0xffu) << (8 * (i & 3));
+        }
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+template <typename S, typename T, int D> __global__ __launch_bounds__(NTHREADS) void cache_write_kernel(const MoveArgs a)
+{
+    constexpr int TPR = D / 8, RPB = NTHREADS / TPR;   // threads of a row, rows of a block at a time
+    const int n = blockIdx.y, b = a.by_hk(n), h = n - b * a.Hk, c = (threadIdx.x % TPR) * 8;
+    const int len = sm_len(a.len, b, a.L);
+    const long start = a.start ? a.start[b] : 0;
+    const int l0 = blockIdx.x * (RPB * MOVE_ROWS) + threadIdx.x / TPR;
+    float f[MOVE_ROWS][2][8];
+    bool on[MOVE_ROWS];
+#pragma unroll
+    for (int i = 0; i < MOVE_ROWS; ++i) {
+        const int l = l0 + i * RPB;
+        on[i] = l < len && start + l >= 0 && start + l < a.Lc;
+        if (on[i]) {
+            load8<T>(f[i][0], reinterpret_cast<const T *>(a.k.p) + b * a.k.b + h * a.k.h + l * a.k.l + c);
+            load8<T>(f[i][1], reinterpret_cast<const T *>(a.v.p) + b * a.v.b + h * a.v.h + l * a.v.l + c);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MOVE_ROWS; ++i) {
+        if (!on[i]) continue;   // (all threads of a row alike)
+        const long at = start + l0 + i * RPB;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            unsigned m = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(f[i][w][k]) & 0x7fffffffu);
+#pragma unroll
+            for (int d = 1; d < TPR; d <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, d));
+            const float scale = move_scale<S>(m);
+            const SmTensor &t = w ? a.vc : a.kc;
+            const Scales &s = w ? a.vs : a.ks;
+            *reinterpret_cast<uint2 *>(reinterpret_cast<unsigned char *>(const_cast<void *>(t.p)) + b * t.b + h * t.h + at * t.l + c) = move_codes<S>(f[i][w], scale);
+            if (c == 0) const_cast<float *>(s.p)[b * s.b + h * s.h + at] = scale;
+        }
+    }
+}
+
+template <typename S, typename T, int D> __global__ __launch_bounds__(NTHREADS) void cache_read_kernel(const MoveArgs a)
+{
+    constexpr int TPR = D / 8, RPB = NTHREADS / TPR;
+    const int n = blockIdx.y, b = a.by_hk(n), h = n - b * a.Hk, c = (threadIdx.x % TPR) * 8;
+    const int len = sm_len(a.len, b, a.Lc);
+    const long start = a.start ? a.start[b] : 0;
+    const int l0 = blockIdx.x * (RPB * MOVE_ROWS) + threadIdx.x / TPR;
+    uint2 w[MOVE_ROWS][2];
+    float s[MOVE_ROWS][2];
+#pragma unroll
+    for (int i = 0; i < MOVE_ROWS; ++i) {
+        const int l = l0 + i * RPB;
+        const long at = start + l;
+        w[i][0] = w[i][1] = make_uint2(0, 0);
+        s[i][0] = s[i][1] = 0.f;
+        if (l < a.L && at >= 0 && at < len) {
+            w[i][0] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const unsigned char *>(a.kc.p) + b * a.kc.b + h * a.kc.h + at * a.kc.l + c);
+            w[i][1] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const unsigned char *>(a.vc.p) + b * a.vc.b + h * a.vc.h + at * a.vc.l + c);
+            s[i][0] = a.ks.p[b * a.ks.b + h * a.ks.h + at];
+            s[i][1] = a.vs.p[b * a.vs.b + h * a.vs.h + at];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MOVE_ROWS; ++i) {
+        const int l = l0 + i * RPB;
+        if (l >= a.L) continue;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const SmTensor &t = k ? a.v : a.k;
+            T *to = reinterpret_cast<T *>(const_cast<void *>(t.p)) + b * t.b + h * t.h + l * t.l + c;
+            const bf16x8 x = ca_codes<S>(w[i][k].x, w[i][k].y);
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = (float)x[j] * s[i][k];
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x8 *>(to) = pack8(y);
+            else {
+                store4<T>(to, y[0], y[1], y[2], y[3]);
+                store4<T>(to + 4, y[4], y[5], y[6], y[7]);
+            }
+        }
+    }
+}
+
+template <typename S, typename T, int D> int move(bool write, const MoveArgs &a, hipStream_t st)
+{
+    const long per = NTHREADS / (D / 8) * MOVE_ROWS;
+    const dim3 grid((unsigned)((a.L + per - 1) / per), (unsigned)(a.B * a.Hk));
+    if (write) hipLaunchKernelGGL((cache_write_kernel<S, T, D>), grid, dim3(NTHREADS), 0, st, a);
+    else hipLaunchKernelGGL((cache_read_kernel<S, T, D>), grid, dim3(NTHREADS), 0, st, a);
+    return hipGetLastError() == hipSuccess ? SKA_OK : SKA_EHIP;
+}
+template <typename S, typename T> int move(int d, bool write, const MoveArgs &a, hipStream_t st)
+{
+    return d == 32 ? move<S, T, 32>(write, a, st) : d == 64 ? move<S, T, 64>(write, a, st) : move<S, T, 128>(write, a, st);
+}
+int move(bool write, const void *K, const ska_strides *k_strides, const void *V, const ska_strides *v_strides, const void *Kc,
+         const ska_strides *kc_strides, const float *Ks, const ska_scale_strides *ks_strides, const void *Vc, const ska_strides *vc_strides,
+         const float *Vs, const ska_scale_strides *vs_strides, const int *start, const int *len, int B, int Hk, int L, int Lc, int d, int dtype,
+         int store, void *stream)
+{
+    if (B < 1 || Hk < 1 || L < 0 || Lc < 1) return SKA_EINVAL;
+    if ((d != 32 && d != 64 && d != 128) || (dtype != SKA_F32 && dtype != SKA_BF16) || !scaled(store)) return SKA_EUNSUPPORTED;
+    if (L > 1 << 24 || Lc > 1 << 24 || (long)B * Hk > 65535) return SKA_EUNSUPPORTED;
+    MoveArgs a{};
+    int rc;
+    if ((rc = tensor_of(a.kc, Kc, kc_strides, B, Hk, Lc, d, store, 8, write)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.vc, Vc, vc_strides, B, Hk, Lc, d, store, 8, write)) != SKA_OK) return rc;
+    if ((rc = scales_of(a.ks, Ks, ks_strides, B, Hk, Lc, write)) != SKA_OK) return rc;
+    if ((rc = scales_of(a.vs, Vs, vs_strides, B, Hk, Lc, write)) != SKA_OK) return rc;
+    if (L == 0) return SKA_OK;
+    if ((rc = tensor_of(a.k, K, k_strides, B, Hk, L, d, dtype, 16, !write)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.v, V, v_strides, B, Hk, L, d, dtype, 16, !write)) != SKA_OK) return rc;
+    a.start = start; a.len = len;
+    a.B = B; a.Hk = Hk; a.L = L; a.Lc = Lc;
+    a.by_hk = SmDiv::by(Hk);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (store == SKA_E4M3) return dtype == SKA_F32 ? move<E4M3, float>(d, write, a, st) : move<E4M3, __bf16>(d, write, a, st);
+    return dtype == SKA_F32 ? move<INT8, float>(d, write, a, st) : move<INT8, __bf16>(d, write, a, st);
+}
+
+// ------------------------------------------------------------------ attention
+struct CaProblem {
+    int B, Hq, Hk, Lq, Lp, Lk, d, W, causal, dtype, store;   // Lp 0: no prefix
+    int G() const { return Hq / Hk; }
+    long R() const { return (long)Lq * G(); }
+    long rows() const { return (long)B * Hk * R(); }
+};
+int check(const CaProblem &p, bool prefix)
+{
+    if (p.B < 1 || p.Hq < 1 || p.Hk < 1 || p.Lq < 1 || p.Lk < 1 || p.W < 0 || p.Hq % p.Hk || (prefix && p.Lp < 1)) return SKA_EINVAL;
+    if (p.d != 32 && p.d != 64 && p.d != 128) return SKA_EUNSUPPORTED;
+    if (p.dtype != SKA_F32 && p.dtype != SKA_BF16) return SKA_EUNSUPPORTED;
+    if (!scaled(p.store) && !(prefix && p.store == p.dtype)) return SKA_EUNSUPPORTED;
+    if (p.Lq > 1 << 24 || p.Lk > 1 << 24 || p.Lp > 1 << 24 || (long)p.B * p.Hk > 65535 || p.R() > 1 << 27) return SKA_EUNSUPPORTED;
+    if (prefix && p.R() * p.B > 1 << 27) return SKA_EUNSUPPORTED;
+    if ((p.R() + 127) / 128 * p.B * p.Hk > (1 << 24) - 8) return SKA_EUNSUPPORTED;   // (fewer than 2^32 threads, as in softmax_attn)
+    return SKA_OK;
+}
+
+// How one side is launched: blocks of 16 rows of a wavefront, wavefronts that share rows, blocks, parts
+struct CaGrid { int kw; long blocks; int parts; };
+int ca_rows_of(const CaProblem &p)
+{
+    const long rows = p.Lp ? p.R() * p.B : p.R();
+    const int most = ca_most(p.dtype == SKA_F32, p.d);
+    return rows <= 16 ? 1 : rows <= 32 ? 2 : most;
+}
+CaGrid ca_grid(const CaProblem &p, int nq, bool prefix)
+{
+    const long rows = prefix ? p.R() * p.B : p.R(), problems = prefix ? p.Hk : (long)p.B * p.Hk, L = prefix ? p.Lp : p.Lk;
+    const long wave_rows = 16 * nq, need = (rows + wave_rows - 1) / wave_rows;
+    CaGrid g;
+    g.kw = need >= 3 ? 1 : need == 2 ? 2 : 4;
+    g.blocks = (need + 4 / g.kw - 1) / (4 / g.kw);
+    const long reach = std::min(L, prefix ? (long)p.W : std::min(wave_rows * (4 / g.kw) / p.G() + 1, (long)p.Lq) + (p.causal ? 1L : 2L) * p.W);
+    const long tile = p.store == SKA_F32 ? 16 : 32, tiles = (reach + tile - 1) / tile;
+    const long room = nq == 1 ? 1024 : 512;
+    g.parts = (int)std::max(1L, std::min({room / (g.blocks * problems), tiles / (4 * g.kw), 256L}));
+    return g;
+}
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+int ca_parts(const CaProblem &p, int nq) { return ca_grid(p, nq, false).parts + (p.Lp ? ca_grid(p, nq, true).parts : 0); }
+size_t ws_lse(const CaProblem &p, int parts) { return up256((size_t)parts * p.rows() * sizeof(float)); }
+size_t ws_bytes(const CaProblem &p)
+{
+    const int parts = ca_parts(p, ca_rows_of(p));
+    return parts > 1 ? ws_lse(p, parts) + (size_t)parts * p.rows() * p.d * sizeof(float) : 0;
+}
+
+struct CaKept {   // keys and values of one side as a caller gives them
+    const void *K; const ska_strides *ks; const float *Ks; const ska_scale_strides *kss;
+    const void *V; const ska_strides *vs; const float *Vs; const ska_scale_strides *vss;
+};
+int side_of(CaSide &s, const CaKept &c, int B, int Hk, int L, int d, int store)
+{
+    int rc;
+    if ((rc = tensor_of(s.k, c.K, c.ks, B, Hk, L, d, store, 16, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(s.v, c.V, c.vs, B, Hk, L, d, store, 16, false)) != SKA_OK) return rc;
+    s.L = L;
+    if (!scaled(store)) return c.Ks || c.Vs ? SKA_EINVAL : SKA_OK;
+    Scales k, v;
+    if ((rc = scales_of(k, c.Ks, c.kss, B, Hk, L, false)) != SKA_OK) return rc;
+    if ((rc = scales_of(v, c.Vs, c.vss, B, Hk, L, false)) != SKA_OK) return rc;
+    s.ks = k.p; s.ks_b = k.b; s.ks_h = k.h;
+    s.vs = v.p; s.vs_b = v.b; s.vs_h = v.h;
+    return SKA_OK;
+}
+void place(CaSide &s, const CaProblem &p, const CaGrid &g, bool prefix)
+{
+    s.rows = (int)(prefix ? p.R() * p.B : p.R());
+    s.problems = prefix ? p.Hk : p.B * p.Hk;
+    s.ks_waves = g.kw;
+    s.blocks = (int)g.blocks;
+    s.parts = g.parts;
+    s.wgs = (int)(g.blocks * g.parts * s.problems);
+    s.by_problems = SmDiv::by(s.problems);
+    s.by_blocks = SmDiv::by(s.blocks);
+    s.by_span = SmDiv::by(s.parts * s.ks_waves);
+}
+typedef int (*Launch)(int, const void *, hipStream_t);
+#define BY_D(NAME) {NAME##_32, NAME##_64, NAME##_128}
+constexpr Launch LAUNCH[6][3] = {BY_D(ska_launch_cache_f32_f32), BY_D(ska_launch_cache_bf16_bf16), BY_D(ska_launch_cache_e4m3_f32),
+                                 BY_D(ska_launch_cache_e4m3_bf16), BY_D(ska_launch_cache_int8_f32), BY_D(ska_launch_cache_int8_bf16)};
+
+int attn(const CaProblem &p, const void *Q, const ska_strides *q_strides, const CaKept *prefix, const CaKept &own, void *O, const ska_strides *o_strides,
+         float *LSE, const int *len_p, const int *start_q, const int *len_q, const int *len_k, const unsigned char *mask_q,
+         const unsigned char *mask_k, const unsigned char *mask_p, float eps, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!LSE || !(eps > 0.f && isfinite(eps))) return SKA_EINVAL;
+    int rc = check(p, prefix != nullptr);
+    if (rc != SKA_OK) return rc;
+    CaArgs a{};
+    const float cs = 1.f / (eps * sqrtf((float)p.d));
+    a.c2 = cs * LOG2E;
+    if (!isnormal(cs) || !isnormal(a.c2)) return SKA_EUNSUPPORTED;   // (at 0 a masked score would be 0 times -inf)
+    if ((rc = tensor_of(a.q, Q, q_strides, p.B, p.Hq, p.Lq, p.d, p.dtype, 16, false)) != SKA_OK) return rc;
+    if ((rc = tensor_of(a.o, O, o_strides, p.B, p.Hq, p.Lq, p.d, p.dtype, 16, true)) != SKA_OK) return rc;
+    if ((rc = side_of(a.side[0], own, p.B, p.Hk, p.Lk, p.d, p.store)) != SKA_OK) return rc;
+    if (prefix && (rc = side_of(a.side[1], *prefix, 1, p.Hk, p.Lp, p.d, p.store)) != SKA_OK) return rc;
+    const int nq = ca_rows_of(p);
+    a.parts = ca_parts(p, nq);
+    const size_t need = ws_bytes(p);
+    if (need && (!workspace || workspace_bytes < need)) return SKA_EWORKSPACE;
+    if (reinterpret_cast<uintptr_t>(workspace) & 15) return SKA_EINVAL;
+    a.part_lse = static_cast<float *>(workspace);
+    a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + ws_lse(p, a.parts));
+    a.lse = LSE;
+    a.start = start_q; a.len_q = len_q; a.mask_q = mask_q;
+    a.side[0].len = len_k; a.side[0].mask = mask_k;
+    a.side[1].len = len_p; a.side[1].mask = mask_p;
+    a.B = p.B; a.Hk = p.Hk; a.G = p.G(); a.Lq = p.Lq; a.causal = p.causal;
+    a.W = std::min(p.W, 1 << 27);   // (positions are below 2^26: this reaches everything, and sums with it stay in 32 bits)
+    a.by_g = SmDiv::by(a.G);
+    a.by_hk = SmDiv::by(a.Hk);
+    a.by_r = SmDiv::by((unsigned)p.R());
+    place(a.side[0], p, ca_grid(p, nq, false), false);
+    if (prefix) place(a.side[1], p, ca_grid(p, nq, true), true);
+    const int at = p.store == SKA_F32 ? 0 : p.store == SKA_BF16 ? 1 : (p.store == SKA_E4M3 ? 2 : 4) + (p.dtype == SKA_BF16);
+    return LAUNCH[at][p.d == 32 ? 0 : p.d == 64 ? 1 : 2](nq, &a, static_cast<hipStream_t>(stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+int ska_cache_write(const void *K, const ska_strides *k_strides, const void *V, const ska_strides *v_strides, void *Kc, const ska_strides *kc_strides,
+                    float *Ks, const ska_scale_strides *ks_strides, void *Vc, const ska_strides *vc_strides, float *Vs,
+                    const ska_scale_strides *vs_strides, const int *start, const int *len_new, int B, int Hk, int L, int Lc, int d, int dtype, int store,
+                    void *stream)
+{
+    return move(true, K, k_strides, V, v_strides, Kc, kc_strides, Ks, ks_strides, Vc, vc_strides, Vs, vs_strides, start, len_new, B, Hk, L, Lc, d, dtype,
+                store, stream);
+}
+
+int ska_cache_read(const void *Kc, const ska_strides *kc_strides, const float *Ks, const ska_scale_strides *ks_strides, const void *Vc,
+                   const ska_strides *vc_strides, const float *Vs, const ska_scale_strides *vs_strides, void *K, const ska_strides *k_strides, void *V,
+                   const ska_strides *v_strides, const int *start, const int *len_k, int B, int Hk, int L, int Lc, int d, int dtype, int store, void *stream)
+{
+    return move(false, K, k_strides, V, v_strides, Kc, kc_strides, Ks, ks_strides, Vc, vc_strides, Vs, vs_strides, start, len_k, B, Hk, L, Lc, d, dtype,
+                store, stream);
+}
+
+size_t ska_cache_attn_workspace_bytes(int B, int Hq, int Hk, int Lq, int Lc, int d, int W, int causal, int dtype, int store)
+{
+    const CaProblem p{B, Hq, Hk, Lq, 0, Lc, d, W, causal, dtype, store};
+    return check(p, false) == SKA_OK ? ws_bytes(p) : 0;
+}
+
+int ska_cache_attn_fwd(const void *Q, const ska_strides *q_strides, const void *Kc, const ska_strides *kc_strides, const float *Ks,
+                       const ska_scale_strides *ks_strides, const void *Vc, const ska_strides *vc_strides, const float *Vs,
+                       const ska_scale_strides *vs_strides, void *O, const ska_strides *o_strides, float *LSE, const int *start_q, const int *len_q,
+                       const int *len_k, const unsigned char *mask_q, const unsigned char *mask_k, int B, int Hq, int Hk, int Lq, int Lc, int d, int W,
+                       int causal, float eps, int dtype, int store, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const CaProblem p{B, Hq, Hk, Lq, 0, Lc, d, W, causal, dtype, store};
+    return attn(p, Q, q_strides, nullptr, {Kc, kc_strides, Ks, ks_strides, Vc, vc_strides, Vs, vs_strides}, O, o_strides, LSE, nullptr, start_q, len_q,
+                len_k, mask_q, mask_k, nullptr, eps, workspace, workspace_bytes, stream);
+}
+
+size_t ska_prefix_attn_workspace_bytes(int B, int Hq, int Hk, int Lq, int Lp, int Lk, int d, int W, int causal, int dtype, int store)
+{
+    const CaProblem p{B, Hq, Hk, Lq, Lp, Lk, d, W, causal, dtype, store};
+    return check(p, true) == SKA_OK ? ws_bytes(p) : 0;
+}
+
+int ska_prefix_attn_fwd(const void *Q, const ska_strides *q_strides, const void *Kp, const ska_strides *kp_strides, const float *Kps,
+                        const ska_scale_strides *kps_strides, const void *Vp, const ska_strides *vp_strides, const float *Vps,
+                        const ska_scale_strides *vps_strides, const void *K, const ska_strides *k_strides, const float *Ks,
+                        const ska_scale_strides *ks_strides, const void *V, const ska_strides *v_strides, const float *Vs,
+                        const ska_scale_strides *vs_strides, void *O, const ska_strides *o_strides, float *LSE, const int *len_p, const int *start_q,
+                        const int *len_q, const int *len_k, const unsigned char *mask_q, const unsigned char *mask_k, const unsigned char *mask_p, int B,
+                        int Hq, int Hk, int Lq, int Lp, int Lk, int d, int W, int causal, float eps, int dtype, int store, void *workspace,
+                        size_t workspace_bytes, void *stream)
+{
+    const CaProblem p{B, Hq, Hk, Lq, Lp, Lk, d, W, causal, dtype, store};
+    const CaKept prefix{Kp, kp_strides, Kps, kps_strides, Vp, vp_strides, Vps, vps_strides};
+    return attn(p, Q, q_strides, &prefix, {K, k_strides, Ks, ks_strides, V, v_strides, Vs, vs_strides}, O, o_strides, LSE, len_p, start_q, len_q, len_k,
+                mask_q, mask_k, mask_p, eps, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

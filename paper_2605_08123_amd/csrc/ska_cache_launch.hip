@@ -1,0 +1,26 @@
+// The attention kernels' instances for one storage type, query type and head dimension (SKA_S, SKA_T, SKA_D; the function's name: SKA_NAME).
+#include "sinkhorn_attn_cache.h"
+#include "ska_cache_launch.h"
+
+namespace {
+template <typename S, typename T, int D> int launch(int nq, const CaArgs &a, hipStream_t st)
+{
+    constexpr int MOST = ca_most(sizeof(T) == 4, D);
+    const dim3 grid((unsigned)(a.side[0].wgs + a.side[1].wgs));
+    if (nq == 1) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 1>), grid, dim3(256), 0, st, a);
+    else if (nq == 2) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 2>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((ca_attn_kernel<S, T, D, MOST>), grid, dim3(256), 0, st, a);
+    if (hipGetLastError() != hipSuccess) return SKA_EHIP;
+    if (a.parts > 1) {
+        const int threads = D / 4;
+        int slices = 1;   // as many as there are parts, or threads
+        while (slices * 2 <= a.parts && slices * 2 * threads <= NTHREADS) slices *= 2;
+        const long per = NTHREADS / threads / slices, rows = (long)a.B * a.Hk * a.Lq * a.G;
+        hipLaunchKernelGGL((ca_join_kernel<T, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(NTHREADS), 0, st, a, slices);
+        if (hipGetLastError() != hipSuccess) return SKA_EHIP;
+    }
+    return SKA_OK;
+}
+}  // namespace
+
+SKA_DECLARE_CACHE(SKA_NAME) { return launch<SKA_S, SKA_T, SKA_D>(nq, *static_cast<const CaArgs *>(args), st); }
