@@ -21,6 +21,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // Keys and values of one side: the items' own, or the prefix.
 struct CaSide {
@@ -32,10 +35,14 @@ struct CaSide {
     int L;
     int rows;                         // query rows of a problem: Lq G, prefix: B Lq G
     int problems;                     // B Hk, prefix: Hk
-    int ks_waves;                     // wavefronts of a workgroup that share rows and split the keys (1, 2, 4)
-    int blocks, parts, wgs;           // blocks of rows, parts of a walk, workgroups: blocks * parts * problems
-    SmDiv by_problems, by_blocks, by_span;   // problems, blocks, parts * ks_waves
+    int blocks, parts;                // blocks of a workgroup's rows in a problem, parts of a walk
+    int units, wgs;                   // blocks * parts * problems; the same as a multiple of 8
+    int order;                        // CaOrder
+    SmDiv by_problems, by_blocks, by_parts, by_span;   // problems, blocks, parts, parts * wavefronts of a workgroup
 };
+// Order of the workgroups.  Blocks of the same keys next to each other and a contiguous piece of them per XCD (workgroups go to the XCDs
+// in turn): few blocks, a prefix, a band.  Many blocks that walk over most of the keys: those with the longest walks first, problems fastest.
+enum CaOrder { CA_NEIGHBOURS, CA_LAST_FIRST };
 struct CaArgs {
     SmTensor q, o;
     float *lse;
@@ -84,43 +91,32 @@ template <typename S, int D> struct CaTile {
     using ST = CaStore<S>;
     static constexpr int NT = ST::NT, KB = D * ST::BYTES / 4, KP = KB < 16 ? KB : 16, VB = D / 16 * ST::BYTES;   // bytes per lane of a key, of a load, of a value
     unsigned k[NT][KB / 4], v[NT][4][VB < 4 ? 1 : VB / 4];
-    float ks[NT][4], vs[NT][4];
+    float ks, vs;   // of key lane & 31
     unsigned char act;
-    // rows 0 ... rows - 1 (>= 1) of the tile at token j0 exist
-    __device__ __forceinline__ void load(const CaSide &s, const unsigned char *kb, const unsigned char *vb, const float *ksb, const float *vsb,
-                                         const unsigned char *mask, int j0, int rows, int x, int g)
+    // Rows 0 ... rows - 1 (>= 1) of the tile at token j0 exist.  Keys, with all scales and activity:
+    __device__ __forceinline__ void load_keys(unsigned st, const unsigned char *kb, const float *ksb, const float *vsb, const unsigned char *mask, int j0, int rows,
+                                              int x, int g)
     {
-        const unsigned kst = (unsigned)(s.k.l * ST::BYTES), vst = (unsigned)(s.v.l * ST::BYTES);
-        const unsigned last = (unsigned)(min(rows, ST::KT) - 1);
-        const CaBuf bk = ca_buffer(kb + (long)j0 * kst, last * kst + D * ST::BYTES), bv = ca_buffer(vb + (long)j0 * vst, last * vst + D * ST::BYTES);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int p = 0; p < KB / KP; ++p) ca_load<KP>(&k[n][p * KP / 4], bk, (unsigned)(16 * n + x) * kst + (unsigned)(p * 4 * KP + g * KP));
-        }
+        const unsigned last = (unsigned)(min(rows, ST::KT) - 1), mine = (unsigned)min(x + 16 * (g & 1), (int)last);
+        const CaBuf b = ca_buffer(kb + (long)j0 * st, last * st + D * ST::BYTES);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ca_load<VB>(v[n][e], bv, (unsigned)(16 * n + 4 * g + e) * vst + (unsigned)(x * VB));
+            for (int p = 0; p < KB / KP; ++p) ca_load<KP>(&k[n][p * KP / 4], b, (unsigned)(16 * n + x) * st + (unsigned)(p * 4 * KP + g * KP));
         if constexpr (ST::SCALED) {
-            const CaBuf b0 = ca_buffer(reinterpret_cast<const unsigned char *>(ksb + j0), 4 * last + 4), b1 = ca_buffer(reinterpret_cast<const unsigned char *>(vsb + j0), 4 * last + 4);
-            if (rows >= ST::KT) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    ca_load<16>(reinterpret_cast<unsigned *>(ks[n]), b0, (unsigned)(16 * n + 4 * g) * 4);
-                    ca_load<16>(reinterpret_cast<unsigned *>(vs[n]), b1, (unsigned)(16 * n + 4 * g) * 4);
-                }
-            } else {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        ca_load<4>(reinterpret_cast<unsigned *>(&ks[n][e]), b0, (unsigned)(16 * n + 4 * g + e) * 4);
-                        ca_load<4>(reinterpret_cast<unsigned *>(&vs[n][e]), b1, (unsigned)(16 * n + 4 * g + e) * 4);
-                    }
-            }
+            ks = ksb[j0 + mine];
+            vs = vsb[j0 + mine];
         }
-        if (mask) act = mask[j0 + min(x + 16 * (g & 1), (int)last)];
+        if (mask) act = mask[j0 + mine];
+    }
+    __device__ __forceinline__ void load_values(unsigned st, const unsigned char *vb, int j0, int rows, int x, int g)
+    {
+        const unsigned last = (unsigned)(min(rows, ST::KT) - 1);
+        const CaBuf b = ca_buffer(vb + (long)j0 * st, last * st + D * ST::BYTES);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ca_load<VB>(v[n][e], b, (unsigned)(16 * n + 4 * g + e) * st + (unsigned)(x * VB));
     }
 };
 
@@ -159,40 +155,44 @@ template <typename S> __device__ __forceinline__ bf16x2 ca_feature(unsigned a, u
     }
 }
 
-// Query rows as operands: lane (x, g) has of row x the features that its pieces of a key hold.  fp32 queries of 8-bit caches are the
-// sum of three bf16 numbers, cut off and not rounded: all 24 bits, and none overflows.
+// the same in fp16, of codes in 8 bits
+template <typename S> __device__ __forceinline__ f16x2 ca_feature_half(unsigned a, unsigned b, int j)
+{
+    if constexpr (std::is_same<S, E4M3>::value) {
+        const unsigned w = (j & 3) < 2 ? __builtin_amdgcn_perm(b, a, 0x05010400u) : __builtin_amdgcn_perm(b, a, 0x07030602u);
+        return j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false);
+    } else {
+        const int at = 8 * (j & 3);
+        return f16x2{(_Float16)(float)(signed char)(a >> at), (_Float16)(float)(signed char)(b >> at)};
+    }
+}
+
+// Query rows as operands in LDS, a piece of 16 bytes for each lane: lane (x, g) has of row x the features that its pieces of a key hold.
+// fp32 queries of 8-bit caches are the sum of three bf16 numbers, cut off and not rounded: all 24 bits, and none overflows.
 template <typename S, typename T, int D> struct CaQuery {
-    static constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    bf16x8 v[PARTS][D / 32];
-    __device__ __forceinline__ void load(const T *row, int g)
+    static constexpr bool PLAIN = CaStore<S>::BYTES == 4;                  // products in fp32
+    static constexpr int PARTS = !PLAIN && sizeof(T) == 4 ? 3 : 1, STEPS = PLAIN ? D / 16 : D / 32, PIECES = PARTS * STEPS;   // of a block of 16 rows
+    // step s of a block whose row x is at `row`, into `to`: the block's pieces, this lane's 16 bytes of each
+    static __device__ __forceinline__ void put(uint4 *to, const T *row, int s, int g, bool on)
     {
+        const auto keep = [&](uint4 y) { return on ? y : make_uint4(0, 0, 0, 0); };
+        // 8 bits: 16 features adjacent (d = 32: 8), two operands; bf16: 8; fp32: 4
+        const int at = PLAIN ? 16 * s + 4 * g : CaStore<S>::BYTES == 1 && D > 32 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+        if constexpr (PARTS == 1) to[s * 64] = keep(*reinterpret_cast<const uint4 *>(row + at));
+        else {
+            float f[8];
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            // 8 bits: 16 features adjacent (d = 32: 8), two operands; bf16: 8
-            const int at = CaStore<S>::BYTES == 1 && D > 32 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-            if constexpr (PARTS == 1) v[0][s] = *reinterpret_cast<const bf16x8 *>(row + at);
-            else {
-                float f[8];
+            for (int i = 0; i < 2; ++i) load4<float>(reinterpret_cast<const float *>(row) + at + 4 * i, reinterpret_cast<float(&)[4]>(f[4 * i]));
 #pragma unroll
-                for (int i = 0; i < 2; ++i) load4<float>(reinterpret_cast<const float *>(row) + at + 4 * i, reinterpret_cast<float(&)[4]>(f[4 * i]));
+            for (int p = 0; p < 3; ++p) {
+                unsigned w[4];
 #pragma unroll
-                for (int p = 0; p < 3; ++p)
+                for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(__float_as_uint(f[2 * i + 1]), __float_as_uint(f[2 * i]), 0x07060302u);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float cut = __uint_as_float(__float_as_uint(f[i]) & 0xffff0000u);
-                        v[p][s][i] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(f[i]) >> 16));
-                        f[i] = isinf(f[i]) ? 0.f : f[i] - cut;
-                    }
+                for (int i = 0; i < 8; ++i) f[i] = isinf(f[i]) ? 0.f : f[i] - __uint_as_float(__float_as_uint(f[i]) & 0xffff0000u);
+                to[(p * STEPS + s) * 64] = keep(make_uint4(w[0], w[1], w[2], w[3]));
             }
         }
-    }
-};
-template <int D> struct CaQuery<float, float, D> {
-    float v[D / 4];   // 16 c + 4 g + j at 4 c + j
-    __device__ __forceinline__ void load(const float *row, int g)
-    {
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) load4<float>(row + 16 * c + 4 * g, reinterpret_cast<float(&)[4]>(v[4 * c]));
     }
 };
 
@@ -214,6 +214,8 @@ __device__ __forceinline__ CaRow ca_row(const CaArgs &a, bool prefix, int b, int
     return w;
 }
 
+constexpr float CA_LEAST = -3.402823466e38f;   // a running maximum before the first score
+
 // Results of a row from its running maximum (powers of two), sum and whether it has met a key: factor of the accumulators, LSE
 __device__ __forceinline__ float ca_finish(float m, float sum, bool live, bool parts, float &lse)
 {
@@ -223,217 +225,428 @@ __device__ __forceinline__ float ca_finish(float m, float sum, bool live, bool p
     return nothing && parts ? 0.f : 1.f / sum;
 }
 
+// Wavefronts of a workgroup, which share their rows and split the keys
+constexpr int ca_waves(int nq, int d) { return nq == 1 && d < 128 ? 16 : 8; }
 template <typename S, typename T, int D, int NQ>
-__global__ __launch_bounds__(256, 1) void ca_attn_kernel(const CaArgs a)
+__global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) void ca_attn_kernel(const CaArgs a)
 {
     using ST = CaStore<S>;
     using TL = CaTile<S, D>;
-    constexpr int NT = ST::NT, KT = ST::KT, F = D / 16, PITCH = D + 4;
-    constexpr int PP = sizeof(T) == 4 ? 3 : 2;   // bf16 parts of P
-    __shared__ __align__(16) float red[4][16][PITCH];
-    __shared__ float red_m[4][16], red_l[4][16];
-    __shared__ int red_live[4][16];
+    using QL = CaQuery<S, T, D>;
+    constexpr int NW = ca_waves(NQ, D), NT = ST::NT, KT = ST::KT, F = D / 16, PITCH = D + 4;
+    // P in fp16 times 2^4 (HALF: codes in 8 bits for bf16 results), as the sum of two bf16 numbers (bf16 caches) or three (codes for fp32
+    // results), in fp32 (fp32 caches).  Sums of the first two are products with ones.
+    constexpr bool HALF = ST::BYTES == 1 && sizeof(T) == 2, ONES = HALF || ST::BYTES == 2;
+    constexpr int PP = HALF ? 1 : sizeof(T) == 4 ? 3 : 2;
+    constexpr float BIAS = HALF ? 4.f : 0.f;
+    // Powers of two that a row's maximum may grow by before its sums are scaled to it: fp16 ends at 2^16, and P keeps its bits down to 2^-18;
+    // the others lose nothing, and leave room for large values
+    constexpr float MANY = HALF ? 11.9f : 16.f;
+    union Lds {
+        uint4 q[NQ][QL::PIECES][64];
+        float red[NW][16 * NQ][PITCH];
+    };
+    __shared__ __align__(16) Lds lds;
+    __shared__ float red_m[NW][16 * NQ], red_l[NW][16 * NQ];
+    __shared__ int red_met[NW][16 * NQ];
+    __shared__ __align__(16) float scales[NW][ST::SCALED ? 64 : 4];   // of a wavefront's tile: keys' times c2, values'
+    __shared__ __align__(16) _Float16 halves[NW][HALF ? 32 : 4];       // HALF: values' next to the unit
+    __shared__ int row_at[16 * NQ], row_live[16 * NQ], reach[2];
 
     const bool prefix = (int)blockIdx.x >= a.side[0].wgs;
     const CaSide &s = a.side[prefix ? 1 : 0];
-    int at = (int)blockIdx.x - (prefix ? a.side[0].wgs : 0);
+    const int id = (int)blockIdx.x - (prefix ? a.side[0].wgs : 0);
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), x = lane & 15, g = lane >> 4;
-    // problems fastest, then blocks, then parts
-    int rest = s.by_problems(at);
-    const int prob = at - rest * s.problems, part = s.by_blocks(rest), blk = rest - part * s.blocks;
+    int prob, part, blk;
+    if (s.order == CA_NEIGHBOURS) {
+        const int u = (id & 7) * (s.wgs >> 3) + (id >> 3), v = s.by_blocks(u);
+        if (u >= s.units) return;
+        prob = s.by_parts(v); part = v - prob * s.parts; blk = u - v * s.blocks;
+    } else {
+        if (id >= s.units) return;
+        const int u = s.by_problems(id), v = s.by_parts(u);
+        prob = id - u * s.problems; part = u - v * s.parts; blk = s.blocks - 1 - v;
+    }
     const int b0 = prefix ? 0 : a.by_hk(prob), hk = prefix ? prob : prob - b0 * a.Hk;
-    const int kw = s.ks_waves, rw = wv / kw, kq = wv - rw * kw;
-    const int r0 = (blk * (4 / kw) + rw) * 16 * NQ;
+    const int r0 = blk * (16 * NQ), R1 = a.Lq * a.G;
     const int P = prefix ? sm_len(s.len, 0, s.L) : 0, up = a.causal ? 0 : a.W;
-    const int nb_live = min(NQ, (s.rows - r0 + 15) >> 4);   // blocks of rows that exist (may be <= 0)
+    const int nb_live = min(NQ, (s.rows - r0 + 15) >> 4);   // blocks of rows that exist
 
-    // this lane's rows
-    CaQuery<S, T, D> q[NQ];
-    int my_lo[NQ], my_hi[NQ];
-    unsigned live = 0, keys = 0;   // a bit per block: the row takes part; it has met a key
-    int lo = 0x7fffffff, hi = -1, all_lo = 0, all_hi = 0x7fffffff;
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const int r = r0 + 16 * n + x;
+    const unsigned char *kb = reinterpret_cast<const unsigned char *>(s.k.p) + (b0 * s.k.b + hk * s.k.h) * ST::BYTES;
+    const unsigned char *vb = reinterpret_cast<const unsigned char *>(s.v.p) + (b0 * s.v.b + hk * s.v.h) * ST::BYTES;
+    const float *ksb = ST::SCALED ? s.ks + b0 * s.ks_b + hk * s.ks_h : nullptr, *vsb = ST::SCALED ? s.vs + b0 * s.vs_b + hk * s.vs_h : nullptr;
+    const unsigned kst = (unsigned)(s.k.l * ST::BYTES), vst = (unsigned)(s.v.l * ST::BYTES);
+    const unsigned char *mk = s.mask ? s.mask + (long)b0 * s.L : nullptr;
+
+    // Keys that any, and that all, of the rows reach; tiles of the part, of which this wavefront takes every NW-th.  Of several items' rows
+    // (prefix) the starts decide: the first tiles are asked for as if one stood at the prefix's end, where that is not so once more.
+    int lo, hi, all_lo, all_hi, t = 0, t1 = 0;
+    TL ta;
+    auto fetch_keys = [&](TL &tl, int t) __attribute__((always_inline)) { tl.load_keys(kst, kb, ksb, vsb, mk, lo + t * KT, hi + 1 - lo - t * KT, x, g); };
+    auto fetch_values = [&](TL &tl, int t) __attribute__((always_inline)) { tl.load_values(vst, vb, lo + t * KT, hi + 1 - lo - t * KT, x, g); };
+    auto begin = [&]() __attribute__((always_inline)) {
+        const int tiles = hi < lo ? 0 : (hi - lo + KT) / KT;
+        const int per = s.by_span(tiles + s.parts * NW - 1) * NW;
+        t = part * per + wv;
+        t1 = min(tiles, (part + 1) * per);
+        if (t < t1) {   // (before the rows: all are under way at a time)
+            fetch_keys(ta, t);
+            fetch_values(ta, t);
+        }
+    };
+    const int start0 = a.start && !prefix ? min(max(a.start[b0], 0), 1 << 24) : 0, lq0 = sm_len(a.len_q, b0, a.Lq), lk0 = prefix ? P : sm_len(s.len, b0, s.L);
+    if (prefix) {
+        lo = max(0, P - a.W); hi = P - 1;
+        all_lo = 0; all_hi = hi;
+    } else {
+        const int first = start0 + a.by_g(r0), last = start0 + min(a.by_g(min(r0 + 16 * NQ, s.rows) - 1), lq0 - 1);
+        lo = max(0, first - a.W); hi = last < first ? -1 : min(last + up, lk0 - 1);
+        all_lo = last - a.W; all_hi = min(first + up, lk0 - 1);
+    }
+    begin();
+
+    // the rows' operands, positions and whether they take part, into LDS; rows that do not are zeros, so that what they hold decides nothing
+    for (int i = wv; i < NQ * QL::STEPS; i += NW) {
+        const int n = i / QL::STEPS, r = r0 + 16 * n + x;
         const CaRow w = ca_row(a, prefix, b0, hk, min(r, s.rows - 1));
-        bool on = r < s.rows && w.i < sm_len(a.len_q, w.b, a.Lq);
+        bool on = r < s.rows && w.i < (prefix ? sm_len(a.len_q, w.b, a.Lq) : lq0);
+        if (a.mask_q) on = on && a.mask_q[(long)w.b * a.Lq + w.i] != 0;
+        QL::put(&lds.q[n][0][lane], reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + w.hq * a.q.h + w.i * a.q.l, i - n * QL::STEPS, g, on);
+    }
+    if (wv == 0) {   // (16 NQ rows at most: one wavefront has them all)
+        const int r = r0 + lane;
+        const CaRow w = ca_row(a, prefix, b0, hk, min(r, s.rows - 1));
+        const int lq = prefix ? sm_len(a.len_q, w.b, a.Lq) : lq0, start = prefix && a.start ? min(max(a.start[w.b], 0), 1 << 24) : start0;
+        bool on = lane < 16 * NQ && r < s.rows && w.i < lq;
+        const int p = P + start + w.i;
+        if (prefix) {
+            int first = on ? p - a.W : 0x7fffffff, last = on ? p - a.W : 0;
+#pragma unroll
+            for (int d = 1; d < 16 * NQ; d <<= 1) first = min(first, __shfl_xor(first, d)), last = max(last, __shfl_xor(last, d));
+            if (lane == 0) reach[0] = first, reach[1] = last;
+        }
         if (on && a.mask_q) on = a.mask_q[(long)w.b * a.Lq + w.i] != 0;
-        const int p = (a.start ? min(max(a.start[w.b], 0), 1 << 24) : 0) + w.i;   // behind the prefix
-        my_lo[n] = max(0, prefix ? P + p - a.W : p - a.W);
-        my_hi[n] = prefix ? P - 1 : min(p + up, sm_len(s.len, w.b, s.L) - 1);
-        if (n < nb_live) q[n].load(reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + w.hq * a.q.h + w.i * a.q.l, g);
-        if (on) {
-            live |= 1u << n;
-            lo = min(lo, my_lo[n]); hi = max(hi, my_hi[n]);
-            all_lo = max(all_lo, my_lo[n]); all_hi = min(all_hi, my_hi[n]);
-        } else {
-            my_lo[n] = 0x3fffffff; my_hi[n] = -1;
+        if (lane < 16 * NQ) row_at[lane] = p, row_live[lane] = on;
+    }
+    __syncthreads();
+    if (prefix) {
+        const int first = max(0, __builtin_amdgcn_readfirstlane(reach[0]));
+        all_lo = __builtin_amdgcn_readfirstlane(reach[1]);
+        if (first != lo) {
+            lo = first;
+            begin();
         }
     }
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) {
-        lo = min(lo, __shfl_xor(lo, d)); hi = max(hi, __shfl_xor(hi, d));
-        all_lo = max(all_lo, __shfl_xor(all_lo, d)); all_hi = min(all_hi, __shfl_xor(all_hi, d));
-    }
-    lo = __builtin_amdgcn_readfirstlane(lo); hi = __builtin_amdgcn_readfirstlane(hi);
-    all_lo = __builtin_amdgcn_readfirstlane(all_lo); all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-    // this wavefront's tiles: every kw-th of the part's
-    const int tiles = hi < lo ? 0 : (hi - lo + KT) / KT;
-    const int per = s.by_span(tiles + s.parts * kw - 1) * kw;
-    const int t1 = min(tiles, (part + 1) * per);
-    int t = part * per + kq;
+    unsigned keys = 0;   // a bit per block: this lane's row has met a key
 
     f32x4 acc[NQ][F];
+    float unit = 0x1p-126f, inv = 0x1p126f;   // HALF: the power of two that accumulators count in, at least the largest scale of a value so far
     float m[NQ], sum[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        m[n] = -INFINITY;
+        m[n] = CA_LEAST;
         sum[n] = 0.f;
 #pragma unroll
         for (int j = 0; j < F; ++j) acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    const unsigned char *kb = reinterpret_cast<const unsigned char *>(s.k.p) + (b0 * s.k.b + hk * s.k.h) * ST::BYTES;
-    const unsigned char *vb = reinterpret_cast<const unsigned char *>(s.v.p) + (b0 * s.v.b + hk * s.v.h) * ST::BYTES;
-    const float *ksb = ST::SCALED ? s.ks + b0 * s.ks_b + hk * s.ks_h : nullptr, *vsb = ST::SCALED ? s.vs + b0 * s.vs_b + hk * s.vs_h : nullptr;
-    const unsigned char *mk = s.mask ? s.mask + (long)b0 * s.L : nullptr;
     const float c2 = sm_vector(a.c2), none = sm_vector(-INFINITY);
 
-    auto fetch = [&](TL &tl, int t) __attribute__((always_inline)) {
-        const int j0 = lo + t * KT;
-        tl.load(s, kb, vb, ksb, vsb, mk, j0, hi + 1 - j0, x, g);
+    constexpr unsigned FULL = KT == 32 ? 0xffffffffu : 0xffffu;
+    // scores of a block of rows with the tile's keys (which: of all of them, one after another, or of one)
+    auto scores = [&](auto &sc, const TL &tl, int nb0, int ql) __attribute__((always_inline)) {
+        constexpr int NB = (int)(sizeof(sc) / sizeof(sc[0]));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sc[nb][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (ST::BYTES == 4) {
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+                u32x4 qw[NB];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) qw[nb] = *reinterpret_cast<const u32x4 *>(&lds.q[nb0 + nb][c][ql]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+                        sc[nb][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.k[0][4 * c + i]), __uint_as_float(qw[nb][i]), sc[nb][0], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                bf16x8 kf[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    if constexpr (ST::BYTES == 1) kf[n] = ca_codes<S>(tl.k[n][2 * c], tl.k[n][2 * c + 1]);
+                    else kf[n] = __builtin_bit_cast(bf16x8, u32x4{tl.k[n][4 * c], tl.k[n][4 * c + 1], tl.k[n][4 * c + 2], tl.k[n][4 * c + 3]});
+#pragma unroll
+                for (int p = QL::PARTS - 1; p >= 0; --p)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        const bf16x8 qf = *reinterpret_cast<const bf16x8 *>(&lds.q[nb0 + nb][p * QL::STEPS + c][ql]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) sc[nb][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n], qf, sc[nb][n], 0, 0, 0);
+                    }
+            }
+        }
     };
-    auto step = [&](TL &tl, int t) __attribute__((always_inline)) {
+    // what the four keys of a lane's accumulators are multiplied by
+    auto key_factors = [&](float (&kc)[NT][4]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            f32x4 y = {c2, c2, c2, c2};
+            if constexpr (ST::SCALED) y = *reinterpret_cast<const f32x4 *>(&scales[wv][16 * n + 4 * g]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kc[n][e] = y[e];
+        }
+    };
+    auto value_factors = [&](float (&vc)[NT][4]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(&scales[wv][32 + 16 * n + 4 * g]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vc[n][e] = y[e];
+        }
+    };
+    // (apart: in a branch, whose conversions the compiler must not take together with those of the way past it)
+    auto value_operand = [&](const TL &tl, int j, bool apart) __attribute__((always_inline)) -> bf16x8 {
+        constexpr int PER = ST::BYTES < 4 ? 4 / ST::BYTES : 1;   // features of a word
+        bf16x8 vf;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {        // tokens 2 i, 2 i + 1 of the operand's 8: four of each tile
+            unsigned a0 = tl.v[(i >> 1) % NT][2 * (i & 1)][j / PER], a1 = tl.v[(i >> 1) % NT][2 * (i & 1) + 1][j / PER];
+            if (apart) asm("" : "+v"(a0), "+v"(a1));
+            const bf16x2 y = ca_feature<S>(a0, a1, j);
+            vf[2 * i] = y[0]; vf[2 * i + 1] = y[1];
+        }
+        return vf;
+    };
+    auto sum_of = [&](const float (&p)[4 * NT]) __attribute__((always_inline)) {
+        float y[4 * NT];
+#pragma unroll
+        for (int e = 0; e < 4 * NT; ++e) y[e] = p[e];
+#pragma unroll
+        for (int d = 2 * NT; d; d >>= 1)
+#pragma unroll
+            for (int e = 0; e < d; ++e) y[e] += y[e + d];
+        return y[0];
+    };
+    // p as the sum of N bf16 numbers
+    auto split = [&](auto &pf, float (&p)[4 * NT]) __attribute__((always_inline)) {
+        constexpr int N = (int)(sizeof(pf) / sizeof(pf[0]));
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            pf[h] = pack8(p);
+            if (h + 1 < N) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] -= (float)pf[h][e];
+            }
+        }
+    };
+
+    auto tile = [&](auto which, TL &tl) __attribute__((always_inline)) {
+        constexpr int NB = decltype(which)::value;   // blocks of rows at work
+        int ql = lane;
+        asm volatile("" : "+v"(ql));   // (queries are read from LDS in every tile, and not kept in registers that the loop has not)
         const int j0 = lo + t * KT;
-        unsigned on = sm_bits(0, hi - j0);
+        unsigned on = sm_bits(0, hi - j0) & FULL;
         if (mk) on &= (unsigned)__ballot(tl.act != 0);   // (lanes 0 ... 31: keys 0 ... 31)
-        if constexpr (KT == 16) on &= 0xffffu;
-        constexpr unsigned FULL = KT == 32 ? 0xffffffffu : 0xffffu;
         const bool whole = on == FULL && j0 >= all_lo && j0 + KT - 1 <= all_hi;
-        if (on != FULL) {   // what does not count must not meet a product: P is 0 there, and may be 0 times anything
-            const unsigned mine = on >> (4 * g);
+        bool even = true;   // HALF: the values' scales are fp16 numbers next to the unit
+        if constexpr (ST::SCALED) {   // from a key per lane to the four of its accumulators
+            const bool ok = on >> (lane & 31) & 1;
+            float rel = ok ? tl.vs : 0.f;
+            if constexpr (HALF) {
+                float v = rel <= 0x1p127f ? rel : 0.f;
+                if (__builtin_expect(__any(v > unit), 0)) {   // (at the first tile, and where a value is larger than all before)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+                    for (int d = 1; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
+                    const unsigned bits = (__float_as_uint(v) + 0x7fffffu) & 0x7f800000u;   // the next power of two
+                    const float u = __uint_as_float((unsigned)__builtin_amdgcn_readfirstlane((int)bits)), f = unit / u;
+                    unit = u;
+                    inv = 1.f / u;   // (exact, a subnormal number at the end)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool ok = mine >> (16 * n + e) & 1;
+                    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int w = 0; w < (TL::VB < 4 ? 1 : TL::VB / 4); ++w) tl.v[n][e][w] = ok ? tl.v[n][e][w] : 0u;
-                    if constexpr (ST::SCALED) tl.vs[n][e] = ok ? tl.vs[n][e] : 0.f;
+                        for (int j = 0; j < F; ++j) acc[nb][j] *= f;
                 }
+                rel *= inv;
+                even = __all(!ok || (rel >= 0x1p-14f && rel <= 1.f));
+                if (lane < 32) halves[wv][lane] = even ? (_Float16)rel : (_Float16)0;
+            }
+            scales[wv][lane] = lane < 32 ? tl.ks * c2 : rel;
         }
-        if (whole) keys = ~0u;
-        bf16x8 kf[NT][D / 32], vf[F];
+        f32x4 sc[NB][NT];
+        scores(sc, tl, 0, ql);
+        // The keys of the next tile are asked for as soon as these are used up, its values likewise; the last one asks for itself again, since
+        // loads under a condition are waited for with all that come after them
+        const int ahead = min(t + NW, t1 - 1);
+        SM_READ_FIRST();
+        fetch_keys(tl, ahead);
+        SM_READ_FIRST();
         float kc[NT][4];
-        if constexpr (ST::BYTES == 1) {
+        key_factors(kc);
+        if (__builtin_expect(!whole, 0)) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) kf[n][c] = ca_codes<S>(tl.k[n][2 * c], tl.k[n][2 * c + 1]);
-        } else if constexpr (ST::BYTES == 2) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c)
-                    kf[n][c] = __builtin_bit_cast(bf16x8, u32x4{tl.k[n][4 * c], tl.k[n][4 * c + 1], tl.k[n][4 * c + 2], tl.k[n][4 * c + 3]});
-        }
-        if constexpr (ST::BYTES < 4) {
-#pragma unroll
-            for (int j = 0; j < F; ++j) {
-                constexpr int PER = 4 / ST::BYTES;   // features of a word
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {        // tokens 2 i, 2 i + 1 of the operand's 8: four of each tile
-                    const bf16x2 y = ca_feature<S>(tl.v[i >> 1][2 * (i & 1)][j / PER], tl.v[i >> 1][2 * (i & 1) + 1][j / PER], j);
-                    vf[j][2 * i] = y[0]; vf[j][2 * i + 1] = y[1];
-                }
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) kc[n][e] = ST::SCALED ? tl.ks[n][e] * c2 : c2;
-#pragma unroll
-        for (int nb = 0; nb < NQ; ++nb) {
-            if (nb >= nb_live) break;
-            f32x4 sc[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                sc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if constexpr (ST::BYTES == 4) {
-#pragma unroll
-                    for (int c = 0; c < D / 4; ++c) sc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.k[n][c]), q[nb].v[c], sc[n], 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (int p = CaQuery<S, T, D>::PARTS - 1; p >= 0; --p)   // (the smallest part first)
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) sc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n][c], q[nb].v[p][c], sc[n], 0, 0, 0);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sc[n][e] *= kc[n][e];
-            }
-            if (!whole) {
-                const unsigned own = sm_bits(my_lo[nb] - j0, my_hi[nb] - j0) & on, keep = own >> (4 * g);
-                if (own) keys |= 1u << nb;
+            for (int nb = 0; nb < NB; ++nb) {
+                const int at = row_at[16 * nb + x] - j0;
+                const unsigned mine = sm_bits(at - a.W, prefix ? 31 : at + up) & on, keep = mine >> (4 * g);
+                if (mine) keys |= 1u << nb;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[n][e] = sm_keep(sc[n][e], keep, 16 * n + e, none);
+                    for (int e = 0; e < 4; ++e) sc[nb][n][e] = sm_keep(sc[nb][n][e] * kc[n][e], keep, 16 * n + e, none);
             }
-            // The running maximum moves when a score of any lane exceeds it by 2^SM_LAZY: lanes are compared with no exchange between them
-            float top = sc[0][0];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[n][e]);
-            if (__any(top > m[nb] + SM_LAZY)) {
-                const float mn = fmaxf(m[nb], ca_max_groups(top)), f = mn > -INFINITY ? fast_exp2(m[nb] - mn) : 1.f;
-                sum[nb] *= f;
+                for (int e = 0; e < 4; ++e) kc[n][e] = 1.f;
+            if (on != FULL) {   // what does not count must not meet a product: P is 0 there, and may be 0 times anything
+                const unsigned mine = on >> (4 * g);
 #pragma unroll
-                for (int j = 0; j < F; ++j) acc[nb][j] *= f;
-                m[nb] = mn;
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int w = 0; w < (TL::VB < 4 ? 1 : TL::VB / 4); ++w) tl.v[n][e][w] = mine >> (16 * n + e) & 1 ? tl.v[n][e][w] : 0u;
             }
-            const float mu = m[nb] > -INFINITY ? m[nb] : 0.f;
-            float p[4 * NT];
+        } else keys = ~0u;
+        float p[NB][4 * NT];
+        bf16x8 pf[NB][PP];
+        f16x8 ph[NB];
+        float down[NB];
+        bool moved = false;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) down[nb] = 1.f;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            // The running maximum moves when a score of any lane exceeds it by MANY: lanes are compared with no exchange between them
+            float top;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[4 * n + e] = fast_exp2(sc[n][e] - mu);
-                    sum[nb] += p[4 * n + e];
-                    if constexpr (ST::SCALED) p[4 * n + e] *= tl.vs[n][e];
-                }
-            if constexpr (ST::BYTES == 4) {
+                for (int e = 0; e < 4; ++e) p[nb][4 * n + e] = fmaf(sc[nb][n][e], kc[n][e], BIAS - m[nb]);
+            top = p[nb][0];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+            for (int e = 1; e < 4 * NT; ++e) top = fmaxf(top, p[nb][e]);
+            if (__builtin_expect(__any(top > BIAS + MANY), 0)) {
+                top = -INFINITY;
 #pragma unroll
-                    for (int j = 0; j < F; ++j) acc[nb][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.v[0][e][j]), p[e], acc[nb][j], 0, 0, 0);
-            } else {
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int h = 0; h < PP; ++h) {
-                    const bf16x8 pf = pack8(p);
-#pragma unroll
-                    for (int j = 0; j < F; ++j) acc[nb][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j], pf, acc[nb][j], 0, 0, 0);
-                    if (h + 1 < PP) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) p[e] -= (float)pf[e];
+                    for (int e = 0; e < 4; ++e) {
+                        sc[nb][n][e] *= kc[n][e];
+                        top = fmaxf(top, sc[nb][n][e]);
                     }
+                const float mn = fmaxf(m[nb], ca_max_groups(top));
+                down[nb] = fast_exp2(m[nb] - mn);
+                m[nb] = mn;
+                sum[nb] *= down[nb];
+                moved = true;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[nb][4 * n + e] = sc[nb][n][e] + (BIAS - mn);
+            }
+#pragma unroll
+            for (int e = 0; e < 4 * NT; ++e) p[nb][e] = fast_exp2(p[nb][e]);
+            if constexpr (HALF) {
+                const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ph[nb][e] = (_Float16)p[nb][e];
+                sum[nb] += __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph[nb], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0)[0];
+            } else if constexpr (ONES) {
+                const bf16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
+                split(pf[nb], p[nb]);
+#pragma unroll
+                for (int h = PP - 1; h >= 0; --h) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[nb][h], y, 0, 0, 0);
+                sum[nb] += y[0];
+            } else sum[nb] += sum_of(p[nb]);
+        }
+        if (__builtin_expect(moved, 0)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int j = 0; j < F; ++j) acc[nb][j] *= down[nb];
+        }
+        if constexpr (ST::BYTES == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < F; ++j)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) acc[nb][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.v[0][e][j]), p[nb][e], acc[nb][j], 0, 0, 0);
+        } else if constexpr (HALF) {
+            if (__builtin_expect(!even, 0)) {   // scales far apart: in fp32, as two bf16 numbers, a block of rows after another; zeros below
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    SM_READ_FIRST();
+                    float vc[NT][4], y[8];
+                    value_factors(vc);
+                    bf16x8 pw[2];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = (float)ph[nb][e] * vc[e >> 2][e & 3];
+                    split(pw, y);
+#pragma unroll
+                    for (int j = 0; j < F; ++j) {
+                        const bf16x8 vf = value_operand(tl, j, true);
+                        acc[nb][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pw[1], acc[nb][j], 0, 0, 0);
+                        acc[nb][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pw[0], acc[nb][j], 0, 0, 0);
+                        SM_READ_FIRST();
+                    }
+                    ph[nb] *= (_Float16)0;
                 }
+            }
+            const f16x4 v0 = *reinterpret_cast<const f16x4 *>(&halves[wv][4 * g]), v1 = *reinterpret_cast<const f16x4 *>(&halves[wv][16 + 4 * g]);
+            const f16x8 v8 = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) ph[nb] *= v8;
+#pragma unroll
+            for (int j = 0; j < F; ++j) {
+                f16x8 vf;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f16x2 y = ca_feature_half<S>(tl.v[i >> 1][2 * (i & 1)][j / 4], tl.v[i >> 1][2 * (i & 1) + 1][j / 4], j);
+                    vf[2 * i] = y[0]; vf[2 * i + 1] = y[1];
+                }
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) acc[nb][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, ph[nb], acc[nb][j], 0, 0, 0);
+            }
+        } else {
+            if constexpr (ST::SCALED) {
+                float vc[NT][4];
+                value_factors(vc);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[nb][e] *= vc[e >> 2][e & 3];
+                    split(pf[nb], p[nb]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < F; ++j) {
+                const bf16x8 vf = value_operand(tl, j, false);
+#pragma unroll
+                for (int h = 0; h < PP; ++h)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) acc[nb][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[nb][h], acc[nb][j], 0, 0, 0);
             }
         }
+        SM_READ_FIRST();
+        fetch_values(tl, ahead);
+        SM_READ_FIRST();
+        t += NW;
     };
-    TL ta, tb;
-    if (t < t1) fetch(ta, t);
-    while (t < t1) {
-        if (t + kw < t1) fetch(tb, t + kw);
-        SM_READ_FIRST();
-        step(ta, t);
-        t += kw;
-        if (t >= t1) break;
-        if (t + kw < t1) fetch(ta, t + kw);
-        SM_READ_FIRST();
-        step(tb, t);
-        t += kw;
-    }
+    auto walk = [&](auto which) __attribute__((always_inline)) {
+#pragma unroll 1
+        while (t < t1) {
+            tile(which, ta);
+        }
+    };
+    if (nb_live <= 1) walk(std::integral_constant<int, 1>{});
+    else walk(std::integral_constant<int, NQ>{});
 
     const long rows = (long)a.B * a.Hk * a.Lq * a.G;
     const int slot = part + (prefix ? a.side[0].parts : 0);
@@ -446,65 +659,61 @@ __global__ __launch_bounds__(256, 1) void ca_attn_kernel(const CaArgs a)
         if (a.parts > 1) a.part_lse[slot * rows + ((long)w.b * a.Hk + hk) * (a.Lq * a.G) + w.at] = lse;
         else a.lse[((long)w.b * a.G * a.Hk + w.hq) * a.Lq + w.i] = lse;
     };
+    bool met[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        float l = sum[n] + __shfl_xor(sum[n], 16);
-        l += __shfl_xor(l, 32);
-        const bool met = (live >> n & 1) && (keys >> n & 1);
-        if (kw == 1) {
-            const int r = r0 + 16 * n + x;
-            if (r < s.rows) {
-                const CaRow w = ca_row(a, prefix, b0, hk, r);
-                float lse;
-                const float scale = ca_finish(m[n], l, met, a.parts > 1, lse);
-#pragma unroll
-                for (int f = 0; f < F; ++f) {   // features (4 g + e) F + j, four at a time
-                    f32x4 y;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) y[c] = met ? acc[n][(4 * f + c) % F][(4 * f + c) / F] * scale : 0.f;
-                    put(w, 4 * F * g + 4 * f, y);
-                }
-                if (g == 0) put_lse(w, lse);
-            }
-        } else {
-            if (n) __syncthreads();
-#pragma unroll
-            for (int f = 0; f < F; ++f) {
-                f32x4 y;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) y[c] = acc[n][(4 * f + c) % F][(4 * f + c) / F];
-                *reinterpret_cast<f32x4 *>(&red[wv][x][4 * F * g + 4 * f]) = y;
-            }
-            if (g == 0) {
-                red_m[wv][x] = m[n];
-                red_l[wv][x] = l;
-                red_live[wv][x] = met;
-            }
-            __syncthreads();
-            // the kw wavefronts of the same rows: each of their threads takes four features of a row at a time
-            for (int u = kq * 64 + lane; u < 16 * (D / 4); u += kw * 64) {
-                const int row = u / (D / 4), f = (u % (D / 4)) * 4, r = r0 + 16 * n + row;
-                float M = -INFINITY, L = 0.f;
-                bool any = false;
-                for (int k = 0; k < kw; ++k) {
-                    M = fmaxf(M, red_m[rw * kw + k][row]);
-                    any |= red_live[rw * kw + k][row] != 0;
-                }
-                f32x4 y = {0.f, 0.f, 0.f, 0.f};
-                for (int k = 0; k < kw; ++k) {
-                    const float mk2 = red_m[rw * kw + k][row], c = mk2 > -INFINITY ? fast_exp2(mk2 - M) : 0.f;
-                    L = fmaf(red_l[rw * kw + k][row], c, L);
-                    y += *reinterpret_cast<const f32x4 *>(&red[rw * kw + k][row][f]) * c;
-                }
-                if (r < s.rows) {
-                    const CaRow w = ca_row(a, prefix, b0, hk, r);
-                    float lse;
-                    const float scale = ca_finish(M, L, any, a.parts > 1, lse);
-                    put(w, f, any ? y * scale : f32x4{0.f, 0.f, 0.f, 0.f});
-                    if (f == 0) put_lse(w, lse);
-                }
-            }
+        if constexpr (!ONES) {
+            sum[n] += __shfl_xor(sum[n], 16);
+            sum[n] += __shfl_xor(sum[n], 32);
         }
+        if constexpr (HALF) {
+            sum[n] *= 1.f / 16.f;   // (BIAS)
+#pragma unroll
+            for (int j = 0; j < F; ++j) acc[n][j] *= unit * (1.f / 16.f);
+        }
+        met[n] = row_live[16 * n + x] && (keys >> n & 1);
+    }
+    // features (4 g + e) F + j of a row, four at a time
+    auto piece = [&](int n, int f) __attribute__((always_inline)) {
+        f32x4 y;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = acc[n][(4 * f + c) % F][(4 * f + c) / F];
+        return y;
+    };
+    __syncthreads();   // (the queries' LDS is used for the results)
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        if (n >= nb_live) break;
+#pragma unroll
+        for (int f = 0; f < F; ++f) *reinterpret_cast<f32x4 *>(&lds.red[wv][16 * n + x][4 * F * g + 4 * f]) = piece(n, f);
+        if (g == 0) {
+            red_m[wv][16 * n + x] = m[n];
+            red_l[wv][16 * n + x] = sum[n];
+            red_met[wv][16 * n + x] = met[n];
+        }
+    }
+    __syncthreads();
+    // a thread takes four features of a row at a time
+    const int here = min(16 * NQ, s.rows - r0) * (D / 4);
+    for (int u = threadIdx.x; u < here; u += NW * 64) {
+        const int row = u / (D / 4), f = (u % (D / 4)) * 4;
+        float M = CA_LEAST, L = 0.f;
+        bool any = false;
+        for (int k = 0; k < NW; ++k) {
+            M = fmaxf(M, red_m[k][row]);
+            any |= red_met[k][row] != 0;
+        }
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < NW; ++k) {
+            const float c = fast_exp2(red_m[k][row] - M);
+            L = fmaf(red_l[k][row], c, L);
+            y += *reinterpret_cast<const f32x4 *>(&lds.red[k][row][f]) * c;
+        }
+        const CaRow w = ca_row(a, prefix, b0, hk, r0 + row);
+        float lse;
+        const float scale = ca_finish(M, L, any, a.parts > 1, lse);
+        put(w, f, any ? y * scale : f32x4{0.f, 0.f, 0.f, 0.f});
+        if (f == 0) put_lse(w, lse);
     }
 }
 

@@ -123,10 +123,9 @@ template <typename S, typename T, int D> __global__ __launch_bounds__(NTHREADS) 
     for (int i = 0; i < MOVE_ROWS; ++i) {
         const int l = l0 + i * RPB;
         on[i] = l < len && start + l >= 0 && start + l < a.Lc;
-        if (on[i]) {
-            load8<T>(f[i][0], reinterpret_cast<const T *>(a.k.p) + b * a.k.b + h * a.k.h + l * a.k.l + c);
-            load8<T>(f[i][1], reinterpret_cast<const T *>(a.v.p) + b * a.v.b + h * a.v.h + l * a.v.l + c);
-        }
+        const long at = min(l, a.L - 1);   // (a load under a condition is waited for at once)
+        load8<T>(f[i][0], reinterpret_cast<const T *>(a.k.p) + b * a.k.b + h * a.k.h + at * a.k.l + c);
+        load8<T>(f[i][1], reinterpret_cast<const T *>(a.v.p) + b * a.v.b + h * a.v.h + at * a.v.l + c);
     }
 #pragma unroll
     for (int i = 0; i < MOVE_ROWS; ++i) {
@@ -157,18 +156,17 @@ template <typename S, typename T, int D> __global__ __launch_bounds__(NTHREADS) 
     const int l0 = blockIdx.x * (RPB * MOVE_ROWS) + threadIdx.x / TPR;
     uint2 w[MOVE_ROWS][2];
     float s[MOVE_ROWS][2];
+    bool on[MOVE_ROWS];
 #pragma unroll
     for (int i = 0; i < MOVE_ROWS; ++i) {
         const int l = l0 + i * RPB;
         const long at = start + l;
-        w[i][0] = w[i][1] = make_uint2(0, 0);
-        s[i][0] = s[i][1] = 0.f;
-        if (l < a.L && at >= 0 && at < len) {
-            w[i][0] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const unsigned char *>(a.kc.p) + b * a.kc.b + h * a.kc.h + at * a.kc.l + c);
-            w[i][1] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const unsigned char *>(a.vc.p) + b * a.vc.b + h * a.vc.h + at * a.vc.l + c);
-            s[i][0] = a.ks.p[b * a.ks.b + h * a.ks.h + at];
-            s[i][1] = a.vs.p[b * a.vs.b + h * a.vs.h + at];
-        }
+        on[i] = at >= 0 && at < len;
+        const long from = min(max(at, 0L), a.Lc - 1L);
+        w[i][0] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const unsigned char *>(a.kc.p) + b * a.kc.b + h * a.kc.h + from * a.kc.l + c);
+        w[i][1] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const unsigned char *>(a.vc.p) + b * a.vc.b + h * a.vc.h + from * a.vc.l + c);
+        s[i][0] = a.ks.p[b * a.ks.b + h * a.ks.h + from];
+        s[i][1] = a.vs.p[b * a.vs.b + h * a.vs.h + from];
     }
 #pragma unroll
     for (int i = 0; i < MOVE_ROWS; ++i) {
@@ -181,7 +179,7 @@ template <typename S, typename T, int D> __global__ __launch_bounds__(NTHREADS) 
             const bf16x8 x = ca_codes<S>(w[i][k].x, w[i][k].y);
             float y[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = (float)x[j] * s[i][k];
+            for (int j = 0; j < 8; ++j) y[j] = on[i] ? (float)x[j] * s[i][k] : 0.f;
             if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x8 *>(to) = pack8(y);
             else {
                 store4<T>(to, y[0], y[1], y[2], y[3]);
@@ -247,8 +245,8 @@ int check(const CaProblem &p, bool prefix)
     return SKA_OK;
 }
 
-// How one side is launched: blocks of 16 rows of a wavefront, wavefronts that share rows, blocks, parts
-struct CaGrid { int kw; long blocks; int parts; };
+// How one side is launched: blocks of rows, parts of a walk, the workgroups' order
+struct CaGrid { long blocks; int parts; int order; };
 int ca_rows_of(const CaProblem &p)
 {
     const long rows = p.Lp ? p.R() * p.B : p.R();
@@ -258,14 +256,19 @@ int ca_rows_of(const CaProblem &p)
 CaGrid ca_grid(const CaProblem &p, int nq, bool prefix)
 {
     const long rows = prefix ? p.R() * p.B : p.R(), problems = prefix ? p.Hk : (long)p.B * p.Hk, L = prefix ? p.Lp : p.Lk;
-    const long wave_rows = 16 * nq, need = (rows + wave_rows - 1) / wave_rows;
+    const long unit_rows = 16 * nq, nw = ca_waves(nq, p.d);
     CaGrid g;
-    g.kw = need >= 3 ? 1 : need == 2 ? 2 : 4;
-    g.blocks = (need + 4 / g.kw - 1) / (4 / g.kw);
-    const long reach = std::min(L, prefix ? (long)p.W : std::min(wave_rows * (4 / g.kw) / p.G() + 1, (long)p.Lq) + (p.causal ? 1L : 2L) * p.W);
+    g.blocks = (rows + unit_rows - 1) / unit_rows;
+    const long reach = std::min(L, prefix ? (long)p.W : std::min(unit_rows / p.G() + 1, (long)p.Lq) + (p.causal ? 1L : 2L) * p.W);
+    g.order = prefix || g.blocks <= 8 || reach < L / 2 ? CA_NEIGHBOURS : CA_LAST_FIRST;
     const long tile = p.store == SKA_F32 ? 16 : 32, tiles = (reach + tile - 1) / tile;
-    const long room = nq == 1 ? 1024 : 512;
-    g.parts = (int)std::max(1L, std::min({room / (g.blocks * problems), tiles / (4 * g.kw), 256L}));
+    const long room = (nq == 1 && p.d < 128 ? 4096 : 2048) / nw, least = 2;   // workgroups
+    long own = 0;   // of the items' own keys, beside a prefix
+    if (prefix) {
+        const CaGrid o = ca_grid(p, nq, false);
+        own = std::min(room / 2, o.blocks * o.parts * p.B * p.Hk);
+    }
+    g.parts = (int)std::max(1L, std::min({(p.Lp && !prefix ? room / 2 : room - own) / (g.blocks * problems), tiles / (least * nw), 256L}));
     return g;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -295,17 +298,19 @@ int side_of(CaSide &s, const CaKept &c, int B, int Hk, int L, int d, int store)
     s.vs = v.p; s.vs_b = v.b; s.vs_h = v.h;
     return SKA_OK;
 }
-void place(CaSide &s, const CaProblem &p, const CaGrid &g, bool prefix)
+void place(CaSide &s, const CaProblem &p, int nq, const CaGrid &g, bool prefix)
 {
     s.rows = (int)(prefix ? p.R() * p.B : p.R());
     s.problems = prefix ? p.Hk : p.B * p.Hk;
-    s.ks_waves = g.kw;
     s.blocks = (int)g.blocks;
     s.parts = g.parts;
-    s.wgs = (int)(g.blocks * g.parts * s.problems);
+    s.order = g.order;
+    s.units = (int)(g.blocks * g.parts * s.problems);
+    s.wgs = (s.units + 7) / 8 * 8;
     s.by_problems = SmDiv::by(s.problems);
     s.by_blocks = SmDiv::by(s.blocks);
-    s.by_span = SmDiv::by(s.parts * s.ks_waves);
+    s.by_parts = SmDiv::by(s.parts);
+    s.by_span = SmDiv::by(s.parts * ca_waves(nq, p.d));
 }
 typedef int (*Launch)(int, const void *, hipStream_t);
 #define BY_D(NAME) {NAME##_32, NAME##_64, NAME##_128}
@@ -343,8 +348,8 @@ int attn(const CaProblem &p, const void *Q, const ska_strides *q_strides, const 
     a.by_g = SmDiv::by(a.G);
     a.by_hk = SmDiv::by(a.Hk);
     a.by_r = SmDiv::by((unsigned)p.R());
-    place(a.side[0], p, ca_grid(p, nq, false), false);
-    if (prefix) place(a.side[1], p, ca_grid(p, nq, true), true);
+    place(a.side[0], p, nq, ca_grid(p, nq, false), false);
+    if (prefix) place(a.side[1], p, nq, ca_grid(p, nq, true), true);
     const int at = p.store == SKA_F32 ? 0 : p.store == SKA_BF16 ? 1 : (p.store == SKA_E4M3 ? 2 : 4) + (p.dtype == SKA_BF16);
     return LAUNCH[at][p.d == 32 ? 0 : p.d == 64 ? 1 : 2](nq, &a, static_cast<hipStream_t>(stream));
 }

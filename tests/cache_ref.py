@@ -58,8 +58,8 @@ def prefix_pairs(B, Lq, P, Lp, W, start, len_q, mask_q, mask_p):
     return ok
 
 
-def attn(q, k, v, ok, eps, dtype_v=None):
-    """q [B,Hq,Lq,d] storage, k, v [B,Hk,L,d] float64 values, ok [B,Lq,L].  (value, bound) of O and LSE.  Tokens that take part in no pair are
+def attn(q, k, v, ok, eps, codes=True):
+    """q [B,Hq,Lq,d] storage, k, v [B,Hk,L,d] float64 values (codes: of 8-bit codes), ok [B,Lq,L].  (value, bound) of O and LSE.  Tokens that take part in no pair are
     left out before anything is multiplied."""
     B, Hq, Lq, d = q.shape
     G = Hq // k.shape[1]
@@ -81,17 +81,22 @@ def attn(q, k, v, ok, eps, dtype_v=None):
     e_s = (3 * d + 6) * F32 * mag
     e_exp = e_s + 4 * F32 * (torch.where(okh, s, 0.0).abs() + top0.abs()) + 4 * F32
     worst = torch.where(okh, e_exp, 0.0).amax(-1, keepdim=True)
-    # P times the value's scale: a rounding; as two bf16 numbers 2^-16 (bf16), as three 2^-24 (fp32); three sums of n terms
-    parts = half(torch.bfloat16) ** 2 if q.dtype == torch.bfloat16 else F32
-    e_o = (p @ vd.abs()) * (parts + 2 * worst + 3 * n * F32 + 12 * F32) * 1.02 + half(q.dtype) * o.abs()
-    e_lse = (worst + n * F32)[..., 0] + 4 * F32 * (lse.abs().nan_to_num(posinf=0.0) + top0[..., 0].abs()) + 4 * F32
+    # P and the value's scale: in fp32 results all their bits; in bf16 ones of codes three fp16 roundings (P, the scale next to its unit, their
+    # product: 2^-11 each, and half of the smallest fp16 number, 2^-25, in P, which is counted in 2^-4, and in the product, where the value
+    # is counted in at most twice the largest: 2^-29 + 2^-28, with the row's sum at least 1 in P's units); of bf16 values P as two bf16 numbers, 2^-16.  Three sums of n terms
+    parts, tiny = F32, 0.0
+    if q.dtype == torch.bfloat16:
+        parts, tiny = (3 * 2.0 ** -11, 2.0 ** -27 * n * vd.abs().amax()) if codes else (half(torch.bfloat16) ** 2, 0.0)
+    e_o = (p @ vd.abs()) * (parts + 2 * worst + 3 * n * F32 + 12 * F32) * 1.02 + tiny + half(q.dtype) * o.abs()
+    # (sums of the P that the products take)
+    e_lse = (worst + n * F32 + parts)[..., 0] + 4 * F32 * (lse.abs().nan_to_num(posinf=0.0) + top0[..., 0].abs()) + 4 * F32
     return {"O": (o, e_o), "LSE": (lse, e_lse)}
 
 
-def prefix_attn(q, pk, pv, k, v, W, causal, eps, P=None, start=None, len_q=None, len_k=None, mask_q=None, mask_k=None, mask_p=None):
+def prefix_attn(q, pk, pv, k, v, W, causal, eps, P=None, start=None, len_q=None, len_k=None, mask_q=None, mask_k=None, mask_p=None, codes=True):
     """pk, pv [Hk,Lp,d], k, v [B,Hk,Lk,d] float64 values."""
     B, Lq, Lp = q.shape[0], q.shape[2], pk.shape[1]
     ok = torch.cat([prefix_pairs(B, Lq, Lp if P is None else P, Lp, W, start, len_q, mask_q, mask_p),
                     pairs(B, Lq, k.shape[2], W, causal, start, len_q, len_k, mask_q, mask_k)], 2)
     both = lambda a, b: torch.cat([a[None].expand(B, *a.shape), b], 2)   # noqa: E731
-    return attn(q, both(pk, k), both(pv, v), ok, eps)
+    return attn(q, both(pk, k), both(pv, v), ok, eps, codes)

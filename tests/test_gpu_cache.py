@@ -265,7 +265,7 @@ def test_prefix(B, Hq, Hk, Lq, Lp, Lk, d, W, causal, eps, store, dtype):
         call = lambda: ska.ska_prefix_attn_fwd(q.cuda(), prefix, own, W, causal, eps, len_p=None if P is None else ints(P).cuda(), mask_p=cuda(mask_p),   # noqa: E731
                                                **{n: x.cuda() for n, x in kw.items()})
         O, LSE = call()
-        want = ref.prefix_attn(q, *pkv, *kv, W, causal, eps, P=P, mask_p=mask_p, **clamped(kw, Lq, Lk))
+        want = ref.prefix_attn(q, *pkv, *kv, W, causal, eps, P=P, mask_p=mask_p, codes=store != "same", **clamped(kw, Lq, Lk))
         check("O", O, want["O"])
         check("LSE", LSE, want["LSE"])
         again = call()
@@ -281,7 +281,7 @@ def test_prefix_lengths_at_their_ends():
     n = ints(0, 4, 9)
     for given, P in ((-7, 0), (0, 0), (50, 50), (2 ** 31 - 1, 50)):
         O, LSE = call(len_p=ints(given).cuda(), len_k=n.cuda(), start_q=(n - 1).cuda())
-        want = ref.prefix_attn(q, pk[0].double(), pv[0].double(), k.double(), v.double(), ALL, True, 1.0, P=P, len_k=n, start=(n - 1).clamp(min=0))
+        want = ref.prefix_attn(q, pk[0].double(), pv[0].double(), k.double(), v.double(), ALL, True, 1.0, P=P, len_k=n, start=(n - 1).clamp(min=0), codes=False)
         check("O", O, want["O"])
         check("LSE", LSE, want["LSE"])
         if P == 0:
