@@ -17,7 +17,7 @@ HIPCC_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # MFMA results straight into VGPRs (no accumulator-register copies before the VALU work)
     "-mllvm", "-amdgpu-mfma-vgpr-form",
-    "-I" + os.path.join(ROOT, "include"), *os.environ.get("XF", "").split(),
+    "-I" + os.path.join(ROOT, "include"),
 ]
 # Objects: the library, the step kernel's instances by storage type and head dimension (most of it), and the operators of the layer
 # around it.  Compiled side by side.
