@@ -46,30 +46,84 @@ int scales_of(Scales &t, const float *p, const ska_scale_strides *s, int B, int 
 }
 
 // ------------------------------------------------------------------ writing and reading
-// A thread takes 8 features of a key's row and of the value's: D / 8 threads a row, one exchange between them for its largest
-// feature.  Memory bounds both; what a row reads and writes is asked for before anything waits.
+// A thread takes 8 features of a key's row and of the value's: D / 8 threads a row, which compare their largest features in registers.
+// Memory bounds both, if only just: the codes are made and read by the conversion instructions, the largest feature of bf16 rows is
+// looked for among bit patterns, two at a time.
 struct MoveArgs {
     SmTensor k, v, kc, vc;
     Scales ks, vs;
     const int *start, *len;
     int B, Hk, L, Lc;
-    SmDiv by_hk;
+    int inner;      // heads that follow one another within a token, as a projection leaves them: Hk, or 1
+    SmDiv by_hk, by_inner;
 };
-constexpr int MOVE_ROWS = 4;   // of a thread
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
-template <typename T> __device__ __forceinline__ void load8(float (&f)[8], const T *p)
-{
-    load4<T>(p, reinterpret_cast<float(&)[4]>(f[0]));
-    load4<T>(p + 4, reinterpret_cast<float(&)[4]>(f[4]));
-}
-template <> __device__ __forceinline__ void load8<__bf16>(float (&f)[8], const __bf16 *p)
-{
-    const bf16x8 x = *reinterpret_cast<const bf16x8 *>(p);
+// 8 features of a row as they are stored
+template <typename T> struct Eight;
+template <> struct Eight<__bf16> {
+    uint4 w;
+    __device__ __forceinline__ void load(const __bf16 *p) { w = *reinterpret_cast<const uint4 *>(p); }
+    // bits of the largest magnitude as fp32: as an unsigned number, so that infinities and NaN are the largest
+    __device__ __forceinline__ unsigned largest() const
+    {
+        const unsigned x[4] = {w.x & 0x7fff7fffu, w.y & 0x7fff7fffu, w.z & 0x7fff7fffu, w.w & 0x7fff7fffu};
+        u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(__builtin_bit_cast(u16x2, x[0]), __builtin_bit_cast(u16x2, x[1])),
+                                            __builtin_elementwise_max(__builtin_bit_cast(u16x2, x[2]), __builtin_bit_cast(u16x2, x[3])));
+        return (unsigned)max(m[0], m[1]) << 16;
+    }
+    __device__ __forceinline__ void floats(float (&f)[8]) const
+    {
+        const unsigned x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)x[i];
+        for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(x[i] << 16), f[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+    }
+    // features 4 i ... 4 i + 3 divided by a power of two, as e4m3 numbers
+    __device__ __forceinline__ unsigned e4m3(int i, float scale) const
+    {
+        const unsigned x[4] = {w.x, w.y, w.z, w.w};
+        s16x2 r = {0, 0};
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, x[2 * i]), scale, false);
+        return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, x[2 * i + 1]), scale, true));
+    }
+};
+template <> struct Eight<float> {
+    float f[8];
+    __device__ __forceinline__ void load(const float *p)
+    {
+        load4<float>(p, reinterpret_cast<float(&)[4]>(f[0]));
+        load4<float>(p + 4, reinterpret_cast<float(&)[4]>(f[4]));
+    }
+    __device__ __forceinline__ unsigned largest() const
+    {
+        unsigned m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+        return m;
+    }
+    __device__ __forceinline__ void floats(float (&y)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = f[i];
+    }
+    __device__ __forceinline__ unsigned e4m3(int i, float scale) const
+    {
+        s16x2 r = {0, 0};
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, f[4 * i], f[4 * i + 1], scale, false);
+        return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, f[4 * i + 2], f[4 * i + 3], scale, true));
+    }
+};
+// the largest among the N adjacent lanes of a row
+template <int N> __device__ __forceinline__ unsigned row_largest(unsigned m)
+{
+    m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, true));             // lanes 1, 0, 3, 2
+    m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, true));             // 2, 3, 0, 1
+    if (N > 4) m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xf, 0xf, true));   // 8 lanes mirrored
+    if (N > 8) m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x140, 0xf, 0xf, true));   // 16 lanes mirrored
+    return m;
 }
-
-// Scale of a row whose largest feature has the bits `a` (as an unsigned number, so that infinities and NaN are the largest)
+// Scale of a row whose largest feature has the bits `a`
 template <typename S> __device__ __forceinline__ float move_scale(unsigned a)
 {
     if (a >= 0x7f800000u) return NAN;
@@ -79,120 +133,112 @@ template <typename S> __device__ __forceinline__ float move_scale(unsigned a)
     else return fminf(fmaxf(__uint_as_float(a) / 127.f, 0x1p-126f), 0x1.020406p+121f);   // (127 times the next number is infinite)
 }
 // 8 features as codes
-template <typename S> __device__ __forceinline__ uint2 move_codes(const float (&f)[8], float scale)
+template <typename S, typename T> __device__ __forceinline__ uint2 move_codes(const Eight<T> &x, float scale)
 {
-    unsigned w[2] = {0, 0};
     if (!(scale > 0.f)) return make_uint2(0, 0);   // (NaN)
     if constexpr (std::is_same<S, E4M3>::value) {
-        const float inv = __uint_as_float((254u << 23) - __float_as_uint(scale));   // a power of two: exact
-        const float most = scale == 0x1p120f ? 240.f : 448.f;                       // (256 2^120 would be infinite)
-        float y[8];
+        uint2 w = make_uint2(x.e4m3(0, scale), x.e4m3(1, scale));
+        if (scale == 0x1p120f) {   // (256 2^120 would be infinite: codes 0x78 of either sign, and no larger ones, become 240's)
+            const auto least = [](unsigned y) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(f[i] * inv, -most), most);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int x = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i], y[4 * i + 1], 0, false);
-            w[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], x, true);
+                for (int i = 0; i < 32; i += 8)
+                    if ((y >> i & 0x7f) > 0x77) y = (y & ~(0x7fu << i)) | 0x77u << i;
+                return y;
+            };
+            w.x = least(w.x); w.y = least(w.y);
         }
+        return w;
     } else {
+        // The nearest integer to a product with the rounded reciprocal, in the lower bits of a sum with 1.5 2^23; its remainder, which is exact
+        // near a border, says where that was not the quotient's (seldom)
+        constexpr float MAGIC = 12582912.f;
         const float inv = 1.f / scale, half = 0.5f * scale;
+        float f[8], n[8], most = 0.f;
+        x.floats(f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            // the nearest integer to a rounded quotient, put right by the remainder, which is exact near a border
-            float n = rintf(f[i] * inv);
-            const float rest = fmaf(-n, scale, f[i]);
-            const bool odd = (int)n & 1;
-            if (rest > half || (rest == half && odd)) n += 1.f;
-            else if (rest < -half || (rest == -half && odd)) n -= 1.f;
-            w[i >> 2] |= ((unsigned)(int)fminf(fmaxf(n, -127.f), 127.f) & 0xffu) << (8 * (i & 3));
+            n[i] = fmaf(f[i], inv, MAGIC);
+            most = fmaxf(most, fabsf(fmaf(MAGIC - n[i], scale, f[i])));
         }
+        if (most >= half) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float rest = fmaf(MAGIC - n[i], scale, f[i]);
+                const bool odd = __float_as_uint(n[i]) & 1;
+                if (rest > half || (rest == half && odd)) n[i] += 1.f;
+                else if (rest < -half || (rest == -half && odd)) n[i] -= 1.f;
+                n[i] = fminf(fmaxf(n[i], MAGIC - 127.f), MAGIC + 127.f);
+            }
+        }
+        unsigned w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const unsigned lo = __builtin_amdgcn_perm(__float_as_uint(n[4 * i + 1]), __float_as_uint(n[4 * i]), 0x0c0c0400u);
+            const unsigned hi = __builtin_amdgcn_perm(__float_as_uint(n[4 * i + 3]), __float_as_uint(n[4 * i + 2]), 0x0c0c0400u);
+            w[i] = lo | hi << 16;
+        }
+        return make_uint2(w[0], w[1]);
     }
-    return make_uint2(w[0], w[1]);
 }
+
+// A thread's 8 features: of which item, token and head
+template <int D> struct MoveAt {
+    int b, h, l, c;
+    __device__ __forceinline__ MoveAt(const MoveArgs &a)
+    {
+        constexpr int TPR = D / 8;
+        const int n = blockIdx.y * a.inner, row = blockIdx.x * (NTHREADS / TPR) + threadIdx.x / TPR;
+        b = a.by_hk(n);
+        l = a.by_inner(row);
+        h = n - b * a.Hk + row - l * a.inner;
+        c = (threadIdx.x % TPR) * 8;
+    }
+    template <typename E> __device__ __forceinline__ E *to(const SmTensor &t, long l) const
+    {
+        return reinterpret_cast<E *>(const_cast<void *>(t.p)) + b * t.b + h * t.h + l * t.l + c;
+    }
+    __device__ __forceinline__ float *to(const Scales &t, long l) const { return const_cast<float *>(t.p) + b * t.b + h * t.h + l; }
+};
 
 template <typename S, typename T, int D> __global__ __launch_bounds__(NTHREADS) void cache_write_kernel(const MoveArgs a)
 {
-    constexpr int TPR = D / 8, RPB = NTHREADS / TPR;   // threads of a row, rows of a block at a time
-    const int n = blockIdx.y, b = a.by_hk(n), h = n - b * a.Hk, c = (threadIdx.x % TPR) * 8;
-    const int len = sm_len(a.len, b, a.L);
-    const long start = a.start ? a.start[b] : 0;
-    const int l0 = blockIdx.x * (RPB * MOVE_ROWS) + threadIdx.x / TPR;
-    float f[MOVE_ROWS][2][8];
-    bool on[MOVE_ROWS];
-#pragma unroll
-    for (int i = 0; i < MOVE_ROWS; ++i) {
-        const int l = l0 + i * RPB;
-        on[i] = l < len && start + l >= 0 && start + l < a.Lc;
-        const long at = min(l, a.L - 1);   // (a load under a condition is waited for at once)
-        load8<T>(f[i][0], reinterpret_cast<const T *>(a.k.p) + b * a.k.b + h * a.k.h + at * a.k.l + c);
-        load8<T>(f[i][1], reinterpret_cast<const T *>(a.v.p) + b * a.v.b + h * a.v.h + at * a.v.l + c);
-    }
-#pragma unroll
-    for (int i = 0; i < MOVE_ROWS; ++i) {
-        if (!on[i]) continue;   // (all threads of a row alike)
-        const long at = start + l0 + i * RPB;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            unsigned m = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(f[i][w][k]) & 0x7fffffffu);
-#pragma unroll
-            for (int d = 1; d < TPR; d <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, d));
-            const float scale = move_scale<S>(m);
-            const SmTensor &t = w ? a.vc : a.kc;
-            const Scales &s = w ? a.vs : a.ks;
-            *reinterpret_cast<uint2 *>(reinterpret_cast<unsigned char *>(const_cast<void *>(t.p)) + b * t.b + h * t.h + at * t.l + c) = move_codes<S>(f[i][w], scale);
-            if (c == 0) const_cast<float *>(s.p)[b * s.b + h * s.h + at] = scale;
-        }
-    }
+    const MoveAt<D> w(a);
+    const long at = (a.start ? a.start[w.b] : 0) + (long)w.l;
+    if (w.l >= sm_len(a.len, w.b, a.L) || at < 0 || at >= a.Lc) return;   // (all threads of a row alike)
+    const bool values = blockIdx.z;
+    Eight<T> x;
+    x.load(w.template to<T>(values ? a.v : a.k, w.l));
+    const float scale = move_scale<S>(row_largest<D / 8>(x.largest()));
+    *reinterpret_cast<uint2 *>(w.template to<unsigned char>(values ? a.vc : a.kc, at)) = move_codes<S>(x, scale);
+    if (w.c == 0) *w.to(values ? a.vs : a.ks, at) = scale;
 }
 
 template <typename S, typename T, int D> __global__ __launch_bounds__(NTHREADS) void cache_read_kernel(const MoveArgs a)
 {
-    constexpr int TPR = D / 8, RPB = NTHREADS / TPR;
-    const int n = blockIdx.y, b = a.by_hk(n), h = n - b * a.Hk, c = (threadIdx.x % TPR) * 8;
-    const int len = sm_len(a.len, b, a.Lc);
-    const long start = a.start ? a.start[b] : 0;
-    const int l0 = blockIdx.x * (RPB * MOVE_ROWS) + threadIdx.x / TPR;
-    uint2 w[MOVE_ROWS][2];
-    float s[MOVE_ROWS][2];
-    bool on[MOVE_ROWS];
+    const MoveAt<D> w(a);
+    if (w.l >= a.L) return;
+    const bool values = blockIdx.z;
+    const long at = (a.start ? a.start[w.b] : 0) + (long)w.l, from = min(max(at, 0L), a.Lc - 1L);   // (loads under a condition are waited for at once)
+    const bool on = at >= 0 && at < sm_len(a.len, w.b, a.Lc);
+    uint2 x = *reinterpret_cast<const uint2 *>(w.template to<unsigned char>(values ? a.vc : a.kc, from));
+    float s = *w.to(values ? a.vs : a.ks, from);
+    if (!on) x = make_uint2(0, 0), s = 0.f;
+    T *to = w.template to<T>(values ? a.v : a.k, w.l);
+    const bf16x8 c = ca_codes<S>(x.x, x.y);
+    float y[8];
 #pragma unroll
-    for (int i = 0; i < MOVE_ROWS; ++i) {
-        const int l = l0 + i * RPB;
-        const long at = start + l;
-        on[i] = at >= 0 && at < len;
-        const long from = min(max(at, 0L), a.Lc - 1L);
-        w[i][0] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const unsigned char *>(a.kc.p) + b * a.kc.b + h * a.kc.h + from * a.kc.l + c);
-        w[i][1] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const unsigned char *>(a.vc.p) + b * a.vc.b + h * a.vc.h + from * a.vc.l + c);
-        s[i][0] = a.ks.p[b * a.ks.b + h * a.ks.h + from];
-        s[i][1] = a.vs.p[b * a.vs.b + h * a.vs.h + from];
-    }
-#pragma unroll
-    for (int i = 0; i < MOVE_ROWS; ++i) {
-        const int l = l0 + i * RPB;
-        if (l >= a.L) continue;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const SmTensor &t = k ? a.v : a.k;
-            T *to = reinterpret_cast<T *>(const_cast<void *>(t.p)) + b * t.b + h * t.h + l * t.l + c;
-            const bf16x8 x = ca_codes<S>(w[i][k].x, w[i][k].y);
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = on[i] ? (float)x[j] * s[i][k] : 0.f;
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x8 *>(to) = pack8(y);
-            else {
-                store4<T>(to, y[0], y[1], y[2], y[3]);
-                store4<T>(to + 4, y[4], y[5], y[6], y[7]);
-            }
-        }
+    for (int j = 0; j < 8; ++j) y[j] = (float)c[j] * s;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x8 *>(to) = pack8(y);
+    else {
+        store4<T>(to, y[0], y[1], y[2], y[3]);
+        store4<T>(to + 4, y[4], y[5], y[6], y[7]);
     }
 }
 
 template <typename S, typename T, int D> int move(bool write, const MoveArgs &a, hipStream_t st)
 {
-    const long per = NTHREADS / (D / 8) * MOVE_ROWS;
-    const dim3 grid((unsigned)((a.L + per - 1) / per), (unsigned)(a.B * a.Hk));
+    const long per = NTHREADS / (D / 8);
+    const dim3 grid((unsigned)(((long)a.L * a.inner + per - 1) / per), (unsigned)(a.B * a.Hk / a.inner), 2);
     if (write) hipLaunchKernelGGL((cache_write_kernel<S, T, D>), grid, dim3(NTHREADS), 0, st, a);
     else hipLaunchKernelGGL((cache_read_kernel<S, T, D>), grid, dim3(NTHREADS), 0, st, a);
     return hipGetLastError() == hipSuccess ? SKA_OK : SKA_EHIP;
@@ -221,6 +267,8 @@ int move(bool write, const void *K, const ska_strides *k_strides, const void *V,
     a.start = start; a.len = len;
     a.B = B; a.Hk = Hk; a.L = L; a.Lc = Lc;
     a.by_hk = SmDiv::by(Hk);
+    a.inner = Hk > 1 && a.k.h == d && (long)L * Hk * (d / 8) < 1L << 31 ? Hk : 1;   // (fewer than 2^32 threads in a dimension)
+    a.by_inner = SmDiv::by(a.inner);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (store == SKA_E4M3) return dtype == SKA_F32 ? move<E4M3, float>(d, write, a, st) : move<E4M3, __bf16>(d, write, a, st);
     return dtype == SKA_F32 ? move<INT8, float>(d, write, a, st) : move<INT8, __bf16>(d, write, a, st);
