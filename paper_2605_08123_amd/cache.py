@@ -51,7 +51,7 @@ def _lib():
 
 def _scales(x, shape, dev, name):
     """Pointer and strides of [B,Hk,L] scales (no strides: contiguous)."""
-    if x.get_device() != dev or x.shape != shape or x.dtype != torch.float32:
+    if x.get_device() != dev or x.shape != shape or x.dtype is not torch.float32:
         _wrong(x, shape, torch.float32, dev, name)
     if x.is_contiguous():
         return x.data_ptr(), None
@@ -71,6 +71,10 @@ def _store(x, name):
 def _kept(kept, shape, dev, name):
     """The eight pointers of keys and values that are kept as codes (shape: [B,Hk,L,d])."""
     K, V, Ks, Vs = kept
+    if K.is_contiguous() and V.is_contiguous() and Ks.is_contiguous() and Vs.is_contiguous() and \
+            K.get_device() == V.get_device() == Ks.get_device() == Vs.get_device() == dev and K.dtype is V.dtype and \
+            Ks.dtype is Vs.dtype is torch.float32 and K.shape == V.shape == shape and Ks.shape == Vs.shape == shape[:3]:
+        return K.data_ptr(), None, Ks.data_ptr(), None, V.data_ptr(), None, Vs.data_ptr(), None
     kp, ks = _heads(K, shape, K.dtype, dev, f"{name}.K")
     vp, vs = _heads(V, shape, K.dtype, dev, f"{name}.V")
     ksp, kss = _scales(Ks, shape[:3], dev, f"{name}.K_scale")
@@ -112,17 +116,34 @@ def ska_cache_read(cache, L=None, start=None, len_k=None, dtype=torch.bfloat16, 
     B, Hk, Lc, d = _four(cache[0], "cache.K")
     dev, store = _here(cache[0], "cache.K"), _store(cache[0], "cache.K")
     if L is None:
-        L = Lc if K is None else _four(K, "K")[2]
+        L = _four(K, "K")[2] if K is not None else _four(V, "V")[2] if V is not None else Lc
     shape = (B, Hk, L, d)
-    if K is None:
-        K = cache[2].new_empty(shape, dtype=dtype)
-    if V is None:
-        V = cache[2].new_empty(shape, dtype=K.dtype)
-    kp, ks = _heads(K, shape, K.dtype, dev, "K")
-    vp, vs = _heads(V, shape, K.dtype, dev, "V")
+    if K is None and V is None:
+        K, V = cache[2].new_empty(shape, dtype=dtype), cache[2].new_empty(shape, dtype=dtype)
+        kp, ks, vp, vs = K.data_ptr(), None, V.data_ptr(), None
+    else:
+        if K is None:
+            K = V.new_empty(shape)
+        if V is None:
+            V = K.new_empty(shape)
+        kp, ks = _heads(K, shape, K.dtype, dev, "K")
+        vp, vs = _heads(V, shape, K.dtype, dev, "V")
     _done(_lib().ska_cache_read(*_kept(cache, (B, Hk, Lc, d), dev, "cache"), kp, ks, vp, vs, _plain(start, (B,), torch.int32, dev, "start"),
                                 _plain(len_k, (B,), torch.int32, dev, "len_k"), B, Hk, L, Lc, d, _code(K), store, _raw_stream(dev)))
     return K, V
+
+
+# Workspaces by sizes: asking the library costs as much as a check of two tensors
+_needs = {}
+
+
+def _need(f, *sizes):
+    n = _needs.get((f, sizes))
+    if n is None:
+        if len(_needs) > 4096:
+            _needs.clear()
+        n = _needs[f, sizes] = getattr(_lib(), f)(*sizes)
+    return n
 
 
 def ska_cache_attn_workspace_bytes(B, Hq, Hk, Lq, Lc, d, W, causal=False, dtype=1, store=SKA_E4M3) -> int:
@@ -134,19 +155,23 @@ def ska_cache_attn_fwd(Q, cache, W, causal=False, eps=1.0, start_q=None, len_q=N
     """ska_softmax_attn_fwd of Q [B,Hq,Lq,d] (float32 or bfloat16) on a cache in 8 bits (KVCache, or its four tensors).  Returns (O, LSE)."""
     qshape, kshape = _four(Q, "Q"), _four(cache[0], "cache.K")
     B, Hq, Lq, d = qshape
-    Hk, Lc = kshape[1], kshape[2]
-    dev, code, store = _here(Q, "Q"), _code(Q), _store(cache[0], "cache.K")
-    qp, qs = _heads(Q, qshape, Q.dtype, dev, "Q")
+    _, Hk, Lc, _ = kshape
+    dev, dt, code, store = _here(Q, "Q"), Q.dtype, _code(Q), _store(cache[0], "cache.K")
+    qp, qs = _heads(Q, qshape, dt, dev, "Q")
     if O is None:
         O = _like(Q)
-    op, os = _heads(O, qshape, Q.dtype, dev, "O")
+        op, os = O.data_ptr(), None
+    else:
+        op, os = _heads(O, qshape, dt, dev, "O")
     if LSE is None:
         LSE = Q.new_empty((B, Hq, Lq), dtype=torch.float32)
-    lib = _lib()
+        lp = LSE.data_ptr()
+    else:
+        lp = _plain(LSE, (B, Hq, Lq), torch.float32, dev, "LSE")
     W, causal, i32, u8 = _int32(W), 1 if causal else 0, torch.int32, torch.uint8
-    ws, n, keep = _workspace(workspace, lib.ska_cache_attn_workspace_bytes(B, Hq, Hk, Lq, Lc, d, W, causal, code, store), Q, dev)
-    _done(lib.ska_cache_attn_fwd(
-        qp, qs, *_kept(cache, (B, Hk, Lc, d), dev, "cache"), op, os, _plain(LSE, (B, Hq, Lq), torch.float32, dev, "LSE"),
+    ws, n, keep = _workspace(workspace, _need("ska_cache_attn_workspace_bytes", B, Hq, Hk, Lq, Lc, d, W, causal, code, store), Q, dev)
+    _done(_lib().ska_cache_attn_fwd(
+        qp, qs, *_kept(cache, (B, Hk, Lc, d), dev, "cache"), op, os, lp,
         _plain(start_q, (B,), i32, dev, "start_q"), _plain(len_q, (B,), i32, dev, "len_q"), _plain(len_k, (B,), i32, dev, "len_k"),
         _plain(mask_q, (B, Lq), u8, dev, "mask_q"), _plain(mask_k, (B, Lc), u8, dev, "mask_k"), B, Hq, Hk, Lq, Lc, d, W, causal, eps, code, store,
         ws, n, _raw_stream(dev)))
@@ -168,6 +193,22 @@ def _side(kept, shape, Q, dev, name):
     return _kept(kept, shape, dev, name), _store(kept[0], f"{name}.K")
 
 
+def _shared(kept, Hk, Lp, d, Q, dev):
+    """_side of the prefix, whose tensors have no first dimension."""
+    shape, dt = (Hk, Lp, d), Q.dtype
+    if len(kept) == 2:
+        K, V = kept
+        if K.is_contiguous() and V.is_contiguous() and K.get_device() == V.get_device() == dev and K.dtype is V.dtype is dt and K.shape == V.shape == shape:
+            return (K.data_ptr(), None, None, None, V.data_ptr(), None, None, None), _code(Q)
+    elif len(kept) == 4:
+        K, V, Ks, Vs = kept
+        if K.is_contiguous() and V.is_contiguous() and Ks.is_contiguous() and Vs.is_contiguous() and \
+                K.get_device() == V.get_device() == Ks.get_device() == Vs.get_device() == dev and K.dtype is V.dtype and \
+                Ks.dtype is Vs.dtype is torch.float32 and K.shape == V.shape == shape and Ks.shape == Vs.shape == (Hk, Lp):
+            return (K.data_ptr(), None, Ks.data_ptr(), None, V.data_ptr(), None, Vs.data_ptr(), None), _store(K, "prefix.K")
+    return _side([x.unsqueeze(0) for x in kept], (1, Hk, Lp, d), Q, dev, "prefix")
+
+
 def ska_prefix_attn_fwd(Q, prefix, own, W, causal=True, eps=1.0, len_p=None, start_q=None, len_q=None, len_k=None, mask_q=None, mask_k=None,
                         mask_p=None, O=None, LSE=None, workspace=None):
     """Softmax attention of Q [B,Hq,Lq,d] on a prefix that all items share, [Hk,Lp,d], and on each item's own keys behind it,
@@ -176,26 +217,30 @@ def ska_prefix_attn_fwd(Q, prefix, own, W, causal=True, eps=1.0, len_p=None, sta
     arguments as in ska_softmax_attn_fwd; mask_p: uint8 [Lp].  Returns (O, LSE)."""
     qshape, kshape = _four(Q, "Q"), _four(own[0], "own.K")
     B, Hq, Lq, d = qshape
-    Hk, Lk = kshape[1], kshape[2]
-    dev, code = _here(Q, "Q"), _code(Q)
+    _, Hk, Lk, _ = kshape
+    dev, dt, code = _here(Q, "Q"), Q.dtype, _code(Q)
     if prefix[0].dim() != 3:
         raise ValueError(f"prefix.K: expected [Hk, Lp, d], got {tuple(prefix[0].shape)}")
     Lp = prefix[0].shape[1]
-    before, store = _side([x.unsqueeze(0) for x in prefix], (1, Hk, Lp, d), Q, dev, "prefix")
+    before, store = _shared(prefix, Hk, Lp, d, Q, dev)
     behind, other = _side(own, (B, Hk, Lk, d), Q, dev, "own")
     if store != other or len(prefix) != len(own):
         raise ValueError("prefix and own: expected the same kind of storage")
-    qp, qs = _heads(Q, qshape, Q.dtype, dev, "Q")
+    qp, qs = _heads(Q, qshape, dt, dev, "Q")
     if O is None:
         O = _like(Q)
-    op, os = _heads(O, qshape, Q.dtype, dev, "O")
+        op, os = O.data_ptr(), None
+    else:
+        op, os = _heads(O, qshape, dt, dev, "O")
     if LSE is None:
         LSE = Q.new_empty((B, Hq, Lq), dtype=torch.float32)
-    lib = _lib()
+        lp = LSE.data_ptr()
+    else:
+        lp = _plain(LSE, (B, Hq, Lq), torch.float32, dev, "LSE")
     W, causal, i32, u8 = _int32(W), 1 if causal else 0, torch.int32, torch.uint8
-    ws, n, keep = _workspace(workspace, lib.ska_prefix_attn_workspace_bytes(B, Hq, Hk, Lq, Lp, Lk, d, W, causal, code, store), Q, dev)
-    _done(lib.ska_prefix_attn_fwd(
-        qp, qs, *before, *behind, op, os, _plain(LSE, (B, Hq, Lq), torch.float32, dev, "LSE"), _plain(len_p, (1,), i32, dev, "len_p"),
+    ws, n, keep = _workspace(workspace, _need("ska_prefix_attn_workspace_bytes", B, Hq, Hk, Lq, Lp, Lk, d, W, causal, code, store), Q, dev)
+    _done(_lib().ska_prefix_attn_fwd(
+        qp, qs, *before, *behind, op, os, lp, _plain(len_p, (1,), i32, dev, "len_p"),
         _plain(start_q, (B,), i32, dev, "start_q"), _plain(len_q, (B,), i32, dev, "len_q"), _plain(len_k, (B,), i32, dev, "len_k"),
         _plain(mask_q, (B, Lq), u8, dev, "mask_q"), _plain(mask_k, (B, Lk), u8, dev, "mask_k"), _plain(mask_p, (Lp,), u8, dev, "mask_p"),
         B, Hq, Hk, Lq, Lp, Lk, d, W, causal, eps, code, store, ws, n, _raw_stream(dev)))
