@@ -253,9 +253,15 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
     __shared__ __align__(16) _Float16 halves[NW][HALF ? 32 : 4];       // HALF: values' next to the unit
     __shared__ int row_at[16 * NQ], row_live[16 * NQ], reach[2];
 
-    const bool prefix = (int)blockIdx.x >= a.side[0].wgs;
+    // both sides' workgroups in turn, eight of each, while there are any: one waits for memory while the other computes
+    int id = (int)blockIdx.x;
+    const int both = min(a.side[0].wgs, a.side[1].wgs);
+    bool prefix = id - both >= a.side[0].wgs;
+    if (id < 2 * both) {
+        prefix = id >> 3 & 1;
+        id = (id >> 4) * 8 + (id & 7);
+    } else id -= both;
     const CaSide &s = a.side[prefix ? 1 : 0];
-    const int id = (int)blockIdx.x - (prefix ? a.side[0].wgs : 0);
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), x = lane & 15, g = lane >> 4;
     int prob, part, blk;
     if (s.order == CA_NEIGHBOURS) {

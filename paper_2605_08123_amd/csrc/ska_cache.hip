@@ -310,13 +310,18 @@ CaGrid ca_grid(const CaProblem &p, int nq, bool prefix)
     const long reach = std::min(L, prefix ? (long)p.W : std::min(unit_rows / p.G() + 1, (long)p.Lq) + (p.causal ? 1L : 2L) * p.W);
     g.order = prefix || g.blocks <= 8 || reach < L / 2 ? CA_NEIGHBOURS : CA_LAST_FIRST;
     const long tile = p.store == SKA_F32 ? 16 : 32, tiles = (reach + tile - 1) / tile;
-    const long room = (nq == 1 && p.d < 128 ? 4096 : 2048) / nw, least = 2;   // workgroups
-    long own = 0;   // of the items' own keys, beside a prefix
+    const long room = (nq == 1 && p.d < 128 ? 4096 : 2048) / nw;   // workgroups at a time
+    // Two tiles to a wavefront at least; four where a prefix's workgroups run beside: more parts only have to be joined (32 tokens of 1024
+    // behind 65536, bf16: 29 us, 31 with two).  The prefix takes the room that the items' own workgroups leave, or if these take more than
+    // half of it all of it, in turn with them (64 tokens of 2048 behind 16384, int8, d = 128: 55 us, 64 with half of it).
+    const long least = p.Lp && !prefix ? 4 : 2;
+    long space = room;
     if (prefix) {
         const CaGrid o = ca_grid(p, nq, false);
-        own = std::min(room / 2, o.blocks * o.parts * p.B * p.Hk);
+        const long own = o.blocks * o.parts * p.B * p.Hk;
+        if (own <= room / 2) space = room - own;
     }
-    g.parts = (int)std::max(1L, std::min({(p.Lp && !prefix ? room / 2 : room - own) / (g.blocks * problems), tiles / (least * nw), 256L}));
+    g.parts = (int)std::max(1L, std::min({space / (g.blocks * problems), tiles / (least * nw), 256L}));
     return g;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
