@@ -239,9 +239,9 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
     constexpr bool HALF = ST::BYTES == 1 && sizeof(T) == 2, ONES = HALF || ST::BYTES == 2;
     constexpr int PP = HALF ? 1 : sizeof(T) == 4 ? 3 : 2;
     constexpr float BIAS = HALF ? 4.f : 0.f;
-    // Powers of two that a row's maximum may grow by before its sums are scaled to it: fp16 ends at 2^16, and P keeps its bits down to 2^-18;
-    // the others lose nothing, and leave room for large values
-    constexpr float MANY = HALF ? 11.9f : 16.f;
+    // What the sum over a tile (ONES) or a lane's exponent may come to before a row's maximum is moved to its scores: fp16 is infinite from
+    // 2^16 on, so that a maximum may grow by 2^12, and P keeps its bits down to 2^-18; the others lose nothing, and leave room for large values
+    constexpr float MANY = HALF ? 3e6f : ONES ? 65536.f : 16.f;
     union Lds {
         uint4 q[NQ][QL::PIECES][64];
         float red[NW][16 * NQ][PITCH];
@@ -461,14 +461,14 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
         const bool whole = on == FULL && j0 >= all_lo && j0 + KT - 1 <= all_hi;
         bool even = true;   // HALF: the values' scales are fp16 numbers next to the unit
         if constexpr (ST::SCALED) {   // from a key per lane to the four of its accumulators
-            const bool ok = on >> (lane & 31) & 1;
-            float rel = ok ? tl.vs : 0.f;
+            float rel = tl.vs;
+            if (__builtin_expect(on != FULL, 0)) rel = on >> (lane & 31) & 1 ? rel : 0.f;
             if constexpr (HALF) {
-                float v = rel <= 0x1p127f ? rel : 0.f;
-                if (__builtin_expect(__any(v > unit), 0)) {   // (at the first tile, and where a value is larger than all before)
+                if (__builtin_expect(__any(rel > unit), 0)) {   // (at the first tile, and where a value is larger than all before)
+                    float v = rel <= 0x1p127f ? rel : 0.f;
 #pragma unroll
                     for (int d = 1; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-                    const unsigned bits = (__float_as_uint(v) + 0x7fffffu) & 0x7f800000u;   // the next power of two
+                    const unsigned bits = (__float_as_uint(fmaxf(v, unit)) + 0x7fffffu) & 0x7f800000u;   // the next power of two
                     const float u = __uint_as_float((unsigned)__builtin_amdgcn_readfirstlane((int)bits)), f = unit / u;
                     unit = u;
                     inv = 1.f / u;   // (exact, a subnormal number at the end)
@@ -478,8 +478,9 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
                         for (int j = 0; j < F; ++j) acc[nb][j] *= f;
                 }
                 rel *= inv;
-                even = __all(!ok || (rel >= 0x1p-14f && rel <= 1.f));
-                if (lane < 32) halves[wv][lane] = even ? (_Float16)rel : (_Float16)0;
+                even = __all(rel >= 0x1p-14f && rel <= 1.f);
+                if (__builtin_expect(!even, 0)) even = __all(!(on >> (lane & 31) & 1) || (rel >= 0x1p-14f && rel <= 1.f));
+                halves[wv][lane & 31] = even ? (_Float16)rel : (_Float16)0;
             }
             scales[wv][lane] = lane < 32 ? tl.ks * c2 : rel;
         }
@@ -518,42 +519,20 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
                         for (int w = 0; w < (TL::VB < 4 ? 1 : TL::VB / 4); ++w) tl.v[n][e][w] = mine >> (16 * n + e) & 1 ? tl.v[n][e][w] : 0u;
             }
         } else keys = ~0u;
-        float p[NB][4 * NT];
+        float p[NB][4 * NT], much[NB];
         bf16x8 pf[NB][PP];
         f16x8 ph[NB];
-        float down[NB];
-        bool moved = false;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) down[nb] = 1.f;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            // The running maximum moves when a score of any lane exceeds it by MANY: lanes are compared with no exchange between them
-            float top;
+        // P of a block from its scores; ONES: as operands, and the tile's sum (of two bf16 numbers the second is NaN where P is infinite),
+        // else a lane's largest exponent
+        auto probabilities = [&](int nb) __attribute__((always_inline)) -> float {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) p[nb][4 * n + e] = fmaf(sc[nb][n][e], kc[n][e], BIAS - m[nb]);
-            top = p[nb][0];
+            float top = p[nb][0];
+            if constexpr (!ONES) {
 #pragma unroll
-            for (int e = 1; e < 4 * NT; ++e) top = fmaxf(top, p[nb][e]);
-            if (__builtin_expect(__any(top > BIAS + MANY), 0)) {
-                top = -INFINITY;
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        sc[nb][n][e] *= kc[n][e];
-                        top = fmaxf(top, sc[nb][n][e]);
-                    }
-                const float mn = fmaxf(m[nb], ca_max_groups(top));
-                down[nb] = fast_exp2(m[nb] - mn);
-                m[nb] = mn;
-                sum[nb] *= down[nb];
-                moved = true;
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) p[nb][4 * n + e] = sc[nb][n][e] + (BIAS - mn);
+                for (int e = 1; e < 4 * NT; ++e) top = fmaxf(top, p[nb][e]);
             }
 #pragma unroll
             for (int e = 0; e < 4 * NT; ++e) p[nb][e] = fast_exp2(p[nb][e]);
@@ -561,22 +540,41 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
                 const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) ph[nb][e] = (_Float16)p[nb][e];
-                sum[nb] += __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph[nb], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0)[0];
+                return __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph[nb], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0)[0];
             } else if constexpr (ONES) {
                 const bf16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
                 f32x4 y = {0.f, 0.f, 0.f, 0.f};
                 split(pf[nb], p[nb]);
 #pragma unroll
                 for (int h = PP - 1; h >= 0; --h) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[nb][h], y, 0, 0, 0);
-                sum[nb] += y[0];
-            } else sum[nb] += sum_of(p[nb]);
-        }
-        if (__builtin_expect(moved, 0)) {
+                return y[0];
+            } else return top;
+        };
+        __builtin_amdgcn_s_setprio(1);   // (of a SIMD's two wavefronts the one in these instructions goes first, the other's products meanwhile)
+        bool fits = true;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb) much[nb] = probabilities(nb);
 #pragma unroll
-                for (int j = 0; j < F; ++j) acc[nb][j] *= down[nb];
+        for (int nb = 0; nb < NB; ++nb) fits = fits && (ST::BYTES == 2 ? much[nb] <= MANY : !(much[nb] > MANY));
+        if (__builtin_expect(!__all(fits), 0)) {   // a row's maximum moves: lanes are compared with no exchange between them before
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[nb][n][e] * kc[n][e]);
+                const float mn = fmaxf(m[nb], ca_max_groups(top)), f = fast_exp2(m[nb] - mn);
+                m[nb] = mn;
+                sum[nb] *= f;
+#pragma unroll
+                for (int j = 0; j < F; ++j) acc[nb][j] *= f;
+                much[nb] = probabilities(nb);
+            }
         }
+        __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) sum[nb] += ONES ? much[nb] : sum_of(p[nb]);
         if constexpr (ST::BYTES == 4) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
