@@ -721,29 +721,40 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
     }
 }
 
-// Joins the parts of a row: weighted by exp(their LSE - the largest).  A thread takes four features over every slices-th part; parts
-// without a key are not read.
+// Joins the parts of a row: weighted by exp(their LSE - the largest).  A thread takes four features over every slices-th part, four parts
+// asked for at a time (a part without a key has LSE = -inf and zeros); the slices are joined by LDS in their order.
 template <typename T, int D> __global__ __launch_bounds__(NTHREADS) void ca_join_kernel(const CaArgs a, int slices)
 {
-    constexpr int FT = D / 4;
+    constexpr int FT = D / 4, U = 4;
     __shared__ f32x4 sx[NTHREADS];
     __shared__ float sm[NTHREADS], sl[NTHREADS];
     const int R = a.Lq * a.G, f = (threadIdx.x % FT) * 4, rest = threadIdx.x / FT, slice = rest % slices;
-    const long rows = (long)a.B * a.Hk * R, row = (long)blockIdx.x * (NTHREADS / FT / slices) + rest / slices;
+    const long rows = (long)a.B * a.Hk * R, row = (long)blockIdx.x * (NTHREADS / FT / slices) + rest / slices, from = min(row, rows - 1);
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    if (row < rows) {
-#pragma unroll 4
-        for (int s = slice; s < a.parts; s += slices) {
-            const float lse = a.part_lse[s * rows + row];
-            if (lse == -INFINITY) continue;
-            const f32x4 y = *reinterpret_cast<const f32x4 *>(a.part + (s * rows + row) * D + f);
-            // (fmaxf passes over a NaN, so that m never is one; c is, and l and x from there on)
-            const float mn = fmaxf(m, lse), old = m > -INFINITY ? fast_exp2((m - mn) * LOG2E) : 0.f, c = fast_exp2((lse - mn) * LOG2E);
-            l = fmaf(l, old, c);
-            x = x * old + y * c;
-            m = mn;
+    float m = CA_LEAST, l = 0.f;
+    for (int s0 = slice; s0 < a.parts; s0 += U * slices) {
+        f32x4 y[U];
+        float lse[U], top = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = min(s0 + u * slices, a.parts - 1);
+            lse[u] = a.part_lse[s * rows + from];
+            y[u] = *reinterpret_cast<const f32x4 *>(a.part + (s * rows + from) * D + f);
+            if (s0 + u * slices >= a.parts) lse[u] = -INFINITY;
         }
+        // (fmaxf passes over a NaN, so that m never is one; a weight is, and l and x from there on)
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = fmaxf(top, lse[u]);
+        const float old = fast_exp2((m - top) * LOG2E);
+        l *= old;
+        x *= old;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float c = lse[u] == -INFINITY ? 0.f : fast_exp2((lse[u] - top) * LOG2E);
+            l += c;
+            x += y[u] * c;
+        }
+        m = top;
     }
     if (slices > 1) {
         sx[threadIdx.x] = x;
@@ -751,19 +762,24 @@ template <typename T, int D> __global__ __launch_bounds__(NTHREADS) void ca_join
         sl[threadIdx.x] = l;
         __syncthreads();
         if (slice) return;
+        float top = m;
+        for (int s = 1; s < slices; ++s) top = fmaxf(top, sm[threadIdx.x + s * FT]);
+        const float c0 = fast_exp2((m - top) * LOG2E);
+        l *= c0;
+        x *= c0;
         for (int s = 1; s < slices; ++s) {
             const int o = threadIdx.x + s * FT;
-            const float mo = sm[o], lo = sl[o];
-            const float mn = fmaxf(m, mo), old = m > -INFINITY ? fast_exp2((m - mn) * LOG2E) : 1.f, c = mo > -INFINITY ? fast_exp2((mo - mn) * LOG2E) : 1.f;
-            l = l * old + lo * c;   // (a slice that has met nothing but NaN has m = -inf and l = NaN)
-            x = x * old + sx[o] * c;
-            m = mn;
+            const float c = fast_exp2((sm[o] - top) * LOG2E);
+            l = fmaf(sl[o], c, l);
+            x += sx[o] * c;
         }
+        m = top;
     }
     if (row >= rows) return;
     const int prob = (int)(row / R), r = (int)(row - (long)prob * R), b = a.by_hk(prob), hk = prob - b * a.Hk;
     const CaRow w = ca_row(a, false, b, hk, r);
-    if (m == SM_NOTHING) l = NAN;   // (keys, whose scores are all -inf)
+    // A row with keys whose scores are all -inf has parts of SM_NOTHING and no others: l counts them, and they are 0 / 0
+    if (m == SM_NOTHING && l > 0.f) l = NAN;
     const float c = l == 0.f ? 0.f : 1.f / l;
     store4<T>(reinterpret_cast<T *>(const_cast<void *>(a.o.p)) + w.b * a.o.b + w.hq * a.o.h + w.i * a.o.l + f, x[0] * c, x[1] * c, x[2] * c, x[3] * c);
     if (f == 0) a.lse[((long)b * a.Hk * a.G + w.hq) * a.Lq + w.i] = l == 0.f ? -INFINITY : m + fast_log2(l) * LN2;
