@@ -58,11 +58,18 @@ int ska_cache_read(const void *Kc, const ska_strides *kc_strides, const float *K
  * Softmax attention (ska_softmax_attn_fwd: band, positions, lengths, masks, rows without a key, NaN) on a cache in 8 bits:
  *   S_ij = <Q_i, c_j> s_j / (eps sqrt d),  LSE_i = log sum_j exp(S_ij),  O_i = sum_j exp(S_ij - LSE_i) s'_j c'_j.
  *   Q, O [B,Hq,Lq,d] of type `dtype`; Kc, Vc [B,Hk,Lc,d] codes of type `store`, Ks, Vs scales; LSE [B,Hq,Lq] fp32.
- *   Codes are exact in bf16; products with queries and with probabilities are accumulated in fp32.  bf16 queries are taken as they
- *   are and exp(S - LSE) s' as the sum of two bf16 numbers (2^-16 relative), fp32 ones as three (all their bits, and 2^-24).
- *   Places of the cache beyond the lengths, inactive, or that no active query of the item reaches by position may hold anything.
- *   A token in reach whose value row is NaN (or a product exp(S - LSE) s' beyond fp32) is in O of the queries around it too.
- *   Limits, alignment and workspace as ska_softmax_attn_fwd (codes: multiples of 16 bytes); scales on any 4 bytes.
+ *   Codes are exact in bf16 and fp16, products with queries and with probabilities are accumulated in fp32.
+ *   fp32 queries are taken as the sum of three bf16 numbers (all their bits), and so is exp(S - LSE) s' (2^-24 relative).
+ *   bf16 queries are taken as they are.  exp(S - m), m near the row's largest S, is rounded to fp16 (2^-11 relative; absolute 2^-29 of
+ *   1 below 2^-18, so that keys with less weight than that add nothing), and LSE is that of the rounded numbers.  Values' scales
+ *   are fp16 numbers next to a power of two, and their products with it rounded to fp16 again (3 2^-11 in all); where values' scales
+ *   of 32 adjacent tokens differ by more than 2^14, the products are sums of two bf16 numbers (2^-16) instead.
+ *   Places of the cache beyond the lengths or inactive may hold anything, and so may those that no query of the item reaches by
+ *   position (inactive ones reach as well).  A token that is reached whose value row is NaN (or a product exp(S - LSE) s' beyond
+ *   fp32) is in O of the queries around it too.
+ *   Limits, alignment and workspace as ska_softmax_attn_fwd (codes: multiples of 16 bytes); scales on any 4 bytes.  Instead of its
+ *   2^24 blocks of 128 rows: fewer than 2^23 - 8 blocks of 64 query rows of a problem (32 with fp32 queries or d = 128), B Hk problems
+ *   of Lq (Hq / Hk) rows (SKA_EUNSUPPORTED otherwise).
  *   The same query can differ by roundings between calls of other sizes; the same call repeats its bits.
  */
 size_t ska_cache_attn_workspace_bytes(int B, int Hq, int Hk, int Lq, int Lc, int d, int W, int causal, int dtype, int store);
@@ -79,9 +86,10 @@ int ska_cache_attn_fwd(const void *Q, const ska_strides *q_strides, const void *
  * both; the prefix is read once for the queries of all items.
  *   Kp, Vp [Hk,Lp,d] (of their strides, h and l count), K, V [B,Hk,Lk,d]: all of type `store`, which is `dtype` (scales NULL) or an
  *   8-bit one (scales Kps, Vps, Ks, Vs).  mask_p [Lp]: uint8, nonzero = active, or NULL.  The other arguments as above.
- *   Places of the prefix that no active query of any item reaches, beyond P or inactive may hold anything.
- *   fp32 caches: products in fp32.  bf16: exp(S - LSE) as the sum of two bf16 numbers.
- *   1 <= Lp, Lk <= 2^24 (an item without tokens of its own: len_k 0), B * Lq * (Hq / Hk) <= 2^27 (SKA_EUNSUPPORTED otherwise).
+ *   Places of the prefix beyond P or inactive may hold anything, and so may those that no query of any item reaches by position.
+ *   fp32 caches: products in fp32.  bf16: exp(S - m) as the sum of two bf16 numbers (2^-16).  Codes: as above.
+ *   1 <= Lp, Lk <= 2^24 (an item without tokens of its own: len_k 0), B * Lq * (Hq / Hk) <= 2^27; the prefix's blocks, of Hk
+ *   problems of B Lq (Hq / Hk) rows, count with the items' own (SKA_EUNSUPPORTED otherwise).
  */
 size_t ska_prefix_attn_workspace_bytes(int B, int Hq, int Hk, int Lq, int Lp, int Lk, int d, int W, int causal, int dtype,
                                        int store);

@@ -3,13 +3,13 @@
 //
 // A wavefront holds up to NQ blocks of 16 query rows and walks over tiles of keys:
 //   S^T = K Q^T  (16x16x32 products, keys as rows),  P = exp(S - m),  O^T += V^T P^T.
-// Nothing passes through LDS on the way: the operand layouts are met by the loads.
+// The queries' operands lie in LDS, read again for each tile; keys and values do not pass through it: the operand layouts are met by the loads.
 //   K: lane (x, g) = (lane & 15, lane >> 4) has 16 adjacent bytes of token x: the features that a product sums over may come in any order, so
 //      these are whole operands, and 4 lanes read 64 adjacent bytes of a row.
 //   V: the second product sums over tokens.  Lane (x, g) reads features x F ... x F + F - 1 (F = d / 16) of the tokens 4 g ... 4 g + 3 of each tile:
 //      the tokens whose P this lane has in the accumulators' layout, and F products' operands of 8 tokens after a transposition of bytes
 //      inside the lane.  Product j gives features x F + j, so that a lane ends up with d / 4 adjacent features of a row.
-// Codes in 8 bits are exact in bf16.  A key's scale is a factor of its score, a value's scale one of its P.
+// Codes in 8 bits are exact in bf16 and in fp16.  A key's scale is a factor of its score, a value's scale one of its P.
 #pragma once
 #include "ska_softmax.h"
 

@@ -281,18 +281,6 @@ struct CaProblem {
     long R() const { return (long)Lq * G(); }
     long rows() const { return (long)B * Hk * R(); }
 };
-int check(const CaProblem &p, bool prefix)
-{
-    if (p.B < 1 || p.Hq < 1 || p.Hk < 1 || p.Lq < 1 || p.Lk < 1 || p.W < 0 || p.Hq % p.Hk || (prefix && p.Lp < 1)) return SKA_EINVAL;
-    if (p.d != 32 && p.d != 64 && p.d != 128) return SKA_EUNSUPPORTED;
-    if (p.dtype != SKA_F32 && p.dtype != SKA_BF16) return SKA_EUNSUPPORTED;
-    if (!scaled(p.store) && !(prefix && p.store == p.dtype)) return SKA_EUNSUPPORTED;
-    if (p.Lq > 1 << 24 || p.Lk > 1 << 24 || p.Lp > 1 << 24 || (long)p.B * p.Hk > 65535 || p.R() > 1 << 27) return SKA_EUNSUPPORTED;
-    if (prefix && p.R() * p.B > 1 << 27) return SKA_EUNSUPPORTED;
-    if ((p.R() + 127) / 128 * p.B * p.Hk > (1 << 24) - 8) return SKA_EUNSUPPORTED;   // (fewer than 2^32 threads, as in softmax_attn)
-    return SKA_OK;
-}
-
 // How one side is launched: blocks of rows, parts of a walk, the workgroups' order
 struct CaGrid { long blocks; int parts; int order; };
 int ca_rows_of(const CaProblem &p)
@@ -323,6 +311,23 @@ CaGrid ca_grid(const CaProblem &p, int nq, bool prefix)
     }
     g.parts = (int)std::max(1L, std::min({space / (g.blocks * problems), tiles / (least * nw), 256L}));
     return g;
+}
+int check(const CaProblem &p, bool prefix)
+{
+    if (p.B < 1 || p.Hq < 1 || p.Hk < 1 || p.Lq < 1 || p.Lk < 1 || p.W < 0 || p.Hq % p.Hk || (prefix && p.Lp < 1)) return SKA_EINVAL;
+    if (p.d != 32 && p.d != 64 && p.d != 128) return SKA_EUNSUPPORTED;
+    if (p.dtype != SKA_F32 && p.dtype != SKA_BF16) return SKA_EUNSUPPORTED;
+    if (!scaled(p.store) && !(prefix && p.store == p.dtype)) return SKA_EUNSUPPORTED;
+    if (p.Lq > 1 << 24 || p.Lk > 1 << 24 || p.Lp > 1 << 24 || (long)p.B * p.Hk > 65535 || p.R() > 1 << 27) return SKA_EUNSUPPORTED;
+    if (prefix && p.R() * p.B > 1 << 27) return SKA_EUNSUPPORTED;
+    // Fewer than 2^32 threads with both sides' rounding up to 8 workgroups (a launch is accepted with more, and runs their number modulo 2^32)
+    const int nq = ca_rows_of(p);
+    long wgs = 0;
+    for (int side = 0; side <= (prefix ? 1 : 0); ++side) {
+        const CaGrid g = ca_grid(p, nq, side == 1);
+        wgs += g.blocks * g.parts * (side ? p.Hk : (long)p.B * p.Hk) + 7;
+    }
+    return wgs * 64 * ca_waves(nq, p.d) < 1L << 32 ? SKA_OK : SKA_EUNSUPPORTED;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 int ca_parts(const CaProblem &p, int nq) { return ca_grid(p, nq, false).parts + (p.Lp ? ca_grid(p, nq, true).parts : 0); }
