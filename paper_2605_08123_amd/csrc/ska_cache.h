@@ -459,7 +459,7 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
         unsigned on = sm_bits(0, hi - j0) & FULL;
         if (mk) on &= (unsigned)__ballot(tl.act != 0);   // (lanes 0 ... 31: keys 0 ... 31)
         const bool whole = on == FULL && j0 >= all_lo && j0 + KT - 1 <= all_hi;
-        bool even = true;   // HALF: the values' scales are fp16 numbers next to the unit
+        bool even = true;   // HALF: the values' scales are taken as fp16 numbers next to the unit
         if constexpr (ST::SCALED) {   // from a key per lane to the four of its accumulators
             float rel = tl.vs;
             if (__builtin_expect(on != FULL, 0)) rel = on >> (lane & 31) & 1 ? rel : 0.f;
@@ -478,8 +478,9 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
                         for (int j = 0; j < F; ++j) acc[nb][j] *= f;
                 }
                 rel *= inv;
-                even = __all(rel >= 0x1p-14f && rel <= 1.f);
-                if (__builtin_expect(!even, 0)) even = __all(!(on >> (lane & 31) & 1) || (rel >= 0x1p-14f && rel <= 1.f));
+                // (P times a scale is rounded to a multiple of 2^-24, with P in 2^-4: 2^-19 of a value by itself at 2^-9 of the unit)
+                even = __all(rel >= 0x1p-9f && rel <= 1.f);
+                if (__builtin_expect(!even, 0)) even = __all(!(on >> (lane & 31) & 1) || (rel >= 0x1p-9f && rel <= 1.f));
                 halves[wv][lane & 31] = even ? (_Float16)rel : (_Float16)0;
             }
             scales[wv][lane] = lane < 32 ? tl.ks * c2 : rel;
