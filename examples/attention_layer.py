@@ -4,7 +4,7 @@
 
 with the paper's banded Sinkhorn attention or softmax attention on the same band, forward and backward by hand (the library has
 no autograd functions; projections are plain matrix products), and the softmax layer's form for single tokens against a
-cache.  Run on a GPU: python examples/attention_layer.py
+cache, which may be held in 8 bits and stand behind a prompt that all sequences share.  Run on a GPU: python examples/attention_layer.py
 """
 import argparse
 import os
@@ -71,17 +71,26 @@ class AttentionLayer:
         dx, grads["norm"], grads["norm_bias"] = ska.ska_layer_norm_bwd(dqkv @ p["qkv"].t(), S, p["norm"], stats, dS=dS)
         return dx, grads
 
-    def token(self, x, r, cache, length):
-        """One more token per sequence (softmax, causal): x, r [B, 1, D]; cache: keys and values [B, Hk, L, d], of which length [B]
-        (int32) tokens are there and to which this one is appended.  -> output and sum."""
-        p = self.params
+    def token(self, x, r, cache, length, prefix=None):
+        """One more token per sequence, or several (softmax, causal): x, r [B, n, D]; cache: keys and values [B, Hk, L, d], of which length
+        [B] (int32) tokens are there and to which these are appended, or a cache in 8 bits (ska_cache_empty).  prefix: a cache in 8 bits
+        without the first dimension, whose tokens stand before all sequences.  -> output and sum."""
+        p, n = self.params, x.shape[1]
+        at = length if prefix is None else length + prefix.K.shape[1]
         Y, S, _ = ska.ska_layer_norm_fwd(x, p["norm"], p["norm_bias"], residual=r)
         q, k, v = self._heads(Y @ p["qkv"])
-        Q, K = ska.ska_rope_fwd(q, k, self.freq, self.amplitude, start=length)
-        b = torch.arange(x.shape[0], device=x.device)
-        cache[0][b, :, length.long()], cache[1][b, :, length.long()] = K[:, :, 0], v[:, :, 0]
-        O, _ = ska.ska_softmax_attn_fwd(Q, cache[0], cache[1], self.W, True, self.eps, len_k=length + 1, start_q=length)
-        return O.transpose(1, 2).reshape(x.shape[0], 1, -1) @ p["out"], S
+        Q, K = ska.ska_rope_fwd(q, k, self.freq, self.amplitude, start=at)
+        if isinstance(cache, ska.KVCache):
+            ska.ska_cache_write(cache, K, v, start=length)
+            if prefix is None:
+                O, _ = ska.ska_cache_attn_fwd(Q, cache, self.W, True, self.eps, start_q=length, len_k=length + n)
+            else:
+                O, _ = ska.ska_prefix_attn_fwd(Q, prefix, cache, self.W, True, self.eps, start_q=length, len_k=length + n)
+        else:
+            b, i = torch.arange(x.shape[0], device=x.device)[:, None], length.long()[:, None] + torch.arange(n, device=x.device)
+            cache[0][b, :, i], cache[1][b, :, i] = K.transpose(1, 2), v.transpose(1, 2)
+            O, _ = ska.ska_softmax_attn_fwd(Q, cache[0], cache[1], self.W, True, self.eps, len_k=length + n, start_q=length)
+        return O.transpose(1, 2).reshape(x.shape[0], n, -1) @ p["out"], S
 
 
 def train(kind, steps=12, B=2, L=1024, D=256, H=4, d=64, W=128, rate=30.0, seed=1):
@@ -112,14 +121,24 @@ def main():
     B, L = 3, 40
     x, r = (torch.randn((B, L, 256), generator=g, device="cuda").bfloat16() for _ in range(2))
     whole, _, _ = layer.forward(x, r)
-    cache = [torch.zeros((B, 2, L, 64), device="cuda", dtype=torch.bfloat16) for _ in range(2)]
-    length = torch.zeros(B, device="cuda", dtype=torch.int32)
-    off = 0.0
-    for t in range(L):
-        out, _ = layer.token(x[:, t:t + 1], r[:, t:t + 1], cache, length)
-        length += 1
-        off = max(off, (out[:, 0].float() - whole[:, t].float()).abs().max().item())
-    print(f"token by token against all at once: largest difference {off:.4f} (outputs of size {whole.float().abs().mean().item():.2f})")
+    zero = torch.zeros(B, device="cuda", dtype=torch.int32)
+    size = whole.float().abs().mean().item()
+
+    def answer(cache, prefix=None, begin=0):
+        off = 0.0
+        for t in range(begin, L):
+            out, _ = layer.token(x[:, t:t + 1], r[:, t:t + 1], cache, zero + (t - begin), prefix)
+            off = max(off, (out[:, 0].float() - whole[:, t].float()).abs().max().item())
+        return f"largest difference {off:.4f} (outputs of size {size:.2f})"
+    print("token by token against all at once:", answer([torch.zeros((B, 2, L, 64), device="cuda", dtype=torch.bfloat16) for _ in range(2)]))
+    for store in ("e4m3", "int8"):
+        print(f"keys and values in {store}:", answer(ska.ska_cache_empty(B, 2, L, 64, store)))
+        # all sequences begin with the first one's 30 tokens, which are kept once
+        x[:, :30], r[:, :30] = x[:1, :30], r[:1, :30]
+        whole, _, _ = layer.forward(x, r)
+        prompt = ska.ska_cache_empty(1, 2, 30, 64, store)
+        layer.token(x[:1, :30], r[:1, :30], prompt, zero[:1])
+        print(f"behind a shared prompt in {store}:", answer(ska.ska_cache_empty(B, 2, L - 30, 64, store), ska.KVCache(*(y[0] for y in prompt)), 30))
 
 
 if __name__ == "__main__":
