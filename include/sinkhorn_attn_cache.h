@@ -61,7 +61,7 @@ int ska_cache_read(const void *Kc, const ska_strides *kc_strides, const float *K
  *   Codes are exact in bf16 and fp16, products with queries and with probabilities are accumulated in fp32.
  *   fp32 queries are taken as the sum of three bf16 numbers (all their bits), and so is exp(S - LSE) s' (2^-24 relative).
  *   bf16 queries are taken as they are.  exp(S - m), m near the row's largest S, is rounded to fp16 (2^-11 relative; absolute 2^-29
- *   below 2^-18, so that keys with less weight than that add nothing), and LSE is that of the rounded numbers.  Values' scales are
+ *   below 2^-18, so that keys with less weight than that add nothing to O).  Values' scales are
  *   fp16 numbers next to a power of two, and their products with it rounded to fp16 again (3 2^-11 in all; absolute 2^-20 of the
  *   value); in 32 tokens with a scale 2^9 times smaller than a value's before, the products are sums of two bf16 numbers (2^-16).
  *   Values 2^100 times smaller than another that is reached may be lost.

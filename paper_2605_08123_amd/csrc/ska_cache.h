@@ -235,13 +235,14 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
     using QL = CaQuery<S, T, D>;
     constexpr int NW = ca_waves(NQ, D), NT = ST::NT, KT = ST::KT, F = D / 16, PITCH = D + 4;
     // P in fp16 times 2^4 (HALF: codes in 8 bits for bf16 results), as the sum of two bf16 numbers (bf16 caches) or three (codes for fp32
-    // results), in fp32 (fp32 caches).  Sums of the first two are products with ones.
-    constexpr bool HALF = ST::BYTES == 1 && sizeof(T) == 2, ONES = HALF || ST::BYTES == 2;
+    // results), in fp32 (fp32 caches).  Its sums are in fp32: of two bf16 numbers by a product with ones, else of P before it is rounded.
+    constexpr bool HALF = ST::BYTES == 1 && sizeof(T) == 2, ONES = ST::BYTES == 2;
     constexpr int PP = HALF ? 1 : sizeof(T) == 4 ? 3 : 2;
     constexpr float BIAS = HALF ? 4.f : 0.f;
-    // What the sum over a tile (ONES) or a lane's exponent may come to before a row's maximum is moved to its scores: fp16 is infinite from
-    // 2^16 on, so that a maximum may grow by 2^12, and P keeps its bits down to 2^-18; the others lose nothing, and leave room for large values
-    constexpr float MANY = HALF ? 3e6f : ONES ? 65536.f : 16.f;
+    // What the sum over a tile (ONES), a lane's part of it (HALF) or a lane's exponent may come to before a row's maximum is moved to its
+    // scores: fp16 is infinite from 2^16 on, so that a maximum may grow by 2^9 and more, and P keeps its bits down to 2^-18; the others lose
+    // nothing, and leave room for large values
+    constexpr float MANY = HALF ? 65504.f : ONES ? 65536.f : 16.f;
     union Lds {
         uint4 q[NQ][QL::PIECES][64];
         float red[NW][16 * NQ][PITCH];
@@ -523,25 +524,24 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
         float p[NB][4 * NT], much[NB];
         bf16x8 pf[NB][PP];
         f16x8 ph[NB];
-        // P of a block from its scores; ONES: as operands, and the tile's sum (of two bf16 numbers the second is NaN where P is infinite),
-        // else a lane's largest exponent
+        // P of a block from its scores, and what is compared with MANY; ONES, HALF: also as operands (of two bf16 numbers the second is NaN
+        // where P is infinite)
         auto probabilities = [&](int nb) __attribute__((always_inline)) -> float {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) p[nb][4 * n + e] = fmaf(sc[nb][n][e], kc[n][e], BIAS - m[nb]);
             float top = p[nb][0];
-            if constexpr (!ONES) {
+            if constexpr (!ONES && !HALF) {
 #pragma unroll
                 for (int e = 1; e < 4 * NT; ++e) top = fmaxf(top, p[nb][e]);
             }
 #pragma unroll
             for (int e = 0; e < 4 * NT; ++e) p[nb][e] = fast_exp2(p[nb][e]);
             if constexpr (HALF) {
-                const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) ph[nb][e] = (_Float16)p[nb][e];
-                return __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph[nb], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0)[0];
+                return sum_of(p[nb]);
             } else if constexpr (ONES) {
                 const bf16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
                 f32x4 y = {0.f, 0.f, 0.f, 0.f};
@@ -575,7 +575,7 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
         }
         __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) sum[nb] += ONES ? much[nb] : sum_of(p[nb]);
+        for (int nb = 0; nb < NB; ++nb) sum[nb] += ONES || HALF ? much[nb] : sum_of(p[nb]);
         if constexpr (ST::BYTES == 4) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)

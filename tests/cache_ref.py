@@ -88,8 +88,8 @@ def attn(q, k, v, ok, eps, codes=True):
     if q.dtype == torch.bfloat16:
         parts, tiny = (3 * 2.0 ** -11, 2.0 ** -27 * n * vd.abs().amax()) if codes else (half(torch.bfloat16) ** 2, 0.0)
     e_o = (p @ vd.abs()) * (parts + 2 * worst + 3 * n * F32 + 12 * F32) * 1.02 + tiny + half(q.dtype) * o.abs()
-    # (sums of the P that the products take)
-    e_lse = (worst + n * F32 + parts)[..., 0] + 4 * F32 * (lse.abs().nan_to_num(posinf=0.0) + top0[..., 0].abs()) + 4 * F32
+    # (sums of P before it is rounded, or of two bf16 numbers)
+    e_lse = (worst + n * F32 + (F32 if codes else parts))[..., 0] + 4 * F32 * (lse.abs().nan_to_num(posinf=0.0) + top0[..., 0].abs()) + 4 * F32
     return {"O": (o, e_o), "LSE": (lse, e_lse)}
 
 
