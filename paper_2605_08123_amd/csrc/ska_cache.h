@@ -204,11 +204,11 @@ __device__ __forceinline__ float ca_max_groups(float x)   // over the four lanes
 
 // A row of a problem: item, query, head
 struct CaRow { int b, i, hq, at; };   // at: row of (b, hk)'s Lq G
-__device__ __forceinline__ CaRow ca_row(const CaArgs &a, bool prefix, int b, int hk, int r)
+__device__ __forceinline__ CaRow ca_row(const CaArgs &a, bool shared, int b, int hk, int r)
 {
     CaRow w;
-    w.b = prefix ? a.by_r(r) : b;
-    w.at = prefix ? r - w.b * (a.Lq * a.G) : r;
+    w.b = shared ? a.by_r(r) : b;
+    w.at = shared ? r - w.b * (a.Lq * a.G) : r;
     w.i = a.by_g(w.at);
     w.hq = hk * a.G + (w.at - w.i * a.G);
     return w;
@@ -227,7 +227,8 @@ __device__ __forceinline__ float ca_finish(float m, float sum, bool live, bool p
 
 // Wavefronts of a workgroup, which share their rows and split the keys
 constexpr int ca_waves(int nq, int d) { return nq == 1 && d < 128 ? 16 : 8; }
-template <typename S, typename T, int D, int NQ>
+// BOTH: an item's workgroups walk over the prefix too, which has none of its own (its `wgs` is 0)
+template <typename S, typename T, int D, int NQ, bool BOTH>
 __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) void ca_attn_kernel(const CaArgs a)
 {
     using ST = CaStore<S>;
@@ -257,12 +258,12 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
     // both sides' workgroups in turn, eight of each, while there are any: one waits for memory while the other computes
     int id = (int)blockIdx.x;
     const int both = min(a.side[0].wgs, a.side[1].wgs);
-    bool prefix = id - both >= a.side[0].wgs;
-    if (id < 2 * both) {
-        prefix = id >> 3 & 1;
+    bool shared = !BOTH && id - both >= a.side[0].wgs;   // rows of all items, on the prefix's keys
+    if (!BOTH && id < 2 * both) {
+        shared = id >> 3 & 1;
         id = (id >> 4) * 8 + (id & 7);
     } else id -= both;
-    const CaSide &s = a.side[prefix ? 1 : 0];
+    const CaSide &s = a.side[shared ? 1 : 0];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), x = lane & 15, g = lane >> 4;
     int prob, part, blk;
     if (s.order == CA_NEIGHBOURS) {
@@ -274,16 +275,24 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
         const int u = s.by_problems(id), v = s.by_parts(u);
         prob = id - u * s.problems; part = u - v * s.parts; blk = s.blocks - 1 - v;
     }
-    const int b0 = prefix ? 0 : a.by_hk(prob), hk = prefix ? prob : prob - b0 * a.Hk;
+    const int b0 = shared ? 0 : a.by_hk(prob), hk = shared ? prob : prob - b0 * a.Hk;
     const int r0 = blk * (16 * NQ), R1 = a.Lq * a.G;
-    const int P = prefix ? sm_len(s.len, 0, s.L) : 0, up = a.causal ? 0 : a.W;
+    bool front = BOTH || shared;                        // the prefix's keys, which come first, or the items' own
+    const int P = front ? sm_len(a.side[1].len, 0, a.side[1].L) : 0, up = a.causal ? 0 : a.W;
     const int nb_live = min(NQ, (s.rows - r0 + 15) >> 4);   // blocks of rows that exist
 
-    const unsigned char *kb = reinterpret_cast<const unsigned char *>(s.k.p) + (b0 * s.k.b + hk * s.k.h) * ST::BYTES;
-    const unsigned char *vb = reinterpret_cast<const unsigned char *>(s.v.p) + (b0 * s.v.b + hk * s.v.h) * ST::BYTES;
-    const float *ksb = ST::SCALED ? s.ks + b0 * s.ks_b + hk * s.ks_h : nullptr, *vsb = ST::SCALED ? s.vs + b0 * s.vs_b + hk * s.vs_h : nullptr;
-    const unsigned kst = (unsigned)(s.k.l * ST::BYTES), vst = (unsigned)(s.v.l * ST::BYTES);
-    const unsigned char *mk = s.mask ? s.mask + (long)b0 * s.L : nullptr;
+    const unsigned char *kb, *vb, *mk;
+    const float *ksb, *vsb;
+    unsigned kst, vst;
+    auto keys_of = [&](const CaSide &y, int b) __attribute__((always_inline)) {
+        kb = reinterpret_cast<const unsigned char *>(y.k.p) + (b * y.k.b + hk * y.k.h) * ST::BYTES;
+        vb = reinterpret_cast<const unsigned char *>(y.v.p) + (b * y.v.b + hk * y.v.h) * ST::BYTES;
+        ksb = ST::SCALED ? y.ks + b * y.ks_b + hk * y.ks_h : nullptr;
+        vsb = ST::SCALED ? y.vs + b * y.vs_b + hk * y.vs_h : nullptr;
+        kst = (unsigned)(y.k.l * ST::BYTES);
+        vst = (unsigned)(y.v.l * ST::BYTES);
+        mk = y.mask ? y.mask + (long)b * y.L : nullptr;
+    };
 
     // Keys that any, and that all, of the rows reach; tiles of the part, of which this wavefront takes every NW-th.  Of several items' rows
     // (prefix) the starts decide: the first tiles are asked for as if one stood at the prefix's end, where that is not so once more.
@@ -301,33 +310,38 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
             fetch_values(ta, t);
         }
     };
-    const int start0 = a.start && !prefix ? min(max(a.start[b0], 0), 1 << 24) : 0, lq0 = sm_len(a.len_q, b0, a.Lq), lk0 = prefix ? P : sm_len(s.len, b0, s.L);
-    if (prefix) {
-        lo = max(0, P - a.W); hi = P - 1;
-        all_lo = 0; all_hi = hi;
-    } else {
-        const int first = start0 + a.by_g(r0), last = start0 + min(a.by_g(min(r0 + 16 * NQ, s.rows) - 1), lq0 - 1);
-        lo = max(0, first - a.W); hi = last < first ? -1 : min(last + up, lk0 - 1);
-        all_lo = last - a.W; all_hi = min(first + up, lk0 - 1);
-    }
+    const int start0 = a.start && !shared ? min(max(a.start[b0], 0), 1 << 24) : 0, lq0 = sm_len(a.len_q, b0, a.Lq);
+    const int first0 = start0 + a.by_g(r0), last0 = start0 + min(a.by_g(min(r0 + 16 * NQ, s.rows) - 1), lq0 - 1);
+    auto range = [&]() __attribute__((always_inline)) {
+        if (shared) {
+            lo = max(0, P - a.W); hi = P - 1;
+            all_lo = 0; all_hi = hi;
+        } else {
+            const int off = front ? P : 0, end = front ? P - 1 : sm_len(s.len, b0, s.L) - 1;   // (all queries stand behind the prefix)
+            lo = max(0, off + first0 - a.W); hi = last0 < first0 ? -1 : front ? end : min(last0 + up, end);
+            all_lo = off + last0 - a.W; all_hi = front ? end : min(first0 + up, end);
+        }
+    };
+    keys_of(a.side[front ? 1 : 0], front ? 0 : b0);
+    range();
     begin();
 
     // the rows' operands, positions and whether they take part, into LDS; rows that do not are zeros, so that what they hold decides nothing
     for (int i = wv; i < NQ * QL::STEPS; i += NW) {
         const int n = i / QL::STEPS, r = r0 + 16 * n + x;
-        const CaRow w = ca_row(a, prefix, b0, hk, min(r, s.rows - 1));
-        bool on = r < s.rows && w.i < (prefix ? sm_len(a.len_q, w.b, a.Lq) : lq0);
+        const CaRow w = ca_row(a, shared, b0, hk, min(r, s.rows - 1));
+        bool on = r < s.rows && w.i < (shared ? sm_len(a.len_q, w.b, a.Lq) : lq0);
         if (a.mask_q) on = on && a.mask_q[(long)w.b * a.Lq + w.i] != 0;
         QL::put(&lds.q[n][0][lane], reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + w.hq * a.q.h + w.i * a.q.l, i - n * QL::STEPS, g, on);
     }
     if (wv == 0) {   // (16 NQ rows at most: one wavefront has them all)
         const int r = r0 + lane;
-        const CaRow w = ca_row(a, prefix, b0, hk, min(r, s.rows - 1));
-        const int lq = prefix ? sm_len(a.len_q, w.b, a.Lq) : lq0, start = prefix && a.start ? min(max(a.start[w.b], 0), 1 << 24) : start0;
+        const CaRow w = ca_row(a, shared, b0, hk, min(r, s.rows - 1));
+        const int lq = shared ? sm_len(a.len_q, w.b, a.Lq) : lq0, start = shared && a.start ? min(max(a.start[w.b], 0), 1 << 24) : start0;
         bool on = lane < 16 * NQ && r < s.rows && w.i < lq;
-        const int p = P + start + w.i;
-        if (prefix) {
-            int first = on ? p - a.W : 0x7fffffff, last = on ? p - a.W : 0;
+        const int p = start + w.i;
+        if (shared) {
+            int first = on ? P + p - a.W : 0x7fffffff, last = on ? P + p - a.W : 0;
 #pragma unroll
             for (int d = 1; d < 16 * NQ; d <<= 1) first = min(first, __shfl_xor(first, d)), last = max(last, __shfl_xor(last, d));
             if (lane == 0) reach[0] = first, reach[1] = last;
@@ -336,7 +350,7 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
         if (lane < 16 * NQ) row_at[lane] = p, row_live[lane] = on;
     }
     __syncthreads();
-    if (prefix) {
+    if (shared) {
         const int first = max(0, __builtin_amdgcn_readfirstlane(reach[0]));
         all_lo = __builtin_amdgcn_readfirstlane(reach[1]);
         if (first != lo) {
@@ -499,8 +513,8 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
         if (__builtin_expect(!whole, 0)) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                const int at = row_at[16 * nb + x] - j0;
-                const unsigned mine = sm_bits(at - a.W, prefix ? 31 : at + up) & on, keep = mine >> (4 * g);
+                const int at = row_at[16 * nb + x] + (front ? P : 0) - j0;
+                const unsigned mine = sm_bits(at - a.W, front ? 31 : at + up) & on, keep = mine >> (4 * g);
                 if (mine) keys |= 1u << nb;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -650,11 +664,21 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
             tile(which, ta);
         }
     };
-    if (nb_live <= 1) walk(std::integral_constant<int, 1>{});
+    if constexpr (BOTH) {
+#pragma unroll 1
+        for (;;) {
+            walk(std::integral_constant<int, NQ>{});
+            if (!front) break;
+            front = false;
+            keys_of(s, b0);
+            range();
+            begin();
+        }
+    } else if (nb_live <= 1) walk(std::integral_constant<int, 1>{});
     else walk(std::integral_constant<int, NQ>{});
 
     const long rows = (long)a.B * a.Hk * a.Lq * a.G;
-    const int slot = part + (prefix ? a.side[0].parts : 0);
+    const int slot = part + (shared ? a.side[0].parts : 0);
     // four adjacent features of a row, from feature f on
     auto put = [&](const CaRow &w, int f, const f32x4 &y) {
         if (a.parts > 1) *reinterpret_cast<f32x4 *>(a.part + ((slot * rows + ((long)w.b * a.Hk + hk) * (a.Lq * a.G) + w.at) * D + f)) = y;
@@ -714,7 +738,7 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
             L = fmaf(red_l[k][row], c, L);
             y += *reinterpret_cast<const f32x4 *>(&lds.red[k][row][f]) * c;
         }
-        const CaRow w = ca_row(a, prefix, b0, hk, r0 + row);
+        const CaRow w = ca_row(a, shared, b0, hk, r0 + row);
         float lse;
         const float scale = ca_finish(M, L, any, a.parts > 1, lse);
         put(w, f, any ? y * scale : f32x4{0.f, 0.f, 0.f, 0.f});

@@ -283,22 +283,33 @@ struct CaProblem {
 };
 // How one side is launched: blocks of rows, parts of a walk, the workgroups' order
 struct CaGrid { long blocks; int parts; int order; };
-int ca_rows_of(const CaProblem &p)
+int ca_rows_for(const CaProblem &p, long rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : ca_most(p.dtype == SKA_F32, p.d); }
+int ca_tile(const CaProblem &p) { return p.store == SKA_F32 ? 16 : 32; }
+long ca_room(const CaProblem &p, int nq) { return (nq == 1 && p.d < 128 ? 4096 : 2048) / ca_waves(nq, p.d); }   // workgroups at a time
+// Keys that a block of an item's rows reaches at most
+long ca_reach(const CaProblem &p, int nq)
 {
-    const long rows = p.Lp ? p.R() * p.B : p.R();
-    const int most = ca_most(p.dtype == SKA_F32, p.d);
-    return rows <= 16 ? 1 : rows <= 32 ? 2 : most;
+    return std::min((long)p.Lk, std::min(16L * nq / p.G() + 1, (long)p.Lq) + (p.causal ? 1L : 2L) * p.W);
 }
+// Whether an item's workgroups take the prefix too: one launch and nothing to join, but the prefix is read by each.  Few rows, all workgroups
+// at a time, and a wavefront's walk short (30 items, 4 heads on each of 2, together and apart: e4m3, d = 64, 30 tokens behind 500 8.7 and
+// 14.9 us, 100 behind 2000 12.3 and 15.8, behind 8000 23.8 and 16.8; fp32, d = 128, 30 behind 500 17.0 and 19.7, 100 behind 1000 27.7 and 23.8)
+bool ca_together(const CaProblem &p)
+{
+    if (!p.Lp || p.R() > 16 || (long)p.B * p.Hk > ca_room(p, 1)) return false;
+    return std::min(p.Lp, p.W) + ca_reach(p, 1) <= (scaled(p.store) ? 5L : 4L) * ca_tile(p) * ca_waves(1, p.d);
+}
+int ca_rows_of(const CaProblem &p) { return ca_rows_for(p, p.Lp && !ca_together(p) ? p.R() * p.B : p.R()); }
 CaGrid ca_grid(const CaProblem &p, int nq, bool prefix)
 {
     const long rows = prefix ? p.R() * p.B : p.R(), problems = prefix ? p.Hk : (long)p.B * p.Hk, L = prefix ? p.Lp : p.Lk;
     const long unit_rows = 16 * nq, nw = ca_waves(nq, p.d);
+    const bool together = ca_together(p);
     CaGrid g;
     g.blocks = (rows + unit_rows - 1) / unit_rows;
-    const long reach = std::min(L, prefix ? (long)p.W : std::min(unit_rows / p.G() + 1, (long)p.Lq) + (p.causal ? 1L : 2L) * p.W);
+    const long reach = prefix ? std::min(L, (long)p.W) : ca_reach(p, nq);
     g.order = prefix || g.blocks <= 8 || reach < L / 2 ? CA_NEIGHBOURS : CA_LAST_FIRST;
-    const long tile = p.store == SKA_F32 ? 16 : 32, tiles = (reach + tile - 1) / tile;
-    const long room = (nq == 1 && p.d < 128 ? 4096 : 2048) / nw;   // workgroups at a time
+    const long tile = ca_tile(p), tiles = (reach + tile - 1) / tile, room = ca_room(p, nq);
     // Two tiles to a wavefront at least; four where a prefix's workgroups run beside: more parts only have to be joined (32 tokens of 1024
     // behind 65536, bf16: 29 us, 31 with two).  The prefix takes the room that the items' own workgroups leave, or if these take more than
     // half of it all of it, in turn with them (64 tokens of 2048 behind 16384, int8, d = 128: 55 us, 64 with half of it).
@@ -309,6 +320,7 @@ CaGrid ca_grid(const CaProblem &p, int nq, bool prefix)
         const long own = o.blocks * o.parts * p.B * p.Hk;
         if (own <= room / 2) space = room - own;
     }
+    if (together) space = g.blocks * problems;
     g.parts = (int)std::max(1L, std::min({space / (g.blocks * problems), tiles / (least * nw), 256L}));
     return g;
 }
@@ -323,14 +335,14 @@ int check(const CaProblem &p, bool prefix)
     // Fewer than 2^32 threads with both sides' rounding up to 8 workgroups (a launch is accepted with more, and runs their number modulo 2^32)
     const int nq = ca_rows_of(p);
     long wgs = 0;
-    for (int side = 0; side <= (prefix ? 1 : 0); ++side) {
+    for (int side = 0; side <= (prefix && !ca_together(p) ? 1 : 0); ++side) {
         const CaGrid g = ca_grid(p, nq, side == 1);
         wgs += g.blocks * g.parts * (side ? p.Hk : (long)p.B * p.Hk) + 7;
     }
     return wgs * 64 * ca_waves(nq, p.d) < 1L << 32 ? SKA_OK : SKA_EUNSUPPORTED;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-int ca_parts(const CaProblem &p, int nq) { return ca_grid(p, nq, false).parts + (p.Lp ? ca_grid(p, nq, true).parts : 0); }
+int ca_parts(const CaProblem &p, int nq) { return ca_grid(p, nq, false).parts + (p.Lp && !ca_together(p) ? ca_grid(p, nq, true).parts : 0); }
 size_t ws_lse(const CaProblem &p, int parts) { return up256((size_t)parts * p.rows() * sizeof(float)); }
 size_t ws_bytes(const CaProblem &p)
 {
@@ -370,7 +382,7 @@ void place(CaSide &s, const CaProblem &p, int nq, const CaGrid &g, bool prefix)
     s.by_parts = SmDiv::by(s.parts);
     s.by_span = SmDiv::by(s.parts * ca_waves(nq, p.d));
 }
-typedef int (*Launch)(int, const void *, hipStream_t);
+typedef int (*Launch)(int, bool, const void *, hipStream_t);
 #define BY_D(NAME) {NAME##_32, NAME##_64, NAME##_128}
 constexpr Launch LAUNCH[6][3] = {BY_D(ska_launch_cache_f32_f32), BY_D(ska_launch_cache_bf16_bf16), BY_D(ska_launch_cache_e4m3_f32),
                                  BY_D(ska_launch_cache_e4m3_bf16), BY_D(ska_launch_cache_int8_f32), BY_D(ska_launch_cache_int8_bf16)};
@@ -407,9 +419,10 @@ int attn(const CaProblem &p, const void *Q, const ska_strides *q_strides, const 
     a.by_hk = SmDiv::by(a.Hk);
     a.by_r = SmDiv::by((unsigned)p.R());
     place(a.side[0], p, nq, ca_grid(p, nq, false), false);
-    if (prefix) place(a.side[1], p, nq, ca_grid(p, nq, true), true);
+    const bool both = ca_together(p);
+    if (prefix && !both) place(a.side[1], p, nq, ca_grid(p, nq, true), true);
     const int at = p.store == SKA_F32 ? 0 : p.store == SKA_BF16 ? 1 : (p.store == SKA_E4M3 ? 2 : 4) + (p.dtype == SKA_BF16);
-    return LAUNCH[at][p.d == 32 ? 0 : p.d == 64 ? 1 : 2](nq, &a, static_cast<hipStream_t>(stream));
+    return LAUNCH[at][p.d == 32 ? 0 : p.d == 64 ? 1 : 2](nq, both, &a, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace

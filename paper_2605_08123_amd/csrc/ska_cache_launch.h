@@ -4,8 +4,9 @@
 
 #include "ska_cache.h"
 
-// nq: blocks of 16 query rows of a wavefront, 1, 2 or 4; args: CaArgs.  Joins the parts where there are several.
-#define SKA_DECLARE_CACHE(NAME) extern "C" __attribute__((visibility("hidden"))) int NAME(int nq, const void *args, hipStream_t st)
+// nq: blocks of 16 query rows of a wavefront, 1, 2 or 4; both: an item's workgroups take the prefix too (nq 1); args: CaArgs.  Joins the
+// parts where there are several.
+#define SKA_DECLARE_CACHE(NAME) extern "C" __attribute__((visibility("hidden"))) int NAME(int nq, bool both, const void *args, hipStream_t st)
 #define SKA_DECLARE_CACHE_D(NAME) SKA_DECLARE_CACHE(NAME##_32); SKA_DECLARE_CACHE(NAME##_64); SKA_DECLARE_CACHE(NAME##_128)
 SKA_DECLARE_CACHE_D(ska_launch_cache_f32_f32);
 SKA_DECLARE_CACHE_D(ska_launch_cache_bf16_bf16);

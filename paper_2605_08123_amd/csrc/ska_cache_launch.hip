@@ -3,13 +3,14 @@
 #include "ska_cache_launch.h"
 
 namespace {
-template <typename S, typename T, int D> int launch(int nq, const CaArgs &a, hipStream_t st)
+template <typename S, typename T, int D> int launch(int nq, bool both, const CaArgs &a, hipStream_t st)
 {
     constexpr int MOST = ca_most(sizeof(T) == 4, D);
     const dim3 grid((unsigned)(a.side[0].wgs + a.side[1].wgs));
-    if (nq == 1) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 1>), grid, dim3(64 * ca_waves(1, D)), 0, st, a);
-    else if (nq == 2) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 2>), grid, dim3(64 * ca_waves(2, D)), 0, st, a);
-    else hipLaunchKernelGGL((ca_attn_kernel<S, T, D, MOST>), grid, dim3(64 * ca_waves(MOST, D)), 0, st, a);
+    if (both) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 1, true>), grid, dim3(64 * ca_waves(1, D)), 0, st, a);
+    else if (nq == 1) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 1, false>), grid, dim3(64 * ca_waves(1, D)), 0, st, a);
+    else if (nq == 2) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 2, false>), grid, dim3(64 * ca_waves(2, D)), 0, st, a);
+    else hipLaunchKernelGGL((ca_attn_kernel<S, T, D, MOST, false>), grid, dim3(64 * ca_waves(MOST, D)), 0, st, a);
     if (hipGetLastError() != hipSuccess) return SKA_EHIP;
     if (a.parts > 1) {
         const int threads = D / 4;
@@ -23,4 +24,4 @@ template <typename S, typename T, int D> int launch(int nq, const CaArgs &a, hip
 }
 }  // namespace
 
-SKA_DECLARE_CACHE(SKA_NAME) { return launch<SKA_S, SKA_T, SKA_D>(nq, *static_cast<const CaArgs *>(args), st); }
+SKA_DECLARE_CACHE(SKA_NAME) { return launch<SKA_S, SKA_T, SKA_D>(nq, both, *static_cast<const CaArgs *>(args), st); }

@@ -82,12 +82,12 @@ def test_attention_refusals():
     # keys and values in the queries' type are for the prefix operator; elsewhere softmax_attn takes them
     for t in (F32, BF16):
         assert _attn(lib, False, dt=t, store=t, ksc=None, vsc=None) == EUNSUPPORTED
-    # many keys for few queries: parts, and a workspace; a prefix has one always
+    # many keys for few queries: parts, and a workspace
     need = ska.ska_cache_attn_workspace_bytes(1, 4, 2, 1, 65536, 64, 1 << 20, True)
     assert need > 0
     for kw in (dict(ws=None), dict(n=need - 1)):
         assert _attn(lib, False, Lq=1, Lk=65536, W=1 << 20, **kw) == EWORKSPACE
-    assert ska.ska_prefix_attn_workspace_bytes(1, 4, 2, 1, 64, 64, 64, 8) > 0 and f(ws=None) == EWORKSPACE
+    assert ska.ska_prefix_attn_workspace_bytes(1, 4, 2, 1, 65536, 64, 64, 1 << 20) > 0 and f(Lq=1, Lp=65536, W=1 << 20, ws=None) == EWORKSPACE
     assert ska.ska_cache_attn_workspace_bytes(1, 4, 2, 1, 65536, 48, 8) == 0 and ska.ska_prefix_attn_workspace_bytes(1, 4, 2, 1, 0, 64, 64, 8) == 0
 
 

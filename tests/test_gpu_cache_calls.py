@@ -32,7 +32,7 @@ def test_refusals_of_the_binding():
     c = ska.ska_cache_empty(2, 2, 40, 64)
     i8 = ska.ska_cache_empty(2, 2, 40, 64, "int8")
     pre, ipre = ska.KVCache(*(x[0] for x in c)), ska.KVCache(*(x[0] for x in i8))
-    n = ints(1, 2).cuda()
+    n, long = ints(1, 2).cuda(), ska.ska_cache_empty(2, 2, 20000, 64)
     for n_th, call in enumerate((
             lambda: ska.ska_cache_write(c, k, v[:, :, :39]),
             lambda: ska.ska_cache_write(c, k, v.float()),
@@ -59,7 +59,7 @@ def test_refusals_of_the_binding():
             lambda: ska.ska_cache_attn_fwd(q, c, -1),
             lambda: ska.ska_cache_attn_fwd(q, c, 4, eps=0.0),
             lambda: ska.ska_cache_attn_fwd(q, c, 4, O=q[:, :2]),
-            lambda: ska.ska_prefix_attn_fwd(q, pre, c, ALL, workspace=torch.empty(8, dtype=torch.uint8, device="cuda")),
+            lambda: ska.ska_cache_attn_fwd(q, long, ALL, workspace=torch.empty(8, dtype=torch.uint8, device="cuda")),
             lambda: ska.ska_prefix_attn_fwd(q, pre, i8, 4),
             lambda: ska.ska_prefix_attn_fwd(q, ipre, c, 4),
             lambda: ska.ska_prefix_attn_fwd(q, pre, (k, v), 4),
