@@ -473,7 +473,7 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
         const int j0 = lo + t * KT;
         unsigned on = sm_bits(0, hi - j0) & FULL;
         if (mk) on &= (unsigned)__ballot(tl.act != 0);   // (lanes 0 ... 31: keys 0 ... 31)
-        const bool whole = on == FULL && j0 >= all_lo && j0 + KT - 1 <= all_hi;
+        const bool inside = j0 >= all_lo && j0 + KT - 1 <= all_hi;   // of all rows' reach
         bool even = true;   // HALF: the values' scales are taken as fp16 numbers next to the unit
         if constexpr (ST::SCALED) {   // from a key per lane to the four of its accumulators
             float rel = tl.vs;
@@ -510,7 +510,7 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
         SM_READ_FIRST();
         float kc[NT][4];
         key_factors(kc);
-        if (__builtin_expect(!whole, 0)) {
+        if (__builtin_expect(!inside, 0)) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 const int at = row_at[16 * nb + x] + (front ? P : 0) - j0;
@@ -525,16 +525,21 @@ __global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) v
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) kc[n][e] = 1.f;
-            if (on != FULL) {   // what does not count must not meet a product: P is 0 there, and may be 0 times anything
-                const unsigned mine = on >> (4 * g);
+        } else if (on) keys = ~0u;
+        if (__builtin_expect(on != FULL, 0)) {   // what does not count must not meet a product: P is 0 there, and may be 0 times anything
+            const unsigned mine = on >> (4 * g);
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e) {
+                    const bool y = mine >> (16 * n + e) & 1;
+                    kc[n][e] = y ? kc[n][e] : 1.f;
 #pragma unroll
-                        for (int w = 0; w < (TL::VB < 4 ? 1 : TL::VB / 4); ++w) tl.v[n][e][w] = mine >> (16 * n + e) & 1 ? tl.v[n][e][w] : 0u;
-            }
-        } else keys = ~0u;
+                    for (int nb = 0; nb < NB; ++nb) sc[nb][n][e] = y ? sc[nb][n][e] : none;
+#pragma unroll
+                    for (int w = 0; w < (TL::VB < 4 ? 1 : TL::VB / 4); ++w) tl.v[n][e][w] = y ? tl.v[n][e][w] : 0u;
+                }
+        }
         float p[NB][4 * NT], much[NB];
         bf16x8 pf[NB][PP];
         f16x8 ph[NB];
