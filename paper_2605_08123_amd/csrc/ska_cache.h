@@ -238,6 +238,7 @@ __device__ __forceinline__ CaRow ca_row(const CaArgs &a, bool shared, int b, int
     return w;
 }
 
+constexpr int CA_WAVES = 8;   // of a workgroup: they share their rows and split the keys
 constexpr float CA_LEAST = -3.402823466e38f;   // a running maximum before the first score
 
 // Results of a row from its running maximum (powers of two), sum and whether it has met a key: factor of the accumulators, LSE
@@ -249,16 +250,14 @@ __device__ __forceinline__ float ca_finish(float m, float sum, bool live, bool p
     return nothing && parts ? 0.f : 1.f / sum;
 }
 
-// Wavefronts of a workgroup, which share their rows and split the keys
-constexpr int ca_waves(int nq, int d) { return nq == 1 && d < 128 ? 16 : 8; }
 // BOTH: an item's workgroups walk over the prefix too, which has none of its own (its `wgs` is 0)
 template <typename S, typename T, int D, int NQ, bool BOTH>
-__global__ __launch_bounds__(64 * ca_waves(NQ, D), NQ == 1 && D < 128 ? 4 : 2) void ca_attn_kernel(const CaArgs a)
+__global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_attn_kernel(const CaArgs a)
 {
     using ST = CaStore<S>;
     using TL = CaTile<S, D>;
     using QL = CaQuery<S, T, D>;
-    constexpr int NW = ca_waves(NQ, D), NT = ST::NT, KT = ST::KT, F = D / 16, PITCH = D + 4;
+    constexpr int NW = CA_WAVES, NT = ST::NT, KT = ST::KT, F = D / 16, PITCH = D + 4;
     // P in fp16 times 2^4 (HALF: codes in 8 bits for bf16 results), as the sum of two bf16 numbers (bf16 caches) or three (codes for fp32
     // results), in fp32 (fp32 caches).  Its sums are in fp32: of two bf16 numbers by a product with ones, else of P before it is rounded.
     constexpr bool HALF = ST::BYTES == 1 && sizeof(T) == 2, ONES = ST::BYTES == 2;

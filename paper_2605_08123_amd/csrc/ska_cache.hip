@@ -283,45 +283,50 @@ struct CaProblem {
 };
 // How one side is launched: blocks of rows, parts of a walk, the workgroups' order
 struct CaGrid { long blocks; int parts; int order; };
-int ca_rows_for(const CaProblem &p, long rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : ca_most(p.dtype == SKA_F32, p.d); }
+// Blocks of rows of a workgroup.  One block in workgroups of its own registers gains nothing (a token of 4 items on 65536 keys in e4m3,
+// d = 64: 20.2 us, 20.8 with two; 128 items on 4000: 27.2 and 27.4)
+int ca_rows_for(const CaProblem &p, long rows) { return rows <= 32 ? 2 : ca_most(p.dtype == SKA_F32, p.d); }
 int ca_tile(const CaProblem &p) { return p.store == SKA_F32 ? 16 : 32; }
-long ca_room(const CaProblem &p, int nq) { return (nq == 1 && p.d < 128 ? 4096 : 2048) / ca_waves(nq, p.d); }   // workgroups at a time
+// Workgroups at a time, one on each CU (a token of 8 items, 4 key heads of d = 128 on 32768 in int8: 60 us, with half of them 79, with twice
+// as many 64; eight wavefronts each, and not 16 with half the parts: short caches would wait for the join, 3000 tokens 11.2 us and 12.8)
+constexpr long CA_ROOM = 256;
 // Keys that a block of an item's rows reaches at most
 long ca_reach(const CaProblem &p, int nq)
 {
     return std::min((long)p.Lk, std::min(16L * nq / p.G() + 1, (long)p.Lq) + (p.causal ? 1L : 2L) * p.W);
 }
 // Whether an item's workgroups take the prefix too: one launch and nothing to join, but the prefix is read by each.  Few rows, all workgroups
-// at a time, and a wavefront's walk short (30 items, 4 heads on each of 2, together and apart: e4m3, d = 64, 30 tokens behind 500 8.7 and
-// 14.9 us, 100 behind 2000 12.3 and 15.8, behind 8000 23.8 and 16.8; fp32, d = 128, 30 behind 500 17.0 and 19.7, 100 behind 1000 27.7 and 23.8)
+// at a time, and a walk of five tiles a wavefront at most (4 heads on each key head, together and apart; 30 items, 2 key heads: e4m3, d = 64,
+// 30 tokens behind 500 7.7 and 14.9 us, 100 behind 1000 8.8 and 14.9; int8, d = 128, 100 behind 2000 19.6 and 18.0; fp32, d = 128, 30 behind
+// 500 17.1 and 19.9; one item, 1 key head: 7.1 and 9.1, 8.3 and 9.7, 18.8 and 13.8, 16.3 and 13.7)
 bool ca_together(const CaProblem &p)
 {
-    if (!p.Lp || p.R() > 16 || (long)p.B * p.Hk > ca_room(p, 1)) return false;
-    return std::min(p.Lp, p.W) + ca_reach(p, 1) <= (scaled(p.store) ? 5L : 4L) * ca_tile(p) * ca_waves(1, p.d);
+    if (!p.Lp || p.R() > 16 || (long)p.B * p.Hk > CA_ROOM) return false;
+    return std::min(p.Lp, p.W) + ca_reach(p, 1) <= 5L * ca_tile(p) * CA_WAVES;
 }
-int ca_rows_of(const CaProblem &p) { return ca_rows_for(p, p.Lp && !ca_together(p) ? p.R() * p.B : p.R()); }
+int ca_rows_of(const CaProblem &p) { return ca_together(p) ? 1 : ca_rows_for(p, p.Lp ? p.R() * p.B : p.R()); }
 CaGrid ca_grid(const CaProblem &p, int nq, bool prefix)
 {
     const long rows = prefix ? p.R() * p.B : p.R(), problems = prefix ? p.Hk : (long)p.B * p.Hk, L = prefix ? p.Lp : p.Lk;
-    const long unit_rows = 16 * nq, nw = ca_waves(nq, p.d);
+    const long unit_rows = 16 * nq;
     const bool together = ca_together(p);
     CaGrid g;
     g.blocks = (rows + unit_rows - 1) / unit_rows;
     const long reach = prefix ? std::min(L, (long)p.W) : ca_reach(p, nq);
     g.order = prefix || g.blocks <= 8 || reach < L / 2 ? CA_NEIGHBOURS : CA_LAST_FIRST;
-    const long tile = ca_tile(p), tiles = (reach + tile - 1) / tile, room = ca_room(p, nq);
+    const long tile = ca_tile(p), tiles = (reach + tile - 1) / tile;
     // Two tiles to a wavefront at least; four where a prefix's workgroups run beside: more parts only have to be joined (32 tokens of 1024
     // behind 65536, bf16: 29 us, 31 with two).  The prefix takes the room that the items' own workgroups leave, or if these take more than
     // half of it all of it, in turn with them (64 tokens of 2048 behind 16384, int8, d = 128: 55 us, 64 with half of it).
     const long least = p.Lp && !prefix ? 4 : 2;
-    long space = room;
+    long space = CA_ROOM;
     if (prefix) {
         const CaGrid o = ca_grid(p, nq, false);
         const long own = o.blocks * o.parts * p.B * p.Hk;
-        if (own <= room / 2) space = room - own;
+        if (own <= CA_ROOM / 2) space = CA_ROOM - own;
     }
     if (together) space = g.blocks * problems;
-    g.parts = (int)std::max(1L, std::min({space / (g.blocks * problems), tiles / (least * nw), 256L}));
+    g.parts = (int)std::max(1L, std::min({space / (g.blocks * problems), tiles / (least * CA_WAVES), 256L}));
     return g;
 }
 int check(const CaProblem &p, bool prefix)
@@ -339,7 +344,7 @@ int check(const CaProblem &p, bool prefix)
         const CaGrid g = ca_grid(p, nq, side == 1);
         wgs += g.blocks * g.parts * (side ? p.Hk : (long)p.B * p.Hk) + 7;
     }
-    return wgs * 64 * ca_waves(nq, p.d) < 1L << 32 ? SKA_OK : SKA_EUNSUPPORTED;
+    return wgs * 64 * CA_WAVES < 1L << 32 ? SKA_OK : SKA_EUNSUPPORTED;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 int ca_parts(const CaProblem &p, int nq) { return ca_grid(p, nq, false).parts + (p.Lp && !ca_together(p) ? ca_grid(p, nq, true).parts : 0); }
@@ -368,7 +373,7 @@ int side_of(CaSide &s, const CaKept &c, int B, int Hk, int L, int d, int store)
     s.vs = v.p; s.vs_b = v.b; s.vs_h = v.h;
     return SKA_OK;
 }
-void place(CaSide &s, const CaProblem &p, int nq, const CaGrid &g, bool prefix)
+void place(CaSide &s, const CaProblem &p, const CaGrid &g, bool prefix)
 {
     s.rows = (int)(prefix ? p.R() * p.B : p.R());
     s.problems = prefix ? p.Hk : p.B * p.Hk;
@@ -380,7 +385,7 @@ void place(CaSide &s, const CaProblem &p, int nq, const CaGrid &g, bool prefix)
     s.by_problems = SmDiv::by(s.problems);
     s.by_blocks = SmDiv::by(s.blocks);
     s.by_parts = SmDiv::by(s.parts);
-    s.by_span = SmDiv::by(s.parts * ca_waves(nq, p.d));
+    s.by_span = SmDiv::by(s.parts * CA_WAVES);
 }
 typedef int (*Launch)(int, bool, const void *, hipStream_t);
 #define BY_D(NAME) {NAME##_32, NAME##_64, NAME##_128}
@@ -418,9 +423,9 @@ int attn(const CaProblem &p, const void *Q, const ska_strides *q_strides, const 
     a.by_g = SmDiv::by(a.G);
     a.by_hk = SmDiv::by(a.Hk);
     a.by_r = SmDiv::by((unsigned)p.R());
-    place(a.side[0], p, nq, ca_grid(p, nq, false), false);
+    place(a.side[0], p, ca_grid(p, nq, false), false);
     const bool both = ca_together(p);
-    if (prefix && !both) place(a.side[1], p, nq, ca_grid(p, nq, true), true);
+    if (prefix && !both) place(a.side[1], p, ca_grid(p, nq, true), true);
     const int at = p.store == SKA_F32 ? 0 : p.store == SKA_BF16 ? 1 : (p.store == SKA_E4M3 ? 2 : 4) + (p.dtype == SKA_BF16);
     return LAUNCH[at][p.d == 32 ? 0 : p.d == 64 ? 1 : 2](nq, both, &a, static_cast<hipStream_t>(stream));
 }

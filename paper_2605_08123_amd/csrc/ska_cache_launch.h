@@ -4,7 +4,7 @@
 
 #include "ska_cache.h"
 
-// nq: blocks of 16 query rows of a wavefront, 1, 2 or 4; both: an item's workgroups take the prefix too (nq 1); args: CaArgs.  Joins the
+// nq: blocks of 16 query rows of a wavefront, 2 or 4; both: an item's workgroups take the prefix too (nq 1); args: CaArgs.  Joins the
 // parts where there are several.
 #define SKA_DECLARE_CACHE(NAME) extern "C" __attribute__((visibility("hidden"))) int NAME(int nq, bool both, const void *args, hipStream_t st)
 #define SKA_DECLARE_CACHE_D(NAME) SKA_DECLARE_CACHE(NAME##_32); SKA_DECLARE_CACHE(NAME##_64); SKA_DECLARE_CACHE(NAME##_128)
@@ -15,5 +15,5 @@ SKA_DECLARE_CACHE_D(ska_launch_cache_e4m3_bf16);
 SKA_DECLARE_CACHE_D(ska_launch_cache_int8_f32);
 SKA_DECLARE_CACHE_D(ska_launch_cache_int8_bf16);
 
-// Most blocks of rows that a wavefront has registers for
+// Most blocks of rows that a wavefront has registers for (2048 tokens of 8 heads on 2, 16384 keys in e4m3, d = 64: 4 blocks 96 us, 2 119)
 constexpr int ca_most(bool wide_query, int d) { return wide_query || d == 128 ? 2 : 4; }

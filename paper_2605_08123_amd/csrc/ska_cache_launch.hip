@@ -7,10 +7,9 @@ template <typename S, typename T, int D> int launch(int nq, bool both, const CaA
 {
     constexpr int MOST = ca_most(sizeof(T) == 4, D);
     const dim3 grid((unsigned)(a.side[0].wgs + a.side[1].wgs));
-    if (both) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 1, true>), grid, dim3(64 * ca_waves(1, D)), 0, st, a);
-    else if (nq == 1) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 1, false>), grid, dim3(64 * ca_waves(1, D)), 0, st, a);
-    else if (nq == 2) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 2, false>), grid, dim3(64 * ca_waves(2, D)), 0, st, a);
-    else hipLaunchKernelGGL((ca_attn_kernel<S, T, D, MOST, false>), grid, dim3(64 * ca_waves(MOST, D)), 0, st, a);
+    if (both) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 1, true>), grid, dim3(64 * CA_WAVES), 0, st, a);
+    else if (nq == 2) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 2, false>), grid, dim3(64 * CA_WAVES), 0, st, a);
+    else hipLaunchKernelGGL((ca_attn_kernel<S, T, D, MOST, false>), grid, dim3(64 * CA_WAVES), 0, st, a);
     if (hipGetLastError() != hipSuccess) return SKA_EHIP;
     if (a.parts > 1) {
         const int threads = D / 4;
