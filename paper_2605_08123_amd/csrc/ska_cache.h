@@ -1,15 +1,23 @@
 // Softmax attention on caches for gfx950 (sinkhorn_attn_cache.h): keys and values in 8 bits, bf16 or fp32, and a prefix that the items
 // of a batch share.
 //
-// A wavefront holds up to NQ blocks of 16 query rows and walks over tiles of keys:
+// A wavefront holds NQ blocks of 16 query rows and walks over tiles of keys:
 //   S^T = K Q^T  (16x16x32 products, keys as rows),  P = exp(S - m),  O^T += V^T P^T.
-// The queries' operands lie in LDS, read again for each tile; keys and values do not pass through it: the operand layouts are met by the loads.
+// Eight wavefronts of a workgroup have the same rows and take every eighth tile each; their sums are joined in LDS at the end, parts of a
+// walk in other workgroups by ca_join_kernel.  The queries' operands lie in LDS, read again for each tile; keys and values go straight from memory
+// into registers (bf16 rows of 256 bytes by way of LDS), where the operand layouts are met by the loads:
 //   K: lane (x, g) = (lane & 15, lane >> 4) has 16 adjacent bytes of token x: the features that a product sums over may come in any order, so
 //      these are whole operands, and 4 lanes read 64 adjacent bytes of a row.
 //   V: the second product sums over tokens.  Lane (x, g) reads features x F ... x F + F - 1 (F = d / 16) of the tokens 4 g ... 4 g + 3 of each tile:
 //      the tokens whose P this lane has in the accumulators' layout, and F products' operands of 8 tokens after a transposition of bytes
 //      inside the lane.  Product j gives features x F + j, so that a lane ends up with d / 4 adjacent features of a row.
 // Codes in 8 bits are exact in bf16 and in fp16.  A key's scale is a factor of its score, a value's scale one of its P.
+//
+// What bounds it, in us of the kernel alone: few rows, memory (a token of 8 items, 16 heads on 4 of d = 128, int8 caches of 32768: 46, 4.5 TB/s; four
+// items, 8 heads on 2 of d = 64, e4m3, 65536: 15.7, 3.4 TB/s, of which about 5 are the first loads' and the last sums' latency).  Many rows,
+// vector instructions (2048 tokens of 8 heads on 2, d = 64, 16384 keys in e4m3: 71; a wavefront issues 207 of
+// them beside the 32 products of a tile of 32 keys and 64 rows: 128 for P, 48 that turn codes into operands; they take 55 % of the time, products
+// 24 %, with two wavefronts to a SIMD).  One look at a tile decides for all blocks whether a maximum moves (a maximum per tile and block: 81).
 #pragma once
 #include "ska_softmax.h"
 
@@ -41,7 +49,8 @@ struct CaSide {
     SmDiv by_problems, by_blocks, by_parts, by_span;   // problems, blocks, parts, parts * wavefronts of a workgroup
 };
 // Order of the workgroups.  Blocks of the same keys next to each other and a contiguous piece of them per XCD (workgroups go to the XCDs
-// in turn): few blocks, a prefix, a band.  Many blocks that walk over most of the keys: those with the longest walks first, problems fastest.
+// in turn): few blocks, a prefix, a band.  Many blocks that walk over most of the keys: those with the longest walks first, problems fastest
+// (4096 tokens of 2 items, 8 heads on 2, causal, e4m3, d = 64: 78 us, and 100 as neighbours; 16 heads on 2, int8, d = 128: 178 and 258).
 enum CaOrder { CA_NEIGHBOURS, CA_LAST_FIRST };
 struct CaArgs {
     SmTensor q, o;
