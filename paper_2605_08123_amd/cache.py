@@ -9,7 +9,7 @@ from typing import NamedTuple
 import torch
 
 from .binding import load
-from .layer import (_code, _done, _f, _heads, _here, _i, _int32, _like, _ll, _plain, _raw_stream, _sz, _vp, _workspace, _wrong)
+from .layer import (_code, _done, _f, _heads, _here, _i, _int32, _ll, _plain, _raw_stream, _sz, _vp, _workspace, _wrong)
 
 SKA_E4M3, SKA_INT8 = 2, 3
 CACHE_STORES = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
@@ -91,6 +91,11 @@ def ska_cache_empty(B, Hk, L, d, store="e4m3", device=None) -> KVCache:
     return KVCache(*codes, *(torch.empty((B, Hk, L), dtype=torch.float32, device=device) for _ in range(2)))
 
 
+def _queries(Q, qshape, dev):
+    """_heads of a tensor that is checked against nothing but its own shape."""
+    return (Q.data_ptr(), None) if Q.is_contiguous() else _heads(Q, qshape, Q.dtype, dev, "Q")
+
+
 def _four(x, name):
     if x.dim() != 4:
         raise ValueError(f"{name}: expected [B, H, L, d], got {tuple(x.shape)}")
@@ -119,7 +124,8 @@ def ska_cache_read(cache, L=None, start=None, len_k=None, dtype=torch.bfloat16, 
         L = _four(K, "K")[2] if K is not None else _four(V, "V")[2] if V is not None else Lc
     shape = (B, Hk, L, d)
     if K is None and V is None:
-        K, V = cache[2].new_empty(shape, dtype=dtype), cache[2].new_empty(shape, dtype=dtype)
+        K = cache[2].new_empty(shape, dtype=dtype)
+        V = torch.empty_like(K)
         kp, ks, vp, vs = K.data_ptr(), None, V.data_ptr(), None
     else:
         if K is None:
@@ -157,9 +163,9 @@ def ska_cache_attn_fwd(Q, cache, W, causal=False, eps=1.0, start_q=None, len_q=N
     B, Hq, Lq, d = qshape
     _, Hk, Lc, _ = kshape
     dev, dt, code, store = _here(Q, "Q"), Q.dtype, _code(Q), _store(cache[0], "cache.K")
-    qp, qs = _heads(Q, qshape, dt, dev, "Q")
+    qp, qs = _queries(Q, qshape, dev)
     if O is None:
-        O = _like(Q)
+        O = torch.empty_like(Q) if qs is None else Q.new_empty(qshape)
         op, os = O.data_ptr(), None
     else:
         op, os = _heads(O, qshape, dt, dev, "O")
@@ -226,9 +232,9 @@ def ska_prefix_attn_fwd(Q, prefix, own, W, causal=True, eps=1.0, len_p=None, sta
     behind, other = _side(own, (B, Hk, Lk, d), Q, dev, "own")
     if store != other or len(prefix) != len(own):
         raise ValueError("prefix and own: expected the same kind of storage")
-    qp, qs = _heads(Q, qshape, dt, dev, "Q")
+    qp, qs = _queries(Q, qshape, dev)
     if O is None:
-        O = _like(Q)
+        O = torch.empty_like(Q) if qs is None else Q.new_empty(qshape)
         op, os = O.data_ptr(), None
     else:
         op, os = _heads(O, qshape, dt, dev, "O")

@@ -99,3 +99,25 @@ def test_rows_that_do_not_reach_a_large_value(apart, store):
     floor = (2.0 ** -20 + 2.0 ** -29) * n[:, :, :-1] * vmax * top
     check("O", O[:, :, :-1], (want[:, :, :-1], bound[:, :, :-1] + floor))
     assert (floor < 4 * half(BF16) * want[:, :, :-1].abs().amax()).all()   # (the bound says something)
+
+
+@pytest.mark.parametrize("store", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("W", [0, 3])
+def test_values_at_the_ends_of_fp32(W, dtype, store):
+    """Each item with values of a size of its own, from the largest (alone: sums of several pass fp32) to the smallest that a scale has."""
+    say("ends of fp32", W, dtype, store)
+    g = torch.Generator().manual_seed(9)
+    sizes = [2.9e38 if W == 0 else 5e37, 1e30, 1.0, 1e-20, 1e-30, 1e-36]
+    B, Hq, Hk, L, d = len(sizes), 2, 1, 40, 64
+    q, k = rnd(g, B, Hq, L, d, dtype=dtype), rnd(g, B, Hk, L, d, dtype=dtype)
+    v = (torch.rand(B, Hk, L, d, generator=g) * 2 - 1).to(dtype) * torch.tensor(sizes).view(-1, 1, 1, 1).to(dtype)
+    v = v.to(dtype)
+    cache = ska.ska_cache_write(ska.ska_cache_empty(B, Hk, L, d, store), k.cuda(), v.cuda())
+    O, LSE = ska.ska_cache_attn_fwd(q.cuda(), cache, W, True)
+    kv = [ref.values(*kept(x, store)) for x in (k, v)]
+    for b in range(B):   # (the bound takes the largest value of all: one item at a time)
+        want = ref.attn(q[b:b + 1], *(x[b:b + 1] for x in kv), pairs(1, L, L, W, True), 1.0)
+        # below 2^-126 a number has a rounding of 2^-150 at least, and flushing it is 2^-126 in units of the value's scale
+        check("O", O[b:b + 1], (want["O"][0], want["O"][1] + 2.0 ** -126 * (1 + 2.0 ** -8)))
+        check("LSE", LSE[b:b + 1], want["LSE"])
