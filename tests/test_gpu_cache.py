@@ -286,3 +286,28 @@ def test_prefix_lengths_at_their_ends():
         check("LSE", LSE, want["LSE"])
         if P == 0:
             assert not O[0].any() and (LSE[0] == -math.inf).all()
+
+
+@pytest.mark.parametrize("store,dtype", [("same", F32), ("same", BF16), ("e4m3", F32), ("e4m3", BF16), ("int8", BF16)])
+@pytest.mark.parametrize("B,Hq,Hk,Lq,Lp,Lk,d,W", [(120, 4, 2, 1, 300, 900, 32, ALL), (250, 1, 1, 3, 700, 1500, 32, 1800), (64, 8, 4, 2, 900, 60, 64, ALL)])
+def test_prefix_of_many_items(B, Hq, Hk, Lq, Lp, Lk, d, W, store, dtype):
+    """As many workgroups as there are CUs, or nearly: these walk over the prefix and their own keys of ragged lengths."""
+    say("prefix of many", B, Hq, Hk, Lq, Lp, Lk, d, W, store, dtype)
+    g = torch.Generator().manual_seed(Lp + Lk)
+    q, k, v = case(g, B, Hq, Hk, Lq, Lk, d, dtype)
+    _, pk, pv = case(g, 1, Hq, Hk, Lq, Lp, d, dtype)
+    if store == "same":
+        own, prefix, kv, pkv = (k.cuda(), v.cuda()), (pk[0].cuda(), pv[0].cuda()), (k.double(), v.double()), (pk[0].double(), pv[0].double())
+    else:
+        own, prefix = cache_of(k, v, store), ska.KVCache(*(x[0] for x in cache_of(pk, pv, store)))
+        kv, pkv = ([ref.values(*kept(x, store)) for x in two] for two in ((k, v), (pk[0], pv[0])))
+    lens = torch.randint(0, Lk + 1, (B,), generator=g, dtype=torch.int32)
+    start, P = torch.clamp(lens - Lq, min=0).int(), Lp - 5
+    mask_p = (torch.rand(Lp, generator=g) > 0.1).to(torch.uint8)
+    call = lambda: ska.ska_prefix_attn_fwd(q.cuda(), prefix, own, W, start_q=start.cuda(), len_k=lens.cuda(), len_p=ints(P).cuda(), mask_p=mask_p.cuda())   # noqa: E731
+    O, LSE = call()
+    want = ref.prefix_attn(q, *pkv, *kv, W, True, 1.0, P=P, mask_p=mask_p, codes=store != "same", start=start, len_k=lens)
+    check("O", O, want["O"])
+    check("LSE", LSE, want["LSE"])
+    again = call()
+    assert torch.equal(O, again[0]) and torch.equal(LSE, again[1])
