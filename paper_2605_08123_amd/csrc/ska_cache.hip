@@ -315,24 +315,34 @@ CaGrid ca_grid(const CaProblem &p, int nq, bool prefix)
 {
     const long rows = prefix ? p.R() * p.B : p.R(), problems = prefix ? p.Hk : (long)p.B * p.Hk, L = prefix ? p.Lp : p.Lk;
     const long unit_rows = 16 * nq;
-    const bool together = ca_together(p);
     CaGrid g;
     g.blocks = (rows + unit_rows - 1) / unit_rows;
     const long reach = prefix ? std::min(L, (long)p.W) : ca_reach(p, nq);
     g.order = prefix || g.blocks <= 8 || reach < L / 2 ? CA_NEIGHBOURS : CA_LAST_FIRST;
-    const long tile = ca_tile(p), tiles = (reach + tile - 1) / tile;
-    // Two tiles to a wavefront at least; four where a prefix's workgroups run beside: more parts only have to be joined (32 tokens of 1024
+    const long tile = ca_tile(p), tiles = (reach + tile - 1) / tile, units = g.blocks * problems;
+    g.parts = 1;
+    if (ca_together(p)) return g;
+    if (!p.Lp) {
+        // The parts that cost least, in tiles of a wavefront: rounds of CA_ROOM workgroups, each a part's tiles and five for its start and end, and
+        // four for the join; two tiles to a wavefront at least (one part and these: 132 problems of 16000 tokens, e4m3, d = 64, 61 and 57 us, int8, d = 32,
+        // 44 and 33; 320 of 12000, int8, d = 128, 227 and 194; 1500 tokens of 8 heads on 6000, int8, d = 128, 85 and 89)
+        double least = 0;
+        for (long n = 1; n <= 256 && (n == 1 || n * 2 * CA_WAVES <= tiles); ++n) {
+            const double cost = (double)((units * n + CA_ROOM - 1) / CA_ROOM) * (tiles / (double)(n * CA_WAVES) + 5) + (n > 1 ? 4 : 0);
+            if (n == 1 || cost < least) least = cost, g.parts = (int)n;
+        }
+        return g;
+    }
+    // Two tiles to a wavefront at least; four for an item's keys beside a prefix's workgroups: more parts only have to be joined (32 tokens of 1024
     // behind 65536, bf16: 29 us, 31 with two).  The prefix takes the room that the items' own workgroups leave, or if these take more than
     // half of it all of it, in turn with them (64 tokens of 2048 behind 16384, int8, d = 128: 55 us, 64 with half of it).
-    const long least = p.Lp && !prefix ? 4 : 2;
     long space = CA_ROOM;
     if (prefix) {
         const CaGrid o = ca_grid(p, nq, false);
         const long own = o.blocks * o.parts * p.B * p.Hk;
         if (own <= CA_ROOM / 2) space = CA_ROOM - own;
     }
-    if (together) space = g.blocks * problems;
-    g.parts = (int)std::max(1L, std::min({space / (g.blocks * problems), tiles / (least * CA_WAVES), 256L}));
+    g.parts = (int)std::max(1L, std::min({space / units, tiles / ((prefix ? 2 : 4) * CA_WAVES), 256L}));
     return g;
 }
 int check(const CaProblem &p, bool prefix)

@@ -311,3 +311,21 @@ def test_prefix_of_many_items(B, Hq, Hk, Lq, Lp, Lk, d, W, store, dtype):
     check("LSE", LSE, want["LSE"])
     again = call()
     assert torch.equal(O, again[0]) and torch.equal(LSE, again[1])
+
+
+@pytest.mark.parametrize("B,Hq,Hk,Lq,Lk,d", [(66, 4, 2, 1, 4000, 32), (3, 4, 2, 700, 2100, 64), (150, 2, 2, 2, 1300, 128)])
+@pytest.mark.parametrize("store", ["e4m3", "int8"])
+def test_parts_of_many_problems(B, Hq, Hk, Lq, Lk, d, store):
+    """More problems than fill whole rounds of workgroups: walks in parts, ragged lengths, some of which leave parts without a key."""
+    say("parts", B, Hq, Hk, Lq, Lk, d, store)
+    g = torch.Generator().manual_seed(Lk)
+    q, k, v = case(g, B, Hq, Hk, Lq, Lk, d, BF16)
+    lens = torch.randint(0, Lk + 1, (B,), generator=g, dtype=torch.int32)
+    start = torch.clamp(lens - Lq, min=0).int()
+    call = lambda: ska.ska_cache_attn_fwd(q.cuda(), cache_of(k, v, store), ALL, True, start_q=start.cuda(), len_k=lens.cuda())   # noqa: E731
+    O, LSE = call()
+    want = ref.attn(q, *(ref.values(*kept(x, store)) for x in (k, v)), pairs(B, Lq, Lk, ALL, True, start=start, len_k=lens), 1.0)
+    check("O", O, want["O"])
+    check("LSE", LSE, want["LSE"])
+    again = call()
+    assert torch.equal(O, again[0]) and torch.equal(LSE, again[1])
