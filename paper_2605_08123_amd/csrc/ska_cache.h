@@ -205,25 +205,35 @@ template <typename S> __device__ __forceinline__ f16x2 ca_feature_half(unsigned 
 template <typename S, typename T, int D> struct CaQuery {
     static constexpr bool PLAIN = CaStore<S>::BYTES == 4;                  // products in fp32
     static constexpr int PARTS = !PLAIN && sizeof(T) == 4 ? 3 : 1, STEPS = PLAIN ? D / 16 : D / 32, PIECES = PARTS * STEPS;   // of a block of 16 rows
-    // step s of a block whose row x is at `row`, into `to`: the block's pieces, this lane's 16 bytes of each
-    static __device__ __forceinline__ void put(uint4 *to, const T *row, int s, int g, bool on)
+    static constexpr int WORDS = PARTS == 1 ? 4 : 8;
+    unsigned w[WORDS];   // of step s of a block whose row x is at `row`
+    __device__ __forceinline__ void load(const T *row, int s, int g)
     {
-        const auto keep = [&](uint4 y) { return on ? y : make_uint4(0, 0, 0, 0); };
         // 8 bits: 16 features adjacent (d = 32: 8), two operands; bf16: 8; fp32: 4
         const int at = PLAIN ? 16 * s + 4 * g : CaStore<S>::BYTES == 1 && D > 32 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-        if constexpr (PARTS == 1) to[s * 64] = keep(*reinterpret_cast<const uint4 *>(row + at));
+#pragma unroll
+        for (int i = 0; i < WORDS / 4; ++i) {
+            const uint4 y = *reinterpret_cast<const uint4 *>(row + at + 4 * i);
+            w[4 * i] = y.x; w[4 * i + 1] = y.y; w[4 * i + 2] = y.z; w[4 * i + 3] = y.w;
+        }
+    }
+    // into `to`: the block's pieces, this lane's 16 bytes of each
+    __device__ __forceinline__ void put(uint4 *to, int s, bool on) const
+    {
+        const auto keep = [&](uint4 y) { return on ? y : make_uint4(0, 0, 0, 0); };
+        if constexpr (PARTS == 1) to[s * 64] = keep(make_uint4(w[0], w[1], w[2], w[3]));
         else {
             float f[8];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) load4<float>(reinterpret_cast<const float *>(row) + at + 4 * i, reinterpret_cast<float(&)[4]>(f[4 * i]));
+            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
-                unsigned w[4];
+                unsigned y[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(__float_as_uint(f[2 * i + 1]), __float_as_uint(f[2 * i]), 0x07060302u);
+                for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_perm(__float_as_uint(f[2 * i + 1]), __float_as_uint(f[2 * i]), 0x07060302u);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] = isinf(f[i]) ? 0.f : f[i] - __uint_as_float(__float_as_uint(f[i]) & 0xffff0000u);
-                to[(p * STEPS + s) * 64] = keep(make_uint4(w[0], w[1], w[2], w[3]));
+                to[(p * STEPS + s) * 64] = keep(make_uint4(y[0], y[1], y[2], y[3]));
             }
         }
     }
@@ -340,10 +350,10 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
         const int per = s.by_span(tiles + s.parts * NW - 1) * NW;
         t = part * per + wv;
         t1 = min(tiles, (part + 1) * per);
-        if (t < t1) {   // (before the rows: all are under way at a time)
-            fetch_keys(ta, t);
-            fetch_values(ta, t);
-        }
+        // (of a place that exists where there is nothing to do: loads under a condition are waited for with all that come after them)
+        const int j0 = t < t1 ? lo + t * KT : 0, rows = t < t1 ? hi + 1 - j0 : 1;
+        ta.load_keys(kst, kb, ksb, vsb, mk, j0, rows, x, g);
+        ta.load_values(vst, vb, j0, rows, x, g);
     };
     const int start0 = a.start && !shared ? min(max(a.start[b0], 0), 1 << 24) : 0, lq0 = sm_len(a.len_q, b0, a.Lq);
     const int first0 = start0 + a.by_g(r0), last0 = start0 + min(a.by_g(min(r0 + 16 * NQ, s.rows) - 1), lq0 - 1);
@@ -357,17 +367,27 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
             all_lo = off + last0 - a.W; all_hi = front ? end : min(first0 + up, end);
         }
     };
+    // The rows' operands are asked for before the first tile and put into LDS while that is under way.  Rows that do not take part are zeros, so
+    // that what they hold decides nothing.
+    constexpr int QSTEPS = NQ * QL::STEPS, QN = (QSTEPS + NW - 1) / NW;
+    QL rows_q[QN];
+    bool on_q[QN];
+#pragma unroll
+    for (int i = 0; i < QN; ++i) {
+        const int j = min(wv + i * NW, QSTEPS - 1), n = j / QL::STEPS, r = r0 + 16 * n + x;
+        const CaRow w = ca_row(a, shared, b0, hk, min(r, s.rows - 1));
+        rows_q[i].load(reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + w.hq * a.q.h + w.i * a.q.l, j - n * QL::STEPS, g);
+        on_q[i] = r < s.rows && w.i < (shared ? sm_len(a.len_q, w.b, a.Lq) : lq0);
+        if (a.mask_q) on_q[i] = on_q[i] && a.mask_q[(long)w.b * a.Lq + w.i] != 0;
+    }
     keys_of(a.side[front ? 1 : 0], front ? 0 : b0);
     range();
     begin();
-
-    // the rows' operands, positions and whether they take part, into LDS; rows that do not are zeros, so that what they hold decides nothing
-    for (int i = wv; i < NQ * QL::STEPS; i += NW) {
-        const int n = i / QL::STEPS, r = r0 + 16 * n + x;
-        const CaRow w = ca_row(a, shared, b0, hk, min(r, s.rows - 1));
-        bool on = r < s.rows && w.i < (shared ? sm_len(a.len_q, w.b, a.Lq) : lq0);
-        if (a.mask_q) on = on && a.mask_q[(long)w.b * a.Lq + w.i] != 0;
-        QL::put(&lds.q[n][0][lane], reinterpret_cast<const T *>(a.q.p) + w.b * a.q.b + w.hq * a.q.h + w.i * a.q.l, i - n * QL::STEPS, g, on);
+    SM_READ_FIRST();
+#pragma unroll
+    for (int i = 0; i < QN; ++i) {
+        const int j = wv + i * NW, n = j / QL::STEPS;
+        if (j < QSTEPS) rows_q[i].put(&lds.q[n][0][lane], j - n * QL::STEPS, on_q[i]);
     }
     if (wv == 0) {   // (16 NQ rows at most: one wavefront has them all)
         const int r = r0 + lane;
