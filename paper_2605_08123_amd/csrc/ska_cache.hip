@@ -283,8 +283,9 @@ struct CaProblem {
     long R() const { return (long)Lq * G(); }
     long rows() const { return (long)B * Hk * R(); }
 };
-// How one side is launched: blocks of rows, parts of a walk, the workgroups' order
-struct CaGrid { long blocks; int parts; int order; };
+// How one side is launched: blocks of a problem's rows, those of all problems, tiles that a block reaches at most, parts of a walk, the
+// workgroups' order
+struct CaGrid { long blocks, units, tiles; int parts, order; };
 // Blocks of rows of a workgroup.  One block in workgroups of its own registers gains nothing (a token of 4 items on 65536 keys in e4m3,
 // d = 64: 20.2 us, 20.8 with two; 128 items on 4000: 27.2 and 27.4)
 int ca_rows_for(const CaProblem &p, long rows) { return rows <= 32 ? 2 : ca_most(p.dtype == SKA_F32, p.d); }
@@ -310,42 +311,59 @@ bool ca_together(const CaProblem &p)
     const long turn = (long)ca_tile(p) * CA_WAVES, front = std::min(p.Lp, p.W);
     return front + ca_reach(p, 1) <= 5 * turn || (8L * p.B * p.Hk >= 7 * CA_ROOM && front <= 8 * turn);
 }
-int ca_rows_of(const CaProblem &p) { return ca_together(p) ? 1 : ca_rows_for(p, p.Lp ? p.R() * p.B : p.R()); }
+// One side of a launch without its parts
 CaGrid ca_grid(const CaProblem &p, int nq, bool prefix)
 {
-    const long rows = prefix ? p.R() * p.B : p.R(), problems = prefix ? p.Hk : (long)p.B * p.Hk, L = prefix ? p.Lp : p.Lk;
-    const long unit_rows = 16 * nq;
+    const long rows = prefix ? p.R() * p.B : p.R(), L = prefix ? p.Lp : p.Lk, reach = prefix ? std::min(L, (long)p.W) : ca_reach(p, nq);
     CaGrid g;
-    g.blocks = (rows + unit_rows - 1) / unit_rows;
-    const long reach = prefix ? std::min(L, (long)p.W) : ca_reach(p, nq);
+    g.blocks = (rows + 16 * nq - 1) / (16 * nq);
+    g.units = g.blocks * (prefix ? p.Hk : (long)p.B * p.Hk);
+    g.tiles = (reach + ca_tile(p) - 1) / ca_tile(p);
     g.order = prefix || g.blocks <= 8 || reach < L / 2 ? CA_NEIGHBOURS : CA_LAST_FIRST;
-    const long tile = ca_tile(p), tiles = (reach + tile - 1) / tile, units = g.blocks * problems;
     g.parts = 1;
-    if (ca_together(p)) return g;
+    return g;
+}
+// How a problem is launched
+struct CaPlan {
+    int nq;             // blocks of rows of a workgroup
+    bool both;          // ca_together
+    CaGrid own, front;  // front: of the prefix, where it has workgroups of its own
+    int parts;          // of both sides
+};
+CaPlan ca_plan(const CaProblem &p)
+{
+    CaPlan l{};
+    l.both = ca_together(p);
+    l.nq = l.both ? 1 : ca_rows_for(p, p.Lp ? p.R() * p.B : p.R());
+    l.own = ca_grid(p, l.nq, false);
+    l.parts = 1;
+    if (l.both) return l;
     if (!p.Lp) {
         // The parts that cost least, in tiles of a wavefront: rounds of CA_ROOM workgroups, each a part's tiles and five for its start and end, and
         // four for the join; two tiles to a wavefront at least (one part and these: 132 problems of 16000 tokens, e4m3, d = 64, 61 and 57 us, int8, d = 32,
-        // 44 and 33; 320 of 12000, int8, d = 128, 227 and 194; 1500 tokens of 8 heads on 6000, int8, d = 128, 85 and 89)
-        double least = 0;
-        for (long n = 1; n <= 256 && (n == 1 || n * 2 * CA_WAVES <= tiles); ++n) {
-            const double cost = (double)((units * n + CA_ROOM - 1) / CA_ROOM) * (tiles / (double)(n * CA_WAVES) + 5) + (n > 1 ? 4 : 0);
-            if (n == 1 || cost < least) least = cost, g.parts = (int)n;
+        // 44 and 33; 320 of 12000, int8, d = 128, 227 and 194; 1500 tokens of 8 heads on 6000, int8, d = 128, 85 and 89).  Of the numbers with the
+        // same rounds the largest is taken; 16 rounds more than the least are as even as it gets.
+        const long most = std::min(l.own.tiles / (2 * CA_WAVES), 256L), least = (l.own.units + CA_ROOM - 1) / CA_ROOM;
+        const auto cost = [&](long rounds, long n) { return rounds * (l.own.tiles / (double)(n * CA_WAVES) + 5) + (n > 1 ? 4 : 0); };
+        double best = cost(least, 1);
+        for (long rounds = least; rounds <= least + 16 && 5.0 * rounds < best; ++rounds) {
+            const long n = std::min(CA_ROOM * rounds / l.own.units, most);
+            if (n > 1 && cost(rounds, n) < best) best = cost(rounds, n), l.own.parts = (int)n;
         }
-        return g;
+        l.parts = l.own.parts;
+        return l;
     }
     // Two tiles to a wavefront at least; four for an item's keys beside a prefix's workgroups: more parts only have to be joined (32 tokens of 1024
     // behind 65536, bf16: 29 us, 31 with two).  The prefix takes the room that the items' own workgroups leave, or if these take more than
     // half of it all of it, in turn with them (64 tokens of 2048 behind 16384, int8, d = 128: 55 us, 64 with half of it).
-    long space = CA_ROOM;
-    if (prefix) {
-        const CaGrid o = ca_grid(p, nq, false);
-        const long own = o.blocks * o.parts * p.B * p.Hk;
-        if (own <= CA_ROOM / 2) space = CA_ROOM - own;
-    }
-    g.parts = (int)std::max(1L, std::min({space / units, tiles / ((prefix ? 2 : 4) * CA_WAVES), 256L}));
-    return g;
+    l.front = ca_grid(p, l.nq, true);
+    l.own.parts = (int)std::max(1L, std::min({CA_ROOM / l.own.units, l.own.tiles / (4 * CA_WAVES), 256L}));
+    const long own = l.own.units * l.own.parts, space = own <= CA_ROOM / 2 ? CA_ROOM - own : CA_ROOM;
+    l.front.parts = (int)std::max(1L, std::min({space / l.front.units, l.front.tiles / (2 * CA_WAVES), 256L}));
+    l.parts = l.own.parts + l.front.parts;
+    return l;
 }
-int check(const CaProblem &p, bool prefix)
+int check(const CaProblem &p, bool prefix, CaPlan &l)
 {
     if (p.B < 1 || p.Hq < 1 || p.Hk < 1 || p.Lq < 1 || p.Lk < 1 || p.W < 0 || p.Hq % p.Hk || (prefix && p.Lp < 1)) return SKA_EINVAL;
     if (p.d != 32 && p.d != 64 && p.d != 128) return SKA_EUNSUPPORTED;
@@ -353,22 +371,18 @@ int check(const CaProblem &p, bool prefix)
     if (!scaled(p.store) && !(prefix && p.store == p.dtype)) return SKA_EUNSUPPORTED;
     if (p.Lq > 1 << 24 || p.Lk > 1 << 24 || p.Lp > 1 << 24 || (long)p.B * p.Hk > 65535 || p.R() > 1 << 27) return SKA_EUNSUPPORTED;
     if (prefix && p.R() * p.B > 1 << 27) return SKA_EUNSUPPORTED;
+    l = ca_plan(p);
     // Fewer than 2^32 threads with both sides' rounding up to 8 workgroups (a launch is accepted with more, and runs their number modulo 2^32)
-    const int nq = ca_rows_of(p);
-    long wgs = 0;
-    for (int side = 0; side <= (prefix && !ca_together(p) ? 1 : 0); ++side) {
-        const CaGrid g = ca_grid(p, nq, side == 1);
-        wgs += g.blocks * g.parts * (side ? p.Hk : (long)p.B * p.Hk) + 7;
-    }
+    const long wgs = l.own.units * l.own.parts + 7 + l.front.units * l.front.parts + 7;
     return wgs * 64 * CA_WAVES < 1L << 32 ? SKA_OK : SKA_EUNSUPPORTED;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-int ca_parts(const CaProblem &p, int nq) { return ca_grid(p, nq, false).parts + (p.Lp && !ca_together(p) ? ca_grid(p, nq, true).parts : 0); }
 size_t ws_lse(const CaProblem &p, int parts) { return up256((size_t)parts * p.rows() * sizeof(float)); }
-size_t ws_bytes(const CaProblem &p)
+size_t ws_bytes(const CaProblem &p, int parts) { return parts > 1 ? ws_lse(p, parts) + (size_t)parts * p.rows() * p.d * sizeof(float) : 0; }
+size_t ws_need(const CaProblem &p, bool prefix)
 {
-    const int parts = ca_parts(p, ca_rows_of(p));
-    return parts > 1 ? ws_lse(p, parts) + (size_t)parts * p.rows() * p.d * sizeof(float) : 0;
+    CaPlan l;
+    return check(p, prefix, l) == SKA_OK ? ws_bytes(p, l.parts) : 0;
 }
 
 struct CaKept {   // keys and values of one side as a caller gives them
@@ -396,7 +410,7 @@ void place(CaSide &s, const CaProblem &p, const CaGrid &g, bool prefix)
     s.blocks = (int)g.blocks;
     s.parts = g.parts;
     s.order = g.order;
-    s.units = (int)(g.blocks * g.parts * s.problems);
+    s.units = (int)(g.units * g.parts);
     s.wgs = (s.units + 7) / 8 * 8;
     s.by_problems = SmDiv::by(s.problems);
     s.by_blocks = SmDiv::by(s.blocks);
@@ -413,7 +427,8 @@ int attn(const CaProblem &p, const void *Q, const ska_strides *q_strides, const 
          const unsigned char *mask_k, const unsigned char *mask_p, float eps, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!LSE || !(eps > 0.f && isfinite(eps))) return SKA_EINVAL;
-    int rc = check(p, prefix != nullptr);
+    CaPlan l;
+    int rc = check(p, prefix != nullptr, l);
     if (rc != SKA_OK) return rc;
     CaArgs a{};
     const float cs = 1.f / (eps * sqrtf((float)p.d));
@@ -423,9 +438,8 @@ int attn(const CaProblem &p, const void *Q, const ska_strides *q_strides, const 
     if ((rc = tensor_of(a.o, O, o_strides, p.B, p.Hq, p.Lq, p.d, p.dtype, 16, true)) != SKA_OK) return rc;
     if ((rc = side_of(a.side[0], own, p.B, p.Hk, p.Lk, p.d, p.store)) != SKA_OK) return rc;
     if (prefix && (rc = side_of(a.side[1], *prefix, 1, p.Hk, p.Lp, p.d, p.store)) != SKA_OK) return rc;
-    const int nq = ca_rows_of(p);
-    a.parts = ca_parts(p, nq);
-    const size_t need = ws_bytes(p);
+    a.parts = l.parts;
+    const size_t need = ws_bytes(p, l.parts);
     if (need && (!workspace || workspace_bytes < need)) return SKA_EWORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 15) return SKA_EINVAL;
     a.part_lse = static_cast<float *>(workspace);
@@ -439,11 +453,10 @@ int attn(const CaProblem &p, const void *Q, const ska_strides *q_strides, const 
     a.by_g = SmDiv::by(a.G);
     a.by_hk = SmDiv::by(a.Hk);
     a.by_r = SmDiv::by((unsigned)p.R());
-    place(a.side[0], p, ca_grid(p, nq, false), false);
-    const bool both = ca_together(p);
-    if (prefix && !both) place(a.side[1], p, ca_grid(p, nq, true), true);
+    place(a.side[0], p, l.own, false);
+    if (l.front.units) place(a.side[1], p, l.front, true);
     const int at = p.store == SKA_F32 ? 0 : p.store == SKA_BF16 ? 1 : (p.store == SKA_E4M3 ? 2 : 4) + (p.dtype == SKA_BF16);
-    return LAUNCH[at][p.d == 32 ? 0 : p.d == 64 ? 1 : 2](nq, both, &a, static_cast<hipStream_t>(stream));
+    return LAUNCH[at][p.d == 32 ? 0 : p.d == 64 ? 1 : 2](l.nq, l.both, &a, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace
@@ -470,7 +483,7 @@ int ska_cache_read(const void *Kc, const ska_strides *kc_strides, const float *K
 size_t ska_cache_attn_workspace_bytes(int B, int Hq, int Hk, int Lq, int Lc, int d, int W, int causal, int dtype, int store)
 {
     const CaProblem p{B, Hq, Hk, Lq, 0, Lc, d, W, causal, dtype, store};
-    return check(p, false) == SKA_OK ? ws_bytes(p) : 0;
+    return ws_need(p, false);
 }
 
 int ska_cache_attn_fwd(const void *Q, const ska_strides *q_strides, const void *Kc, const ska_strides *kc_strides, const float *Ks,
@@ -487,7 +500,7 @@ int ska_cache_attn_fwd(const void *Q, const ska_strides *q_strides, const void *
 size_t ska_prefix_attn_workspace_bytes(int B, int Hq, int Hk, int Lq, int Lp, int Lk, int d, int W, int causal, int dtype, int store)
 {
     const CaProblem p{B, Hq, Hk, Lq, Lp, Lk, d, W, causal, dtype, store};
-    return check(p, true) == SKA_OK ? ws_bytes(p) : 0;
+    return ws_need(p, true);
 }
 
 int ska_prefix_attn_fwd(const void *Q, const ska_strides *q_strides, const void *Kp, const ska_strides *kp_strides, const float *Kps,
