@@ -354,12 +354,17 @@ CaPlan ca_plan(const CaProblem &p)
         return l;
     }
     // Two tiles to a wavefront at least; four for an item's keys beside a prefix's workgroups: more parts only have to be joined (32 tokens of 1024
-    // behind 65536, bf16: 29 us, 31 with two).  The prefix takes the room that the items' own workgroups leave, or if these take more than
-    // half of it all of it, in turn with them (64 tokens of 2048 behind 16384, int8, d = 128: 55 us, 64 with half of it).
+    // behind 65536, bf16: 29 us, 31 with two).  The prefix takes the room that the items' own workgroups leave, unless these take more than half of it
+    // and its walk there would be longer than one in all of the room and an item's before it (64 tokens of 2048 behind 16384, 4 key heads, int8, d = 128: 55 us in turn with the items', 64 with
+    // half of the room; 33 of 1000 behind 10000: 35 in turn, 26 beside them); more workgroups than places would take a prefix's blocks apart,
+    // which read its keys together (94 items behind 97725, int8, d = 128: 68 us, 88).
     l.front = ca_grid(p, l.nq, true);
     l.own.parts = (int)std::max(1L, std::min({CA_ROOM / l.own.units, l.own.tiles / (4 * CA_WAVES), 256L}));
-    const long own = l.own.units * l.own.parts, space = own <= CA_ROOM / 2 ? CA_ROOM - own : CA_ROOM;
-    l.front.parts = (int)std::max(1L, std::min({space / l.front.units, l.front.tiles / (2 * CA_WAVES), 256L}));
+    const long own = l.own.units * l.own.parts, rest = CA_ROOM - own;
+    const auto parts = [&](long space) { return std::max(1L, std::min({space / l.front.units, l.front.tiles / (2 * CA_WAVES), 256L})); };
+    const auto walk = [&](long n) { return l.front.tiles / (double)(n * CA_WAVES) + 5; };
+    l.front.parts = (int)parts(rest);
+    if (own > CA_ROOM / 2 && (rest < l.front.units || walk(parts(rest)) > walk(parts(CA_ROOM)) + l.own.tiles / (double)CA_WAVES + 5)) l.front.parts = (int)parts(CA_ROOM);
     l.parts = l.own.parts + l.front.parts;
     return l;
 }
