@@ -517,8 +517,12 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
         for (int h = 0; h < N; ++h) {
             pf[h] = pack8(p);
             if (h + 1 < N) {
+                const u32x4 w = __builtin_bit_cast(u32x4, pf[h]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] -= (float)pf[h][e];
+                for (int i = 0; i < 4; ++i) {   // (by bits: as conversions each number would be rounded once more by itself)
+                    p[2 * i] -= __uint_as_float(w[i] << 16);
+                    p[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+                }
             }
         }
     };
