@@ -69,7 +69,7 @@ int ska_cache_read(const void *Kc, const ska_strides *kc_strides, const float *K
  *   position (inactive ones reach as well).  A token that is reached whose value row is NaN (or a product exp(S - LSE) s' beyond
  *   fp32) is in O of the queries around it too.
  *   Limits, alignment and workspace as ska_softmax_attn_fwd (codes: multiples of 16 bytes); scales on any 4 bytes.  Instead of its
- *   2^24 blocks of 128 rows: fewer than 2^23 - 8 blocks of 64 query rows of a problem (32 with fp32 queries or d = 128), B Hk problems
+ *   2^24 blocks of 128 rows: fewer than 2^23 - 8 blocks of 64 query rows of a problem (32 on fp32 caches or with d = 128), B Hk problems
  *   of Lq (Hq / Hk) rows (SKA_EUNSUPPORTED otherwise).
  *   The same query can differ by roundings between calls of other sizes; the same call repeats its bits.
  */

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "sinkhorn_attn_cache.h"
 #include "ska_cache_launch.h"
@@ -286,9 +287,6 @@ struct CaProblem {
 // How one side is launched: blocks of a problem's rows, those of all problems, tiles that a block reaches at most, parts of a walk, the
 // workgroups' order
 struct CaGrid { long blocks, units, tiles; int parts, order; };
-// Blocks of rows of a workgroup.  One block in workgroups of its own registers gains nothing (a token of 4 items on 65536 keys in e4m3,
-// d = 64: 20.2 us, 20.8 with two; 128 items on 4000: 27.2 and 27.4)
-int ca_rows_for(const CaProblem &p, long rows) { return rows <= 32 ? 2 : ca_most(p.dtype == SKA_F32, p.d); }
 int ca_tile(const CaProblem &p) { return p.store == SKA_F32 ? 16 : 32; }
 // Workgroups at a time, one on each CU (a token of 8 items, 4 key heads of d = 128 on 32768 in int8: 60 us, with half of them 79, with twice
 // as many 64; eight wavefronts each, and not 16 with half the parts: short caches would wait for the join, 3000 tokens 11.2 us and 12.8)
@@ -330,42 +328,69 @@ struct CaPlan {
     CaGrid own, front;  // front: of the prefix, where it has workgroups of its own
     int parts;          // of both sides
 };
-CaPlan ca_plan(const CaProblem &p)
+// ... with workgroups of nq blocks of rows, and what it costs: in us nearly, a tile of a wavefront, a workgroup's start and end, a join
+double ca_plan(const CaProblem &p, int nq, CaPlan &l)
 {
-    CaPlan l{};
-    l.both = ca_together(p);
-    l.nq = l.both ? 1 : ca_rows_for(p, p.Lp ? p.R() * p.B : p.R());
-    l.own = ca_grid(p, l.nq, false);
-    l.parts = 1;
-    if (l.both) return l;
+    l = {};
+    l.nq = nq;
+    l.own = ca_grid(p, nq, false);
+    const double tile = !scaled(p.store) ? (nq == 4 ? 2.2 : 1.7) : (nq == 4 ? 1.65 : 1) * (p.dtype == SKA_F32 ? 1.9 : 1), ends = nq == 4 ? 8 : 5, join = 4;
+    const auto walk = [&](const CaGrid &g, long n) { return (&g == &l.own && p.R() <= 16 ? 0.7 : 1) * tile * g.tiles / (double)(n * CA_WAVES) + ends; };
     if (!p.Lp) {
-        // The parts that cost least, in tiles of a wavefront: rounds of CA_ROOM workgroups, each a part's tiles and five for its start and end, and
-        // four for the join; two tiles to a wavefront at least (one part and these: 132 problems of 16000 tokens, e4m3, d = 64, 61 and 57 us, int8, d = 32,
-        // 44 and 33; 320 of 12000, int8, d = 128, 227 and 194; 1500 tokens of 8 heads on 6000, int8, d = 128, 85 and 89).  Of the numbers with the
-        // same rounds the largest is taken; 16 rounds more than the least are as even as it gets.
+        // Parts: rounds of CA_ROOM workgroups, two tiles to a wavefront at least (one part and the best: 132 problems of 16000 tokens, e4m3, d = 64, 61
+        // and 57 us, int8, d = 32, 44 and 33; 320 of 12000, int8, d = 128, 227 and 194; 1500 tokens of 8 heads on 6000, int8, d = 128, 85 and 89).
+        // Of the numbers with the same rounds the largest is taken; 16 rounds more than the least are as even as it gets.
+        // Causal walks of different lengths, the longest first, fill their rounds: they count as much as they are.
         const long most = std::min(l.own.tiles / (2 * CA_WAVES), 256L), least = (l.own.units + CA_ROOM - 1) / CA_ROOM;
-        const auto cost = [&](long rounds, long n) { return rounds * (l.own.tiles / (double)(n * CA_WAVES) + 5) + (n > 1 ? 4 : 0); };
-        double best = cost(least, 1);
-        for (long rounds = least; rounds <= least + 16 && 5.0 * rounds < best; ++rounds) {
+        const double uneven = p.causal && l.own.order == CA_LAST_FIRST ? std::min(1., p.Lq / (double)p.Lk) : 0;
+        const auto rounds_of = [&](long n) {
+            const double full = l.own.units * n / (double)CA_ROOM, whole = std::ceil(full);
+            return std::max(1., whole - (whole - full) * uneven);
+        };
+        double best = rounds_of(1) * walk(l.own, 1);
+        for (long rounds = least; rounds <= least + 16 && ends * rounds < best; ++rounds) {
             const long n = std::min(CA_ROOM * rounds / l.own.units, most);
-            if (n > 1 && cost(rounds, n) < best) best = cost(rounds, n), l.own.parts = (int)n;
+            const double cost = rounds_of(n) * walk(l.own, n) + join;
+            if (n > 1 && cost < best) best = cost, l.own.parts = (int)n;
         }
         l.parts = l.own.parts;
-        return l;
+        return best;
     }
     // Two tiles to a wavefront at least; four for an item's keys beside a prefix's workgroups: more parts only have to be joined (32 tokens of 1024
     // behind 65536, bf16: 29 us, 31 with two).  The prefix takes the room that the items' own workgroups leave, unless these take more than half of it
-    // and its walk there would be longer than one in all of the room and an item's before it (64 tokens of 2048 behind 16384, 4 key heads, int8, d = 128: 55 us in turn with the items', 64 with
-    // half of the room; 33 of 1000 behind 10000: 35 in turn, 26 beside them); more workgroups than places would take a prefix's blocks apart,
-    // which read its keys together (94 items behind 97725, int8, d = 128: 68 us, 88).
-    l.front = ca_grid(p, l.nq, true);
+    // and its walk there would be longer than one in all of the room and an item's before it (64 tokens of 2048 behind 16384, 4 key heads, int8,
+    // d = 128: 55 us in turn with the items', 64 with half of the room; 33 of 1000 behind 10000: 35 in turn, 26 beside them); more workgroups than
+    // places would take a prefix's blocks apart, which read its keys together (94 items behind 97725, int8, d = 128: 68 us, 88).
+    l.front = ca_grid(p, nq, true);
     l.own.parts = (int)std::max(1L, std::min({CA_ROOM / l.own.units, l.own.tiles / (4 * CA_WAVES), 256L}));
     const long own = l.own.units * l.own.parts, rest = CA_ROOM - own;
     const auto parts = [&](long space) { return std::max(1L, std::min({space / l.front.units, l.front.tiles / (2 * CA_WAVES), 256L})); };
-    const auto walk = [&](long n) { return l.front.tiles / (double)(n * CA_WAVES) + 5; };
     l.front.parts = (int)parts(rest);
-    if (own > CA_ROOM / 2 && (rest < l.front.units || walk(parts(rest)) > walk(parts(CA_ROOM)) + l.own.tiles / (double)CA_WAVES + 5)) l.front.parts = (int)parts(CA_ROOM);
+    double best = (double)((l.front.units + std::max(rest, 1L) - 1) / std::max(rest, 1L)) * walk(l.front, l.front.parts);
+    if (own > CA_ROOM / 2) {
+        const long n = parts(CA_ROOM);
+        const double cost = walk(l.front, n) + walk(l.own, 1);
+        if (rest < l.front.units || cost < best) best = cost, l.front.parts = (int)n;
+    }
     l.parts = l.own.parts + l.front.parts;
+    return best + join;
+}
+// Workgroups of 32 rows or of 64, whose wavefronts turn a key's codes into operands once for twice the rows, but begin and end later (8 problems of 48
+// rows on 2500 keys, e4m3, d = 64: 12.7 us and 15.4; of 400 on 30000 61 and 54; 2048 tokens of 8 heads on 2 on 16384 119 and 96; 128 rows of 32 items behind
+// 60000, bf16: 26 and 22).  One block in workgroups of its own registers gains nothing (a token of 4 items on 65536 keys: 20.2 us, 20.8 with two).
+CaPlan ca_plan(const CaProblem &p)
+{
+    CaPlan l{};
+    if (ca_together(p)) {
+        l.nq = 1;
+        l.both = true;
+        l.own = ca_grid(p, 1, false);
+        l.parts = 1;
+        return l;
+    }
+    const double cost = ca_plan(p, 2, l);
+    CaPlan wide;
+    if (ca_most(p.store == SKA_F32, p.d) == 4 && (p.Lp ? p.R() * p.B : p.R()) > 32 && ca_plan(p, 4, wide) < cost) return wide;
     return l;
 }
 int check(const CaProblem &p, bool prefix, CaPlan &l)

@@ -5,7 +5,7 @@
 namespace {
 template <typename S, typename T, int D> int launch(int nq, bool both, const CaArgs &a, hipStream_t st)
 {
-    constexpr int MOST = ca_most(sizeof(T) == 4, D);
+    constexpr int MOST = ca_most(sizeof(S) == 4, D);
     const dim3 grid((unsigned)(a.side[0].wgs + a.side[1].wgs));
     if (both) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 1, true>), grid, dim3(64 * CA_WAVES), 0, st, a);
     else if (nq == 2) hipLaunchKernelGGL((ca_attn_kernel<S, T, D, 2, false>), grid, dim3(64 * CA_WAVES), 0, st, a);

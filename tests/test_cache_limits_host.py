@@ -7,8 +7,8 @@ from paper_2605_08123_amd import binding, cache
 from .test_cache_host import BF16, E4M3, F32, INT8, _attn
 
 
-# Lq (Hq / Hk) query rows of B Hk problems, 64 to a workgroup of 512 threads (32 for fp32 queries and for d = 128): 2^32 threads are 2^23 workgroups
-@pytest.mark.parametrize("dt,d,rows", [(BF16, 64, 64), (BF16, 32, 64), (BF16, 128, 32), (F32, 32, 32), (F32, 128, 32)])
+# Lq (Hq / Hk) query rows of B Hk problems, 64 to a workgroup of 512 threads (32 for d = 128): 2^32 threads are 2^23 workgroups
+@pytest.mark.parametrize("dt,d,rows", [(BF16, 64, 64), (BF16, 32, 64), (BF16, 128, 32), (F32, 32, 64), (F32, 128, 32)])
 @pytest.mark.parametrize("store", [E4M3, INT8])
 def test_threads_within_32_bits(dt, d, rows, store):
     lib = cache._lib()

@@ -314,12 +314,13 @@ def test_prefix_of_many_items(B, Hq, Hk, Lq, Lp, Lk, d, W, store, dtype):
 
 
 @pytest.mark.parametrize("B,Hq,Hk,Lq,Lk,d", [(66, 4, 2, 1, 4000, 32), (3, 4, 2, 700, 2100, 64), (150, 2, 2, 2, 1300, 128)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("store", ["e4m3", "int8"])
-def test_parts_of_many_problems(B, Hq, Hk, Lq, Lk, d, store):
+def test_parts_of_many_problems(B, Hq, Hk, Lq, Lk, d, store, dtype):
     """More problems than fill whole rounds of workgroups: walks in parts, ragged lengths, some of which leave parts without a key."""
-    say("parts", B, Hq, Hk, Lq, Lk, d, store)
+    say("parts", B, Hq, Hk, Lq, Lk, d, store, dtype)
     g = torch.Generator().manual_seed(Lk)
-    q, k, v = case(g, B, Hq, Hk, Lq, Lk, d, BF16)
+    q, k, v = case(g, B, Hq, Hk, Lq, Lk, d, dtype)
     lens = torch.randint(0, Lk + 1, (B,), generator=g, dtype=torch.int32)
     start = torch.clamp(lens - Lq, min=0).int()
     call = lambda: ska.ska_cache_attn_fwd(q.cuda(), cache_of(k, v, store), ALL, True, start_q=start.cuda(), len_k=lens.cuda())   # noqa: E731
