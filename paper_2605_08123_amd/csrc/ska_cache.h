@@ -95,15 +95,16 @@ template <int BYTES> __device__ __forceinline__ void ca_load(unsigned *to, CaBuf
     }
 }
 
-// KT keys and values as they come from memory.  Keys as they are used, 16 rows of 16 bytes a quarter of a load, unless STAGED: bf16 rows of
-// 256 bytes are loaded as they lie, 1024 adjacent bytes at a time (C lanes a row), and handed over in LDS, where chunk c of 16 bytes of row r
-// lies at c ^ turn(r), so that 8 rows' chunks are in 8 groups of banks.  The cache's lines are asked for once instead of four times: 256
-// queries on 216039 keys in bf16, d = 128, 113 -> 89 us.  Others lose by LDS, which has the queries too, or wait for products (bf16, d = 64:
-// 43 -> 48; fp32, d = 128, on 100039 keys: 145 -> 154; 2048 on 16384 in e4m3, d = 64: 70 -> 77).
-template <typename S, int D> struct CaTile {
+// KT keys and values as they come from memory.  Keys as they are used, 16 rows of 16 bytes a quarter of a load, unless STAGED: bf16 rows of 128
+// and 256 bytes are loaded as they lie, 1024 adjacent bytes at a time (C lanes a row), and handed over in LDS, where chunk c of 16 bytes of row
+// r lies at c ^ turn(r), so that 8 rows' chunks are in 8 groups of banks.  The cache's lines are asked for once instead of four times: five
+// queries of 16 items on 262144 keys, d = 128, 252 -> 178 us; one of 64 items, 4 key heads, 2048 behind 16384, d = 64, 38 -> 33.  Others lose by LDS,
+// which has the queries too, or wait for products (four blocks of rows, d = 64: 40 -> 42 us for 94 items on 97725; fp32, d = 128: 145 -> 154 for 128
+// rows on 100039; e4m3, d = 64: 70 -> 77 for 2048 tokens on 16384; int8, d = 128: 76 -> 85).
+template <typename S, int D, int NQ> struct CaTile {
     using ST = CaStore<S>;
     static constexpr int NT = ST::NT, RB = D * ST::BYTES, C = RB / 16, KB = RB / 4, KP = KB < 16 ? KB : 16, VB = RB / 16;   // bytes of a row, of a lane of a key, of its load, of a value
-    static constexpr bool STAGED = ST::BYTES == 2 && RB >= 256;
+    static constexpr bool STAGED = ST::BYTES == 2 && RB >= (NQ <= 2 ? 128 : 256);
     static constexpr int PER = 64 / C, LOADS = ST::KT / PER;   // rows of a load, loads
     unsigned k[NT][KB / 4], v[NT][4][VB < 4 ? 1 : VB / 4];
     float ks, vs;   // of key lane & 31
@@ -275,7 +276,7 @@ template <typename S, typename T, int D, int NQ, bool BOTH>
 __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_attn_kernel(const CaArgs a)
 {
     using ST = CaStore<S>;
-    using TL = CaTile<S, D>;
+    using TL = CaTile<S, D, NQ>;
     using QL = CaQuery<S, T, D>;
     constexpr int NW = CA_WAVES, NT = ST::NT, KT = ST::KT, F = D / 16, PITCH = D + 4;
     // P in fp16 times 2^4 (HALF: codes in 8 bits for bf16 results), as the sum of two bf16 numbers (bf16 caches) or three (codes for fp32
