@@ -298,11 +298,11 @@ long ca_reach(const CaProblem &p, int nq)
 }
 // Whether an item's workgroups take the prefix too: one launch and nothing to join, but the prefix is read by each.  Few rows, all workgroups
 // at a time, and a walk of five tiles a wavefront at most (4 heads on each key head, together and apart; 30 items, 2 key heads: e4m3, d = 64,
-// 30 tokens behind 500 7.7 and 14.9 us, 100 behind 1000 8.8 and 14.9; int8, d = 128, 100 behind 2000 19.6 and 18.0; fp32, d = 128, 30 behind
-// 500 17.1 and 19.9; one item, 1 key head: 7.1 and 9.1, 8.3 and 9.7, 18.8 and 13.8, 16.3 and 13.7).  Where the items' workgroups fill the CUs
+// 30 tokens behind 500 7.9 and 11.5 us, 100 behind 1000 9.1 and 11.5; int8, d = 128, 100 behind 2000 19.6 and 16.8; fp32, d = 128, 30 behind
+// 500 16.7 and 19.4; one item, 1 key head: 7.3 and 8.9, 8.5 and 9.6, 18.8 and 13.5, 15.8 and 13.2).  Where the items' workgroups fill the CUs
 // by themselves, the prefix's would be a second round: eight tiles of a prefix, and any number behind it (2000 behind 1000, 4 key heads, together
-// and apart; 64 items: e4m3, d = 64, 19.3 and 27.2, int8, d = 128, 33.0 and 41.5, bf16, d = 64, 29.1 and 38.1; 40 items: 16.0 and 16.5, 26.9 and
-// 23.7, 23.0 and 20.9)
+// and apart; 64 items: e4m3, d = 64, 19.9 and 24.4, int8, d = 128, 31.8 and 39.1, bf16, d = 64, 27 and 35; 40 items: 16.0 and 15.5, 26.9 and
+// 22.8, 23.0 and 20.3)
 bool ca_together(const CaProblem &p)
 {
     if (!p.Lp || p.R() > 16 || (long)p.B * p.Hk > CA_ROOM) return false;
