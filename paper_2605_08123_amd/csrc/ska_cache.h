@@ -15,9 +15,9 @@
 //
 // What bounds it, in us of the kernel alone: few rows, memory (a token of 8 items, 16 heads on 4 of d = 128, int8 caches of 32768: 46, 4.5 TB/s; four
 // items, 8 heads on 2 of d = 64, e4m3, 65536: 14.9, 3.6 TB/s, of which about 5 are the first loads' and the last sums' latency).  Many rows,
-// vector instructions (2048 tokens of 8 heads on 2, d = 64, 16384 keys in e4m3: 71; a wavefront issues 207 of
-// them beside the 32 products of a tile of 32 keys and 64 rows: 128 for P, 48 that turn codes into operands; they take 55 % of the time, products
-// 24 %, with two wavefronts to a SIMD).  One look at a tile decides for all blocks whether a maximum moves (a maximum per tile and block: 81).
+// vector instructions (2048 tokens of 8 heads on 2, d = 64, 16384 keys in e4m3: 71; a wavefront issues 187 of
+// them beside the 32 products of a tile of 32 keys and 64 rows: 115 for P, 40 that turn codes into operands, 16 for the values' scales; they take 55 % of
+// the time, products 24 %, with two wavefronts to a SIMD).  One look at a tile decides for all blocks whether a maximum moves (a maximum per tile and block: 81).
 #pragma once
 #include "ska_softmax.h"
 
