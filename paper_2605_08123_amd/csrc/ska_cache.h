@@ -816,14 +816,14 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
 }
 
 // Joins the parts of a row: weighted by exp(their LSE - the largest).  A thread takes four features over every slices-th part, four parts
-// asked for at a time (a part without a key has LSE = -inf and zeros); the slices are joined by LDS in their order.
-template <typename T, int D> __global__ __launch_bounds__(NTHREADS) void ca_join_kernel(const CaArgs a, int slices)
+// asked for at a time (a part without a key has LSE = -inf and zeros); the slices are joined by LDS in their order.  first: the launch's first row.
+template <typename T, int D> __global__ __launch_bounds__(NTHREADS) void ca_join_kernel(const CaArgs a, long first, int slices)
 {
     constexpr int FT = D / 4, U = 4;
     __shared__ f32x4 sx[NTHREADS];
     __shared__ float sm[NTHREADS], sl[NTHREADS];
     const int R = a.Lq * a.G, f = (threadIdx.x % FT) * 4, rest = threadIdx.x / FT, slice = rest % slices;
-    const long rows = (long)a.B * a.Hk * R, row = (long)blockIdx.x * (NTHREADS / FT / slices) + rest / slices, from = min(row, rows - 1);
+    const long rows = (long)a.B * a.Hk * R, row = first + (long)blockIdx.x * (NTHREADS / FT / slices) + rest / slices, from = min(row, rows - 1);
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     float m = CA_LEAST, l = 0.f;
     for (int s0 = slice; s0 < a.parts; s0 += U * slices) {

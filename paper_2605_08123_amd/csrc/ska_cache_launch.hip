@@ -1,8 +1,12 @@
 // The attention kernels' instances for one storage type, query type and head dimension (SKA_S, SKA_T, SKA_D; the function's name: SKA_NAME).
+#include <algorithm>
+
 #include "sinkhorn_attn_cache.h"
 #include "ska_cache_launch.h"
+#include "ska_cache_plan.h"
 
 namespace {
+static_assert(CaJoin::THREADS == NTHREADS, "the join's workgroups");
 template <typename S, typename T, int D> int launch(int nq, bool both, const CaArgs &a, hipStream_t st)
 {
     constexpr int MOST = ca_most(sizeof(S) == 4, D);
@@ -12,12 +16,13 @@ template <typename S, typename T, int D> int launch(int nq, bool both, const CaA
     else hipLaunchKernelGGL((ca_attn_kernel<S, T, D, MOST, false>), grid, dim3(64 * CA_WAVES), 0, st, a);
     if (hipGetLastError() != hipSuccess) return SKA_EHIP;
     if (a.parts > 1) {
-        const int threads = D / 4;
-        int slices = 1;   // as many as there are parts, or threads
-        while (slices * 2 <= a.parts && slices * 2 * threads <= NTHREADS) slices *= 2;
-        const long per = NTHREADS / threads / slices, rows = (long)a.B * a.Hk * a.Lq * a.G;
-        hipLaunchKernelGGL((ca_join_kernel<T, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(NTHREADS), 0, st, a, slices);
-        if (hipGetLastError() != hipSuccess) return SKA_EHIP;
+        const CaJoin join(a.parts, D);
+        const long rows = (long)a.B * a.Hk * a.Lq * a.G;
+        for (long first = 0; first < rows; first += join.most()) {
+            const long n = std::min(rows - first, join.most());
+            hipLaunchKernelGGL((ca_join_kernel<T, D>), dim3((unsigned)((n + join.per - 1) / join.per)), dim3(NTHREADS), 0, st, a, first, join.slices);
+            if (hipGetLastError() != hipSuccess) return SKA_EHIP;
+        }
     }
     return SKA_OK;
 }
