@@ -65,6 +65,8 @@ int ska_cache_read(const void *Kc, const ska_strides *kc_strides, const float *K
  *   fp16 numbers next to a power of two, and their products with it rounded to fp16 again (3 2^-11 in all; absolute 2^-20 of the
  *   value); in 32 tokens with a scale 2^9 times smaller than a value's before, the products are sums of two bf16 numbers (2^-16).
  *   Values 2^100 times smaller than another that is reached may be lost.
+ *   Values up to 2^127 / (n + 64), n the tokens that a query reaches by position, give finite results: sums over them, not yet divided by those
+ *   of exp(S - m), are fp32.
  *   Places of the cache beyond the lengths or inactive may hold anything, and so may those that no query of the item reaches by
  *   position (inactive ones reach as well).  A token that is reached whose value row is NaN (or a product exp(S - LSE) s' beyond
  *   fp32) is in O of the queries around it too.

@@ -285,9 +285,11 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
     constexpr int PP = HALF ? 1 : sizeof(T) == 4 ? 3 : 2;
     constexpr float BIAS = HALF ? 4.f : 0.f;
     // What the sum over a tile (ONES), a lane's part of it (HALF) or a lane's exponent may come to before a row's maximum is moved to its
-    // scores: fp16 is infinite from 2^16 on, so that a maximum may grow by 2^9 and more, and P keeps its bits down to 2^-18; the others lose
-    // nothing, and leave room for large values
-    constexpr float MANY = HALF ? 65504.f : ONES ? 65536.f : 16.f;
+    // scores: fp16 is infinite from 2^16 on, so that a maximum may grow by 2^9 and more, and P keeps its bits down to 2^-18; the others may
+    // grow by 2^16.  So that products of a P that has grown are no larger than their values, P is counted in 2^16 there, by a maximum that
+    // stands 16 above the scores (ONES: 2^-20 of P, which is 2^-16 as two numbers) or after the exponential (fp32 caches), and in tiles with
+    // values' scales of more than FAR it may not (codes for fp32 results)
+    constexpr float MANY = HALF ? 65504.f : ONES ? 1.f : 16.f, ABOVE = ONES ? 16.f : 0.f, SMALL = ST::BYTES == 4 ? 0x1p-16f : 1.f, FAR = 0x1p64f;
     union Lds {
         struct {
             uint4 q[NQ][QL::PIECES][64];
@@ -536,6 +538,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
         unsigned on = sm_bits(0, hi - j0) & FULL;
         if (mk) on &= (unsigned)__ballot(tl.act != 0);   // (lanes 0 ... 31: keys 0 ... 31)
         const bool inside = j0 >= all_lo && j0 + KT - 1 <= all_hi;   // of all rows' reach
+        float many = MANY;
         bool even = true;   // HALF: the values' scales are taken as fp16 numbers next to the unit
         if constexpr (ST::SCALED) {   // from a key per lane to the four of its accumulators
             float rel = tl.vs;
@@ -559,7 +562,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
                 even = __all(rel >= 0x1p-9f && rel <= 1.f);
                 if (__builtin_expect(!even, 0)) even = __all(!(on >> (lane & 31) & 1) || (rel >= 0x1p-9f && rel <= 1.f));
                 halves[wv][lane & 31] = even ? (_Float16)rel : (_Float16)0;
-            }
+            } else if (__any(rel > FAR)) many = 0.f;
             scales[wv][lane] = lane < 32 ? tl.ks * c2 : rel;
         }
         // The keys of the next tile are asked for as soon as these are used up (or in LDS), its values likewise; the last one asks for
@@ -620,7 +623,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
                 for (int e = 1; e < 4 * NT; ++e) top = fmaxf(top, p[nb][e]);
             }
 #pragma unroll
-            for (int e = 0; e < 4 * NT; ++e) p[nb][e] = fast_exp2(p[nb][e]);
+            for (int e = 0; e < 4 * NT; ++e) p[nb][e] = fast_exp2(p[nb][e]) * SMALL;
             if constexpr (HALF) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) ph[nb][e] = (_Float16)p[nb][e];
@@ -639,7 +642,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) much[nb] = probabilities(nb);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) fits = fits && (ST::BYTES == 2 ? much[nb] <= MANY : !(much[nb] > MANY));
+        for (int nb = 0; nb < NB; ++nb) fits = fits && (ST::BYTES == 2 ? much[nb] <= many : !(much[nb] > many));
         if (__builtin_expect(!__all(fits), 0)) {   // a row's maximum moves: lanes are compared with no exchange between them before
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -648,7 +651,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[nb][n][e] * kc[n][e]);
-                const float mn = fmaxf(m[nb], ca_max_groups(top)), f = fast_exp2(m[nb] - mn);
+                const float high = ca_max_groups(top), mn = fmaxf(m[nb], ONES ? high + ABOVE : high), f = fast_exp2(m[nb] - mn);
                 m[nb] = mn;
                 sum[nb] *= f;
 #pragma unroll
@@ -766,8 +769,15 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
         }
         if constexpr (HALF) {
             sum[n] *= 1.f / 16.f;   // (BIAS)
+            float f = unit * (1.f / 16.f);
+            if (unit > FAR) {   // a row's weights, of a maximum that may lag, are brought below 1 first
+                const int e = __builtin_amdgcn_frexp_expf(sum[n]);
+                sum[n] = ldexpf(sum[n], -e);
+                f = ldexpf(f, -e);
+                m[n] += (float)e;
+            }
 #pragma unroll
-            for (int j = 0; j < F; ++j) acc[n][j] *= unit * (1.f / 16.f);
+            for (int j = 0; j < F; ++j) acc[n][j] *= f;
         }
         met[n] = row_live[16 * n + x] && (keys >> n & 1);
     }
@@ -809,7 +819,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, NQ == 1 && D < 128 ? 4 : 2) void ca_
         }
         const CaRow w = ca_row(a, shared, b0, hk, r0 + row);
         float lse;
-        const float scale = ca_finish(M, L, any, a.parts > 1, lse);
+        const float scale = ca_finish(M, L * (1.f / SMALL), any, a.parts > 1, lse) * (1.f / SMALL);
         put(w, f, any ? y * scale : f32x4{0.f, 0.f, 0.f, 0.f});
         if (f == 0) put_lse(w, lse);
     }
