@@ -153,9 +153,9 @@ template <typename S, typename T> __device__ __forceinline__ uint2 move_codes(co
         return w;
     } else {
         // The nearest integer to a product with the rounded reciprocal, in the lower bits of a sum with 1.5 2^23; its remainder, which is exact
-        // near a border, says where that was not the quotient's (seldom)
+        // near a border, says where that was not the quotient's (seldom); doubled against the scale, because half of a scale below 2^-125 is rounded
         constexpr float MAGIC = 12582912.f;
-        const float inv = 1.f / scale, half = 0.5f * scale;
+        const float inv = 1.f / scale;
         float f[8], n[8], most = 0.f;
         x.floats(f);
 #pragma unroll
@@ -163,13 +163,13 @@ template <typename S, typename T> __device__ __forceinline__ uint2 move_codes(co
             n[i] = fmaf(f[i], inv, MAGIC);
             most = fmaxf(most, fabsf(fmaf(MAGIC - n[i], scale, f[i])));
         }
-        if (most >= half) {
+        if (2.f * most >= scale) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float rest = fmaf(MAGIC - n[i], scale, f[i]);
+                const float rest = 2.f * fmaf(MAGIC - n[i], scale, f[i]);
                 const bool odd = __float_as_uint(n[i]) & 1;
-                if (rest > half || (rest == half && odd)) n[i] += 1.f;
-                else if (rest < -half || (rest == -half && odd)) n[i] -= 1.f;
+                if (rest > scale || (rest == scale && odd)) n[i] += 1.f;
+                else if (rest < -scale || (rest == -scale && odd)) n[i] -= 1.f;
                 n[i] = fminf(fmaxf(n[i], MAGIC - 127.f), MAGIC + 127.f);
             }
         }

@@ -1,4 +1,5 @@
-"""Numbers at the ends of their ranges on caches: scores that climb while a walk goes on, beside large values."""
+"""Numbers at the ends of their ranges on caches: scores that climb while a walk goes on, beside large values;
+small values; codes of rows whose scale is near the smallest."""
 import math
 
 import pytest
@@ -55,3 +56,24 @@ def test_small_values_of_plain_caches(Lq, size, dtype):
     want = ref.prefix_attn(q, k[0].double(), v[0].double(), k.double(), v.double(), ALL, True, 1.0, start=start, codes=False)
     check("O", O, (want["O"][0], want["O"][1] + 2.0 ** -126), floor=0.0)
     check("LSE", LSE, want["LSE"])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("e", [-126, -125, -100, 0, 100])
+def test_int8_borders_of_small_scales(e, dtype):
+    """Numbers beside (n + 1/2) s, s in [2^e, 2^(e + 1)): half of a scale below 2^-125 need not be an fp32 number."""
+    say("int8 borders", e, dtype)
+    g = torch.Generator().manual_seed(e + 200)
+    n, d = 4000, 128
+    a = (127 * (1 + torch.rand(n, 1, generator=g, dtype=torch.float64)) * 2.0 ** e).to(dtype)
+    s = ref.quantise(a.float(), "int8")[1][:, None]
+    x = ((torch.randint(0, 127, (n, d), generator=g).double() + 0.5) * s).to(dtype)
+    step = torch.randint(-1, 2, (n, d), generator=g)
+    x = torch.where(step < 0, torch.nextafter(x, torch.zeros_like(x)), torch.where(step > 0, torch.nextafter(x, a.expand(n, d)), x))
+    x = x * (torch.randint(0, 2, (n, d), generator=g) * 2 - 1).to(dtype)
+    x[:, :1] = a
+    c, scale = ref.quantise(x, "int8")
+    assert (scale < 2.0 ** (e + 1)).float().mean() > 0.9 and (scale >= 2.0 ** e).float().mean() > 0.9
+    cache = ska.ska_cache_write(ska.ska_cache_empty(1, 1, n, d, "int8"), x[None, None].cuda(), x[None, None].cuda())
+    for codes, got in ((cache.K, cache.K_scale), (cache.V, cache.V_scale)):
+        assert torch.equal(got[0, 0].cpu().double(), scale) and torch.equal(codes[0, 0].cpu().double(), c)
