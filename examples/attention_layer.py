@@ -73,22 +73,25 @@ class AttentionLayer:
 
     def token(self, x, r, cache, length, prefix=None):
         """One more token per sequence, or several (softmax, causal): x, r [B, n, D]; cache: keys and values [B, Hk, L, d], of which length
-        [B] (int32) tokens are there and to which these are appended, or a cache in 8 bits (ska_cache_empty).  prefix: a cache in 8 bits
-        without the first dimension, whose tokens stand before all sequences.  -> output and sum."""
-        p, n = self.params, x.shape[1]
-        at = length if prefix is None else length + prefix.K.shape[1]
+        [B] (int32) tokens are there and to which these are appended, or a cache in 8 bits (ska_cache_empty).  prefix: the same without the
+        first dimension, whose tokens stand before all sequences.  -> output and sum."""
+        p, n, codes = self.params, x.shape[1], isinstance(cache, ska.KVCache)
+        if prefix is not None and len(prefix) != len(cache):
+            raise ValueError("prefix and cache: expected the same kind of storage")
+        at = length if prefix is None else length + prefix[0].shape[1]
         Y, S, _ = ska.ska_layer_norm_fwd(x, p["norm"], p["norm_bias"], residual=r)
         q, k, v = self._heads(Y @ p["qkv"])
         Q, K = ska.ska_rope_fwd(q, k, self.freq, self.amplitude, start=at)
-        if isinstance(cache, ska.KVCache):
+        if codes:
             ska.ska_cache_write(cache, K, v, start=length)
-            if prefix is None:
-                O, _ = ska.ska_cache_attn_fwd(Q, cache, self.W, True, self.eps, start_q=length, len_k=length + n)
-            else:
-                O, _ = ska.ska_prefix_attn_fwd(Q, prefix, cache, self.W, True, self.eps, start_q=length, len_k=length + n)
         else:
             b, i = torch.arange(x.shape[0], device=x.device)[:, None], length.long()[:, None] + torch.arange(n, device=x.device)
             cache[0][b, :, i], cache[1][b, :, i] = K.transpose(1, 2), v.transpose(1, 2)
+        if prefix is not None:
+            O, _ = ska.ska_prefix_attn_fwd(Q, prefix, cache, self.W, True, self.eps, start_q=length, len_k=length + n)
+        elif codes:
+            O, _ = ska.ska_cache_attn_fwd(Q, cache, self.W, True, self.eps, start_q=length, len_k=length + n)
+        else:
             O, _ = ska.ska_softmax_attn_fwd(Q, cache[0], cache[1], self.W, True, self.eps, len_k=length + n, start_q=length)
         return O.transpose(1, 2).reshape(x.shape[0], n, -1) @ p["out"], S
 
