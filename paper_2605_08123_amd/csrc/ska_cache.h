@@ -19,6 +19,7 @@
 // them beside the 32 products of a tile of 32 keys and 64 rows: 115 for P, 40 that turn codes into operands, 16 for the values' scales; they take 55 % of
 // the time, products 24 %, with two wavefronts to a SIMD).  One look at a tile decides for all blocks whether a maximum moves (a maximum per tile and block: 81).
 #pragma once
+#include "ska_cache_plan.h"
 #include "ska_softmax.h"
 
 namespace {
@@ -48,10 +49,6 @@ struct CaSide {
     int order;                        // CaOrder
     SmDiv by_problems, by_blocks, by_parts, by_span;   // problems, blocks, parts, parts * wavefronts of a workgroup
 };
-// Order of the workgroups.  Blocks of the same keys next to each other and a contiguous piece of them per XCD (workgroups go to the XCDs
-// in turn): few blocks, a prefix, a band.  Many blocks that walk over most of the keys: those with the longest walks first, problems fastest
-// (4096 tokens of 2 items, 8 heads on 2, causal, e4m3, d = 64: 78 us, and 100 as neighbours; 16 heads on 2, int8, d = 128: 178 and 258).
-enum CaOrder { CA_NEIGHBOURS, CA_LAST_FIRST };
 struct CaArgs {
     SmTensor q, o;
     float *lse;
@@ -259,7 +256,6 @@ __device__ __forceinline__ CaRow ca_row(const CaArgs &a, bool shared, int b, int
     return w;
 }
 
-constexpr int CA_WAVES = 8;   // of a workgroup: they share their rows and split the keys
 constexpr float CA_LEAST = -3.402823466e38f;   // a running maximum before the first score
 
 // Results of a row from its running maximum (powers of two), sum and whether it has met a key: factor of the accumulators, LSE

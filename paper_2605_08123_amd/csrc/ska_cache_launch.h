@@ -14,7 +14,3 @@ SKA_DECLARE_CACHE_D(ska_launch_cache_e4m3_f32);
 SKA_DECLARE_CACHE_D(ska_launch_cache_e4m3_bf16);
 SKA_DECLARE_CACHE_D(ska_launch_cache_int8_f32);
 SKA_DECLARE_CACHE_D(ska_launch_cache_int8_bf16);
-
-// Most blocks of rows of a wavefront: what it has registers for, and two in fp32, whose products take the time of all rows however they are
-// dealt (64 items behind 60000, d = 64: 52 us, with four 53)
-constexpr int ca_most(bool wide_store, int d) { return wide_store || d == 128 ? 2 : 4; }

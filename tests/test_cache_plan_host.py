@@ -1,14 +1,22 @@
 """How attention on caches is launched (compiled for the host; no GPU)."""
 import os
 import subprocess
+from typing import NamedTuple
+
+import pytest
+
+import paper_2605_08123_amd as ska
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-CSRC = os.path.join(os.path.dirname(HERE), "paper_2605_08123_amd", "csrc")
+ROOT = os.path.dirname(HERE)
+CSRC = os.path.join(ROOT, "paper_2605_08123_amd", "csrc")
+ALL = 1 << 20
+F32, BF16, E4M3, INT8 = 0, 1, 2, 3
 
 
 def build(tmp_path, name):
     exe = str(tmp_path / name)
-    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", CSRC, "-o", exe, os.path.join(HERE, name + ".cpp")], check=True)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", CSRC, "-I", os.path.join(ROOT, "include"), "-o", exe, os.path.join(HERE, name + ".cpp")], check=True)
     return exe
 
 
@@ -17,3 +25,46 @@ def test_joins_within_32_bits_of_threads(tmp_path):
     run = subprocess.run([build(tmp_path, "cache_joins")], capture_output=True, text=True)
     print(run.stdout)
     assert run.returncode == 0, run.stdout
+
+
+class Plan(NamedTuple):
+    both: int         # an item's workgroups take the prefix too
+    nq: int           # blocks of 16 rows of a workgroup
+    own_parts: int
+    front_parts: int  # 0: the prefix has no workgroups
+    last_first: int
+    own_wgs: int
+    front_wgs: int
+
+
+@pytest.fixture(scope="session")
+def plans(tmp_path_factory):
+    """Plans of problems (B, Hq, Hk, Lq, Lp, Lk, d, W, causal, dtype, store); Lp 0: no prefix."""
+    exe = build(tmp_path_factory.mktemp("plans"), "cache_plans")
+
+    def ask(problems):
+        run = subprocess.run([exe], input="\n".join(" ".join(str(int(x)) for x in p) for p in problems), capture_output=True, text=True, check=True)
+        return [Plan(*(int(x) for x in line.split()[:7])) for line in run.stdout.splitlines()]
+    return ask
+
+
+@pytest.mark.parametrize("dtype,store", [(BF16, BF16), (BF16, E4M3), (BF16, INT8), (F32, INT8)])
+def test_large_problems_behind_a_prefix_take_64_rows(dtype, store, plans):
+    """Rounds of workgroups count: half as many of twice the rows take less time."""
+    sizes = [(16, 8, 2, 2048, 16384, 4096), (64, 8, 2, 128, 65536, 256), (16, 8, 2, 512, 16384, 1024), (16, 8, 2, 400, 300, 400), (2, 16, 2, 700, 2000, 3000)]
+    for p in plans([(*s, 64, ALL, 1, dtype, store) for s in sizes]):
+        assert p.nq == 4 and not p.both
+    for p in plans([(*s, 128, ALL, 1, dtype, store) for s in sizes]):
+        assert p.nq == 2
+    # a few rows of many items, short walks: 32
+    for p in plans([(64, 8, 4, 4, 8000, 300, 64, ALL, 1, dtype, store), (16, 8, 2, 1, 1800, 30, 64, ALL, 1, dtype, store)]):
+        assert p.nq == 2
+
+
+@pytest.mark.parametrize("dtype,store,d", [(BF16, BF16, 32), (BF16, BF16, 64), (BF16, E4M3, 32), (BF16, INT8, 64), (F32, E4M3, 32), (F32, INT8, 64)])
+def test_blocks_of_64_rows_up_to_the_headers_limit(dtype, store, d):
+    """Own and prefix's blocks of 64 rows, fewer than 2^23 - 8 together, are taken (of 32 rows there would be more)."""
+    need = lambda Hk: ska.ska_prefix_attn_workspace_bytes(1, 4 * Hk, Hk, 1 << 24, 64, 64, d, ALL, True, dtype, store)   # noqa: E731
+    for Hk in (1, 2, 3):   # 2 Hk 2^20 blocks
+        assert need(Hk) > 0, Hk
+    assert need(4) == 0
