@@ -7,6 +7,10 @@ import pytest
 
 import paper_2605_08123_amd as ska
 
+from . import test_gpu_cache as small
+from . import test_gpu_cache_ends as ends
+from . import test_gpu_cache_rows as rows
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(ROOT, "paper_2605_08123_amd", "csrc")
@@ -68,3 +72,35 @@ def test_blocks_of_64_rows_up_to_the_headers_limit(dtype, store, d):
     for Hk in (1, 2, 3):   # 2 Hk 2^20 blocks
         assert need(Hk) > 0, Hk
     assert need(4) == 0
+
+
+def code(kind):
+    """dtype, store of the C ABI of ("e4m3", torch.bfloat16) and the like."""
+    dtype = F32 if kind[1] == small.F32 else BF16
+    return dtype, {"same": dtype, "e4m3": E4M3, "int8": INT8}[kind[0]]
+
+
+def cache(shape, kind):
+    return (*shape[:4], 0, *shape[4:8], *code(kind))
+
+
+def prefix(shape, kind):
+    return (*shape[:9], *code(kind))
+
+
+def test_which_workgroups_the_gpu_tests_reach(plans):
+    """The tests of 64 rows take them, in one part and in several, blocks in either order; those of small problems the other two forms."""
+    one = plans([cache(s, k) for s in rows.ROWS for k in rows.CODES])
+    assert all(p.nq == 4 and p.own_parts == 1 for p in one) and {p.last_first for p in one} == {0, 1}
+    several = plans([cache(s, k) for s, k in rows.PARTS])
+    assert all(p.nq == 4 and p.own_parts > 1 for p in several) and {p.last_first for p in several} == {0, 1}
+    one = plans([prefix(s, k) for s in rows.PREFIX for k in rows.KINDS[1:]])
+    assert all(p.nq == 4 and p.front_parts == p.own_parts == 1 for p in one)
+    assert all(p.nq == 4 and p.front_parts > 1 for p in plans([prefix(s, k) for s, k in rows.PREFIX_PARTS]))
+    one = plans([prefix(s, k) for s in small.PREFIX for k in rows.KINDS])
+    assert {p.both for p in one} == {0, 1} and all(p.nq == (1 if p.both else 2) for p in one) and any(p.front_parts > 1 for p in one)
+    one = plans([cache(s, k) for s in small.ATTN for k in rows.CODES])
+    assert all(p.nq == 2 for p in one) and any(p.own_parts > 1 for p in one)
+    Lq, Lk, d = ends.CLIMB[-1]
+    one = plans([cache((1, 2, 1, Lq, Lk, d, ALL, 1), k) for k in rows.CODES] + [prefix((1, 2, 1, Lq, 1, Lk, d, ALL, 1), ("same", small.BF16))])
+    assert all(p.nq == 4 for p in one)

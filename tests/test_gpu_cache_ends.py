@@ -12,10 +12,11 @@ from .layer_ref import check, pairs
 from .test_gpu_cache import ALL, BF16, F32, cache_of, ints, kept, say
 
 pytestmark = pytest.mark.gpu
+CLIMB = [(1, 300, 64), (1, 2600, 32), (40, 300, 128), (70, 530, 64), (8000, 300, 64)]   # (the last: workgroups of 64 rows)
 
 
 @pytest.mark.parametrize("store,dtype", [("same", F32), ("same", BF16), ("e4m3", F32), ("e4m3", BF16), ("int8", F32), ("int8", BF16)])
-@pytest.mark.parametrize("Lq,Lk,d", [(1, 300, 64), (1, 2600, 32), (40, 300, 128), (70, 530, 64)])
+@pytest.mark.parametrize("Lq,Lk,d", CLIMB)
 @pytest.mark.parametrize("climb", [11.5, 15.5])
 def test_scores_that_climb_beside_large_values(Lq, Lk, d, climb, store, dtype):
     """Scores of 0 in each wavefront's first tile, and `climb` powers of two above them behind it; values as large as the header says: 2^127
