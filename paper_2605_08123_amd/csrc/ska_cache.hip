@@ -350,7 +350,16 @@ int attn(const CaProblem &p, const void *Q, const ska_strides *q_strides, const 
     if ((rc = tensor_of(a.q, Q, q_strides, p.B, p.Hq, p.Lq, p.d, p.dtype, 16, false)) != SKA_OK) return rc;
     if ((rc = tensor_of(a.o, O, o_strides, p.B, p.Hq, p.Lq, p.d, p.dtype, 16, true)) != SKA_OK) return rc;
     if ((rc = side_of(a.side[0], own, p.B, p.Hk, p.Lk, p.d, p.store)) != SKA_OK) return rc;
-    if (prefix && (rc = side_of(a.side[1], *prefix, 1, p.Hk, p.Lp, p.d, p.store)) != SKA_OK) return rc;
+    if (prefix) {
+        CaKept one = *prefix;   // (its strides between items say nothing)
+        ska_strides k, v;
+        ska_scale_strides ks, vs;
+        if (one.ks) k = *one.ks, k.b = 0, one.ks = &k;
+        if (one.vs) v = *one.vs, v.b = 0, one.vs = &v;
+        if (one.kss) ks = *one.kss, ks.b = 0, one.kss = &ks;
+        if (one.vss) vs = *one.vss, vs.b = 0, one.vss = &vs;
+        if ((rc = side_of(a.side[1], one, 1, p.Hk, p.Lp, p.d, p.store)) != SKA_OK) return rc;
+    }
     a.parts = l.parts;
     const size_t need = ws_bytes(p, l.parts);
     if (need && (!workspace || workspace_bytes < need)) return SKA_EWORKSPACE;
