@@ -64,12 +64,11 @@ int ska_cache_read(const void *Kc, const ska_strides *kc_strides, const float *K
  *   below 2^-18, so that keys with less weight than that add nothing to O).  Values' scales are
  *   fp16 numbers next to a power of two, and their products with it rounded to fp16 again (3 2^-11 in all; absolute 2^-20 of the
  *   value); in 32 tokens with a scale 2^9 times smaller than a value's before, the products are sums of two bf16 numbers (2^-16).
- *   Values 2^100 times smaller than another that is reached may be lost.
+ *   Values 2^100 times smaller than another that is reached may be lost, and so may keys with less than 2^-100 of the largest weight in O.
  *   Values up to 2^127 / (n + 64), n the tokens that a query reaches by position, give finite results: sums over them, not yet divided by those
  *   of exp(S - m), are fp32.
  *   Places of the cache beyond the lengths or inactive may hold anything, and so may those that no query of the item reaches by
- *   position (inactive ones reach as well).  A token that is reached whose value row is NaN (or a product exp(S - LSE) s' beyond
- *   fp32) is in O of the queries around it too.
+ *   position (inactive ones reach as well).  A token that is reached whose value row is not finite is in O of the queries around it too.
  *   Limits, alignment and workspace as ska_softmax_attn_fwd (codes: multiples of 16 bytes); scales on any 4 bytes.  Instead of its
  *   2^24 blocks of 128 rows: fewer than 2^23 - 8 blocks of 64 query rows of a problem (32 on fp32 caches or with d = 128), B Hk problems
  *   of Lq (Hq / Hk) rows (SKA_EUNSUPPORTED otherwise).
@@ -90,7 +89,7 @@ int ska_cache_attn_fwd(const void *Q, const ska_strides *q_strides, const void *
  *   Kp, Vp [Hk,Lp,d] (of their strides, h and l count), K, V [B,Hk,Lk,d]: all of type `store`, which is `dtype` (scales NULL) or an
  *   8-bit one (scales Kps, Vps, Ks, Vs).  mask_p [Lp]: uint8, nonzero = active, or NULL.  The other arguments as above.
  *   Places of the prefix beyond P or inactive may hold anything, and so may those that no query of any item reaches by position.
- *   fp32 caches: products in fp32.  bf16: exp(S - m) as the sum of two bf16 numbers (2^-16).  Codes: as above.
+ *   fp32 caches: products in fp32.  bf16: exp(S - m) as the sum of two bf16 numbers (2^-16), from which the row's sum is taken too.  Codes: as above.
  *   1 <= Lp, Lk <= 2^24 (an item without tokens of its own: len_k 0), B * Lq * (Hq / Hk) <= 2^27; the prefix's blocks, of Hk
  *   problems of B Lq (Hq / Hk) rows, count with the items' own (SKA_EUNSUPPORTED otherwise).
  */

@@ -14,10 +14,12 @@
 // Codes in 8 bits are exact in bf16 and in fp16.  A key's scale is a factor of its score, a value's scale one of its P.
 //
 // What bounds it, in us of the kernel alone: few rows, memory (a token of 8 items, 16 heads on 4 of d = 128, int8 caches of 32768: 46, 4.5 TB/s; four
-// items, 8 heads on 2 of d = 64, e4m3, 65536: 14.9, 3.6 TB/s, of which about 5 are the first loads' and the last sums' latency).  Many rows,
-// vector instructions (2048 tokens of 8 heads on 2, d = 64, 16384 keys in e4m3: 71; a wavefront issues 187 of
-// them beside the 32 products of a tile of 32 keys and 64 rows: 115 for P, 40 that turn codes into operands, 16 for the values' scales; they take 55 % of
-// the time, products 24 %, with two wavefronts to a SIMD).  One look at a tile decides for all blocks whether a maximum moves (a maximum per tile and block: 81).
+// items, 8 heads on 2 of d = 64, e4m3, 65536: 14.6, 3.7 TB/s, of which about 5 are the first loads' and the last sums' latency).  Many rows,
+// vector instructions and products, which do not cover each other (2048 tokens of 8 heads on 2, d = 64, 16384 keys in e4m3: 71; a wavefront issues 187 of
+// the former beside the 32 products of a tile of 32 keys and 64 rows: 115 for P, 40 that turn codes into operands, 16 for the values' scales; they take 65 %
+// of the time that a CU is busy, products 28 %, with two wavefronts to a SIMD).  fp32 queries: six products for two (the same 142: 58 % and 41 %).  One look at
+// a tile decides for all blocks whether a maximum moves (a maximum per tile and block: 81).  bf16 caches, d = 128, 32 rows: the only instance
+// that does not fit its registers (24 spilled; two tokens of 64 items, 2 heads on 1, 216039 shared keys: 78).
 #pragma once
 #include "ska_cache_plan.h"
 #include "ska_softmax.h"
